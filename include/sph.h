@@ -365,6 +365,145 @@ int sph_gcm_open_segments(sph_gcm_key key, const sph_gcm_segment* segments, int 
                           void* stream);
 
 /*
+ * Paged 4-bit key/value cache.  The decoder that produces the hidden states
+ * runs the same windows as the calls above: each of n_sessions sessions has
+ * up to R rows (a verification window of k + 1 rows, or a prompt), the last
+ * ones of its text.  One step is sph_pages_grow, then per layer
+ * sph_kv_append and sph_kv_attend, then the head and its verification, then
+ * sph_pages_trim to the accepted length.
+ *
+ * Format: each key or value vector of head_dim values is held as E2M1 codes
+ * with an E8M0 scale for 32 of them (OCP microscaling FP4): 2^e with
+ * e = floor(log2 m) - 2, m the group's largest magnitude rounded to two
+ * significant bits (ties to even), e clamped to [-127, 125]; a code is the
+ * nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 to |x| 2^-e (ties to even).  A token
+ * whose key or value has an infinity or a NaN is held so that every row that
+ * sees it answers NaN and no other row does.  17 bits for 32 values: a token
+ * of one head is 2 * head_dim * 17/32 bytes.  How a page orders its bytes is
+ * the library's matter; pages may be copied whole.
+ *
+ * The pool holds n_pages pages of page_tokens tokens of all key/value heads
+ * for each layer, and one table for all layers: entry i of a slot's row names
+ * the page of its tokens i * page_tokens ...  A slot is a session's place in
+ * the tables.  lens[slot] tokens are held.  refs[page] counts the slots that
+ * hold a page; a page is free while it is 0.  Start with refs and lens zero
+ * and the table -1.
+ */
+typedef struct {
+  void* pool;            /* device, 16-byte aligned */
+  int64_t layers;        /* >= 1 */
+  int64_t layer_stride;  /* bytes, a multiple of 16 */
+  int64_t n_pages;       /* 1 ... 2^31 - 1 */
+  int64_t page_stride;   /* bytes, a multiple of 16, >= sph_kv_page_bytes */
+  int32_t* table;        /* device int32 [n_slots][ld_table] */
+  int64_t ld_table;      /* >= max_pages */
+  int64_t max_pages;     /* >= 1, entries of a slot */
+  int32_t* lens;         /* device int32 [n_slots] */
+  int32_t* refs;         /* device int32 [n_pages]; the sph_pages_* calls only */
+  int64_t n_slots;       /* >= 1 */
+  int32_t kv_heads;      /* 1 ... 65535 */
+  int32_t head_dim;      /* 64, 128 or 256 */
+  int32_t page_tokens;   /* 16, 32, 64, 128 or 256 */
+} sph_kv_cache;
+
+/* kv_heads * page_tokens * head_dim * 17/16, or -1 for sizes outside those. */
+int64_t sph_kv_page_bytes(int kv_heads, int head_dim, int page_tokens);
+
+/*
+ * Sessions of a call: session s is slot slots[s] (device int32 [n_sessions]; s
+ * itself for NULL) and has rows[s] rows (device int32 [n_sessions], cut to
+ * [0, R]; R for NULL).  Its rows are the last of its lens tokens: row r stands
+ * at position lens - rows[s] + r, and is row s * R + r of a call's tensors.
+ * The struct is host memory read during the call; what its device arrays say
+ * is not validated, but slots, pages and positions outside the cache are never
+ * touched: rows there are not stored, read as zeros and seen by no row.
+ * n_sessions <= 65535.
+ */
+
+/* k, v bf16 [n_sessions * R][kv_heads][head_dim] into layer `layer`: rows and
+ * heads k_row, k_head (v_row, v_head) elements apart.  A slot is at most once
+ * in a call, and a page written by one slot at a time (sph_pages_grow sees to
+ * that). */
+int sph_kv_append(const sph_kv_cache* cache, int64_t layer, const void* k, int64_t k_row,
+                  int64_t k_head, const void* v, int64_t v_row, int64_t v_head,
+                  int64_t n_sessions, int64_t R, const int32_t* rows, const int32_t* slots,
+                  void* stream);
+
+/* The same rows back as bf16, the values that the codes stand for (exact);
+ * zeros for the rows past rows[s]. */
+int sph_kv_read(const sph_kv_cache* cache, int64_t layer, void* k, int64_t k_row, int64_t k_head,
+                void* v, int64_t v_row, int64_t v_head, int64_t n_sessions, int64_t R,
+                const int32_t* rows, const int32_t* slots, void* stream);
+
+/*
+ * Attention of each session's rows over its cache:
+ *   x[j]       = scale * sum_i q[row, h, i] K[j, h / G, i],  G = q_heads / kv_heads
+ *   out[row,h] = sum_j softmax(x)[j] V[j, h / G]             (bf16)
+ *   lse[row,h] = log sum_j exp(x[j])                         (fp32)
+ * over the positions j that the row at position p sees: j <= p and, for
+ * window > 0, j > p - window.  A row that sees nothing has out 0 and lse
+ * -infinity, and so have the rows past rows[s].
+ *
+ * q, out      bf16 [n_sessions * R][q_heads][head_dim], rows and heads q_row,
+ *             q_head (o_row, o_head) elements apart
+ * q_heads     a multiple of kv_heads
+ * scale       0 < scale <= 1e6
+ * window      0: none
+ * max_len     the largest of the sessions' lens, as far as the caller knows (0:
+ *             max_pages * page_tokens).  It shares out the work; results are
+ *             right for any, up to the order of sums.
+ * lse_out     fp32 [n_sessions * R][q_heads] or NULL
+ * workspace   >= sph_kv_attend_workspace bytes for the same arguments, 256-byte
+ *             aligned (NULL if that is 0)
+ * Sums, maxima and the softmax are held in fp32; the weights softmax(x) enter
+ * the second product as bf16.
+ */
+size_t sph_kv_attend_workspace(const sph_kv_cache* cache, int64_t q_heads, int64_t n_sessions,
+                               int64_t R, int64_t window, int64_t max_len);
+int sph_kv_attend(const sph_kv_cache* cache, int64_t layer, const void* q, int64_t q_row,
+                  int64_t q_head, int64_t q_heads, int64_t n_sessions, int64_t R,
+                  const int32_t* rows, const int32_t* slots, float scale, int64_t window,
+                  int64_t max_len, void* out, int64_t o_row, int64_t o_head, float* lse_out,
+                  void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Pages.  These calls change table, lens and refs on the device, without the
+ * host: a step can be captured in a graph.  Pages are given out lowest first,
+ * to slots in their order, so results do not depend on timing.
+ *
+ * sph_pages_grow: lens[s] += add[s] (device int32 [n_slots]; negative counts as
+ * 0), with pages for the new tokens.  Where the first of them falls into a page
+ * that others hold too (refs > 1), the slot gets a copy of its own, in every
+ * layer.  status_out (device int32 [2]): pages lacking in the pool, and slots
+ * whose row of max_pages is too short; if either is not 0, nothing has changed.
+ * sph_pages_trim: lens[s] = min(lens[s], max(kept[s], 0)); pages past that are
+ * given back (free once no slot holds them).  kept 0 frees a slot.
+ * sph_pages_fork: slot children[i] gives back what it holds and shares all of
+ * slot parents[i]'s pages and its length (device int32 [n]).  Children are
+ * distinct and no child is a parent in the same call; pairs outside the slots,
+ * or of a slot with itself, are passed over.
+ * sph_pages_copy: page dst[i] becomes a copy of page src[i] in every layer
+ * (device int32 [n]); no page is both, or written twice.  Pages outside the
+ * pool are passed over.
+ * sph_pages_compact: with L live pages (refs > 0), those from place L on move
+ * into the free ones below, both in ascending order.  table_out [n_slots]
+ * [ld_out] (max_pages entries a row) and refs_out [n_pages] say where pages are
+ * now; they may be the cache's own.  live_out (device int32 [1]) = L.
+ */
+size_t sph_pages_grow_workspace(const sph_kv_cache* cache);
+int sph_pages_grow(const sph_kv_cache* cache, const int32_t* add, int32_t* status_out,
+                   void* workspace, size_t ws_bytes, void* stream);
+int sph_pages_trim(const sph_kv_cache* cache, const int32_t* kept, void* stream);
+int sph_pages_fork(const sph_kv_cache* cache, const int32_t* parents, const int32_t* children,
+                   int64_t n, void* stream);
+int sph_pages_copy(const sph_kv_cache* cache, const int32_t* src, const int32_t* dst, int64_t n,
+                   void* stream);
+size_t sph_pages_compact_workspace(const sph_kv_cache* cache);
+int sph_pages_compact(const sph_kv_cache* cache, int32_t* table_out, int64_t ld_out,
+                      int32_t* refs_out, int32_t* live_out, void* workspace, size_t ws_bytes,
+                      void* stream);
+
+/*
  * Kernel tracing.  While a trace is active, each call records one duration
  * per kernel it launches: start and stop HIP events are attached to the
  * kernel dispatches themselves (hipExtLaunchKernelGGL), so a duration is

@@ -26,6 +26,17 @@ from .api import (  # noqa: F401
     gcm_workspace,
     fuse_verify_hq,
     fuse_verify_hq_workspace,
+    KvCache,
+    kv_append,
+    kv_attend,
+    kv_attend_workspace,
+    kv_page_bytes,
+    kv_read,
+    pages_compact,
+    pages_copy,
+    pages_fork,
+    pages_grow,
+    pages_trim,
     payload_scale_count,
     probe_mfma,
     probe_read,

@@ -98,6 +98,34 @@ SIGNATURES = {
         c_vp, c_vp, c_i64, c_i64,           # iv, aad, ld_aad, aad_bytes
         c_vp, c_vp,                         # tag, ok_out
         c_vp, ctypes.c_size_t, c_vp]),      # workspace, ws_bytes, stream
+    "sph_kv_page_bytes": (c_i64, [ctypes.c_int, ctypes.c_int, ctypes.c_int]),
+    "sph_kv_append": (ctypes.c_int, [
+        c_vp, c_i64,                        # cache, layer
+        c_vp, c_i64, c_i64,                 # k, k_row, k_head
+        c_vp, c_i64, c_i64,                 # v, v_row, v_head
+        c_i64, c_i64, c_vp, c_vp, c_vp]),   # n_sessions, R, rows, slots, stream
+    "sph_kv_read": (ctypes.c_int, [
+        c_vp, c_i64,                        # cache, layer
+        c_vp, c_i64, c_i64,                 # k, k_row, k_head
+        c_vp, c_i64, c_i64,                 # v, v_row, v_head
+        c_i64, c_i64, c_vp, c_vp, c_vp]),   # n_sessions, R, rows, slots, stream
+    "sph_kv_attend_workspace": (ctypes.c_size_t, [c_vp, c_i64, c_i64, c_i64, c_i64, c_i64]),
+    "sph_kv_attend": (ctypes.c_int, [
+        c_vp, c_i64,                        # cache, layer
+        c_vp, c_i64, c_i64, c_i64,          # q, q_row, q_head, q_heads
+        c_i64, c_i64, c_vp, c_vp,           # n_sessions, R, rows, slots
+        ctypes.c_float, c_i64, c_i64,       # scale, window, max_len
+        c_vp, c_i64, c_i64, c_vp,           # out, o_row, o_head, lse_out
+        c_vp, ctypes.c_size_t, c_vp]),      # workspace, ws_bytes, stream
+    "sph_pages_grow_workspace": (ctypes.c_size_t, [c_vp]),
+    "sph_pages_grow": (ctypes.c_int, [c_vp, c_vp, c_vp, c_vp, ctypes.c_size_t, c_vp]),
+    "sph_pages_trim": (ctypes.c_int, [c_vp, c_vp, c_vp]),
+    "sph_pages_fork": (ctypes.c_int, [c_vp, c_vp, c_vp, c_i64, c_vp]),
+    "sph_pages_copy": (ctypes.c_int, [c_vp, c_vp, c_vp, c_i64, c_vp]),
+    "sph_pages_compact_workspace": (ctypes.c_size_t, [c_vp]),
+    "sph_pages_compact": (ctypes.c_int, [
+        c_vp, c_vp, c_i64, c_vp, c_vp,      # cache, table_out, ld_out, refs_out, live_out
+        c_vp, ctypes.c_size_t, c_vp]),      # workspace, ws_bytes, stream
     "sph_trace_start": (ctypes.c_int, [ctypes.c_int]),
     "sph_trace_stop": (ctypes.c_int, [c_vp, ctypes.c_int, ctypes.POINTER(ctypes.c_int)]),
     # include/sph_probe.h
@@ -114,6 +142,14 @@ class GcmSegment(ctypes.Structure):
     """sph_gcm_segment."""
     _fields_ = [("in_", c_vp), ("ld_in", c_i64), ("out", c_vp), ("ld_out", c_i64),
                 ("bytes", c_i64)]
+
+
+class KvCacheStruct(ctypes.Structure):
+    """sph_kv_cache."""
+    _fields_ = [("pool", c_vp), ("layers", c_i64), ("layer_stride", c_i64), ("n_pages", c_i64),
+                ("page_stride", c_i64), ("table", c_vp), ("ld_table", c_i64), ("max_pages", c_i64),
+                ("lens", c_vp), ("refs", c_vp), ("n_slots", c_i64), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_tokens", ctypes.c_int32)]
 
 
 SPH_GCM_MAX_SEGMENTS = 4

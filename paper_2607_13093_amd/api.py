@@ -470,6 +470,230 @@ def fuse_verify_hq(q: torch.Tensor, scale: torch.Tensor, hq: torch.Tensor, h_sca
     return tokens, accept, fused
 
 
+class KvCache:
+    """A paged 4-bit key/value cache (include/sph.h) on tensors of the caller:
+
+    pool  uint8 [layers, pages, >= kv_page_bytes], pages contiguous
+    table int32 [slots, max_pages], -1 where there is no page
+    lens  int32 [slots] tokens held, refs int32 [pages] slots that hold a page
+
+    The tensors are kept alive, and changed in place by the calls below."""
+
+    def __init__(self, pool: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, refs: torch.Tensor,
+                 kv_heads: int, head_dim: int, page_tokens: int):
+        import ctypes
+        for name, t, dims, dtype in (("pool", pool, 3, torch.uint8), ("table", table, 2, torch.int32),
+                                     ("lens", lens, 1, torch.int32), ("refs", refs, 1, torch.int32)):
+            _require_gpu(name, t)
+            if t.dtype != dtype or t.dim() != dims or t.device != pool.device:
+                raise ValueError(f"{name}: expected {dtype} with {dims} dimensions on the pool's device, "
+                                 f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+        need = kv_page_bytes(kv_heads, head_dim, page_tokens)
+        if pool.shape[2] < need:
+            raise ValueError(f"pool: pages of {pool.shape[2]} bytes, need {need}")
+        if lens.shape[0] != table.shape[0] or refs.shape[0] != pool.shape[1]:
+            raise ValueError(f"lens {tuple(lens.shape)} and refs {tuple(refs.shape)} do not fit table "
+                             f"{tuple(table.shape)} and pool {tuple(pool.shape)}")
+        self.pool, self.table, self.lens, self.refs = pool, table, lens, refs
+        self.kv_heads, self.head_dim, self.page_tokens = int(kv_heads), int(head_dim), int(page_tokens)
+        self.layers, self.n_pages, self.n_slots = pool.shape[0], pool.shape[1], table.shape[0]
+        self.device = pool.device
+        self._struct = _lib.KvCacheStruct(
+            pool.data_ptr(), pool.shape[0], pool.stride(0), pool.shape[1], pool.stride(1),
+            table.data_ptr(), table.stride(0), table.shape[1], lens.data_ptr(), refs.data_ptr(),
+            table.shape[0], self.kv_heads, self.head_dim, self.page_tokens)
+        self.ptr = ctypes.addressof(self._struct)
+
+    @classmethod
+    def empty(cls, layers: int, n_pages: int, n_slots: int, max_pages: int, kv_heads: int,
+              head_dim: int, page_tokens: int, device=None) -> "KvCache":
+        """An empty cache with tensors of its own."""
+        dev = torch.device("cuda") if device is None else torch.device(device)
+        nb = kv_page_bytes(kv_heads, head_dim, page_tokens)
+        return cls(torch.empty((layers, n_pages, nb), dtype=torch.uint8, device=dev),
+                   torch.full((n_slots, max_pages), -1, dtype=torch.int32, device=dev),
+                   torch.zeros((n_slots,), dtype=torch.int32, device=dev),
+                   torch.zeros((n_pages,), dtype=torch.int32, device=dev), kv_heads, head_dim, page_tokens)
+
+
+def kv_page_bytes(kv_heads: int, head_dim: int, page_tokens: int) -> int:
+    """Bytes of one page of one layer (include/sph.h)."""
+    n = int(_lib.load().sph_kv_page_bytes(int(kv_heads), int(head_dim), int(page_tokens)))
+    if n < 0:
+        raise SphError(_lib.SPH_E_UNSUPPORTED, f"no cache of kv_heads={kv_heads} head_dim={head_dim} "
+                                               f"page_tokens={page_tokens}")
+    return n
+
+
+def _kv_rows(name: str, t: torch.Tensor, heads: Optional[int], d: int, device):
+    """Row and head strides of a bf16 [M, heads, d] tensor."""
+    shape = t.shape
+    if t.dtype != torch.bfloat16 or len(shape) != 3 or shape[2] != d or (heads is not None and shape[1] != heads):
+        raise ValueError(f"{name}: expected bf16 [rows, {'heads' if heads is None else heads}, {d}], "
+                         f"got {t.dtype} {tuple(shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the cache on {device}")
+    row, head, one = t.stride()
+    if one != 1:
+        raise ValueError(f"{name} must be contiguous along its last dimension")
+    # strides of axes of length one or none mean nothing
+    return row if shape[0] > 1 else max(row, d), head if shape[1] > 1 else max(head, d)
+
+
+def _kv_ints(name: str, t: Optional[torch.Tensor], n: int, device) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.shape != (n,) or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected contiguous int32 ({n},) on {device}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _kv_sessions(M: int, R: int) -> int:
+    if R < 1 or M % R != 0:
+        raise ValueError(f"{M} rows are no whole number of sessions of {R}")
+    return M // R
+
+
+def kv_append(cache: KvCache, layer: int, k: torch.Tensor, v: torch.Tensor, rows_per_session: int,
+              rows: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None) -> None:
+    """Quantise the rows k, v bf16 [sessions * R, kv_heads, head_dim] (rows and
+    heads may be strided) into their pages: row r of a session stands at position
+    lens - rows + r of its slot, so pages_grow comes first.  rows int32
+    [sessions]: rows of each (R if None); slots int32 [sessions]: where each is
+    (0, 1, ... if None)."""
+    R, dev = int(rows_per_session), cache.device
+    ks = _kv_rows("k", k, cache.kv_heads, cache.head_dim, dev)
+    vs = _kv_rows("v", v, cache.kv_heads, cache.head_dim, dev)
+    if k.shape[0] != v.shape[0]:
+        raise ValueError(f"k has {k.shape[0]} rows, v {v.shape[0]}")
+    n = _kv_sessions(k.shape[0], R)
+    check(_lib.load().sph_kv_append(cache.ptr, int(layer), k.data_ptr(), *ks, v.data_ptr(), *vs, n, R,
+                                    _kv_ints("rows", rows, n, dev), _kv_ints("slots", slots, n, dev),
+                                    _stream_handle(dev)))
+
+
+def kv_read(cache: KvCache, layer: int, rows_per_session: int, rows: Optional[torch.Tensor] = None,
+            slots: Optional[torch.Tensor] = None, n_sessions: Optional[int] = None, out=None):
+    """The same rows as the values that the cache holds: (k, v) bf16 [sessions *
+    R, kv_heads, head_dim], zeros past a session's rows.  n_sessions: all slots
+    (or all of `rows` or `slots`) if None."""
+    R, dev = int(rows_per_session), cache.device
+    n = n_sessions
+    if n is None:
+        given = rows if rows is not None else slots
+        n = cache.n_slots if given is None else given.shape[0]
+    if out is None:
+        shape = (int(n) * R, cache.kv_heads, cache.head_dim)
+        out = (torch.empty(shape, dtype=torch.bfloat16, device=dev),
+               torch.empty(shape, dtype=torch.bfloat16, device=dev))
+    k, v = out
+    ks = _kv_rows("k", k, cache.kv_heads, cache.head_dim, dev)
+    vs = _kv_rows("v", v, cache.kv_heads, cache.head_dim, dev)
+    if k.shape[0] != n * R or v.shape[0] != n * R:
+        raise ValueError(f"out: expected {n * R} rows, got {k.shape[0]} and {v.shape[0]}")
+    check(_lib.load().sph_kv_read(cache.ptr, int(layer), k.data_ptr(), *ks, v.data_ptr(), *vs, int(n), R,
+                                  _kv_ints("rows", rows, n, dev), _kv_ints("slots", slots, n, dev),
+                                  _stream_handle(dev)))
+    return k, v
+
+
+def kv_attend_workspace(cache: KvCache, q_heads: int, n_sessions: int, rows_per_session: int,
+                        window: int = 0, max_len: int = 0) -> int:
+    return int(_lib.load().sph_kv_attend_workspace(cache.ptr, int(q_heads), int(n_sessions),
+                                                   int(rows_per_session), int(window), int(max_len)))
+
+
+def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, rows_per_session: int, scale: float,
+              rows: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None, window: int = 0,
+              max_len: int = 0, want_lse: bool = False, workspace: Optional[torch.Tensor] = None, out=None):
+    """Attention of each session's last rows over its cache, the rows' own tokens
+    among it (kv_append comes first).  q bf16 [sessions * R, q_heads, head_dim]
+    (rows and heads may be strided), q_heads a multiple of kv_heads.  Returns
+    (out bf16 [sessions * R, q_heads, head_dim], log-sum-exp fp32 [sessions * R,
+    q_heads] or None).  max_len: the longest session, if the caller knows it (the
+    work is shared out better); window: positions a row sees (0: all before it)."""
+    lib = _lib.load()
+    R, dev = int(rows_per_session), cache.device
+    qs = _kv_rows("q", q, None, cache.head_dim, dev)
+    M, heads = q.shape[0], q.shape[1]
+    n = _kv_sessions(M, R)
+    if out is None:
+        out = (torch.empty((M, heads, cache.head_dim), dtype=torch.bfloat16, device=dev),
+               torch.empty((M, heads), dtype=torch.float32, device=dev) if want_lse else None)
+    o, lse = out
+    os = _kv_rows("out", o, heads, cache.head_dim, dev)
+    if o.shape[0] != M:
+        raise ValueError(f"out: expected {M} rows, got {o.shape[0]}")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (M, heads) or not lse.is_contiguous()
+                            or lse.device != dev):
+        raise ValueError(f"lse: expected contiguous float32 ({M}, {heads}) on {dev}")
+    if workspace is None:
+        need = kv_attend_workspace(cache, heads, n, R, window, max_len)
+        if need > 0:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    check(lib.sph_kv_attend(cache.ptr, int(layer), q.data_ptr(), *qs, heads, n, R,
+                            _kv_ints("rows", rows, n, dev), _kv_ints("slots", slots, n, dev),
+                            float(scale), int(window), int(max_len), o.data_ptr(), *os, _ptr(lse),
+                            _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                            _stream_handle(dev)))
+    return o, lse
+
+
+def pages_grow(cache: KvCache, add: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """lens += add (int32 [slots]), with pages for the new tokens; a shared page
+    that they begin in is copied first.  Returns the status, int32 [2]: pages
+    lacking in the pool, slots whose row is too short; if either is not 0,
+    nothing has changed."""
+    lib = _lib.load()
+    dev = cache.device
+    status = torch.empty(2, dtype=torch.int32, device=dev) if out is None else out
+    if workspace is None:
+        workspace = torch.empty(lib.sph_pages_grow_workspace(cache.ptr), dtype=torch.uint8, device=dev)
+    check(lib.sph_pages_grow(cache.ptr, _kv_ints("add", add, cache.n_slots, dev), _kv_ints("out", status, 2, dev),
+                             workspace.data_ptr(), workspace.numel(), _stream_handle(dev)))
+    return status
+
+
+def pages_trim(cache: KvCache, kept: torch.Tensor) -> None:
+    """lens = min(lens, kept) (int32 [slots]); pages past that are given back."""
+    dev = cache.device
+    check(_lib.load().sph_pages_trim(cache.ptr, _kv_ints("kept", kept, cache.n_slots, dev), _stream_handle(dev)))
+
+
+def pages_fork(cache: KvCache, parents: torch.Tensor, children: torch.Tensor) -> None:
+    """Slots children[i] give back what they hold and share the pages of slots
+    parents[i] (int32 [n]; children distinct, none of them a parent)."""
+    n, dev = parents.shape[0], cache.device
+    check(_lib.load().sph_pages_fork(cache.ptr, _kv_ints("parents", parents, n, dev),
+                                     _kv_ints("children", children, n, dev), n, _stream_handle(dev)))
+
+
+def pages_copy(cache: KvCache, src: torch.Tensor, dst: torch.Tensor) -> None:
+    """Pages dst[i] become copies of pages src[i] in every layer (int32 [n])."""
+    n, dev = src.shape[0], cache.device
+    check(_lib.load().sph_pages_copy(cache.ptr, _kv_ints("src", src, n, dev), _kv_ints("dst", dst, n, dev), n,
+                                     _stream_handle(dev)))
+
+
+def pages_compact(cache: KvCache, out=None, workspace: Optional[torch.Tensor] = None):
+    """Move the live pages to the front of the pool.  Returns (table, refs, live
+    int32 [1]): the cache's own, changed in place, or `out` = (table, refs)."""
+    lib = _lib.load()
+    dev = cache.device
+    table, refs = (cache.table, cache.refs) if out is None else out
+    _require_gpu("table", table)
+    if table.dtype != torch.int32 or table.shape != cache.table.shape or table.device != dev:
+        raise ValueError(f"table: expected int32 {tuple(cache.table.shape)} on {dev}")
+    live = torch.empty(1, dtype=torch.int32, device=dev)
+    if workspace is None:
+        workspace = torch.empty(lib.sph_pages_compact_workspace(cache.ptr), dtype=torch.uint8, device=dev)
+    check(lib.sph_pages_compact(cache.ptr, table.data_ptr(), table.stride(0), _kv_ints("refs", refs, cache.n_pages, dev),
+                                live.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_handle(dev)))
+    return table, refs, live
+
+
 def debug_sync(enable: Optional[bool] = None) -> bool:
     """Switch the library's debug synchronisation (a stream synchronisation
     and error check after every kernel launch region) on or off; None only

@@ -15,6 +15,7 @@
 #include "sph.h"
 #include "sph_probe.h"
 #include "sph_internal.h"
+#include "kv_cache.h"
 
 struct sph_subset_s {
   int32_t* d_ids;   // device int32 [n], strictly ascending
@@ -852,6 +853,285 @@ int sph_gcm_open_segments(sph_gcm_key key, const sph_gcm_segment* segments, int 
                           void* stream) {
   return gcm_call("sph_gcm_open_segments", true, key, segments, nseg, rows, iv, aad, ld_aad, aad_bytes,
                   const_cast<uint8_t*>(tag), ok_out, workspace, ws_bytes, stream);
+}
+
+namespace {
+
+constexpr int64_t kMaxSessions = 65535;
+
+bool kv_sizes_ok(int64_t heads, int64_t d, int64_t page) {
+  return heads >= 1 && heads <= 65535 && (d == 64 || d == 128 || d == 256) &&
+         (page == 16 || page == 32 || page == 64 || page == 128 || page == 256);
+}
+
+// Checks a cache description; `pages`: for the calls that keep its counts.
+int kv_check(const char* fn, const sph_kv_cache* c, bool pages) {
+  if (!c) return fail(SPH_E_INVALID_ARG, "%s: cache is NULL", fn);
+  if (!kv_sizes_ok(c->kv_heads, c->head_dim, c->page_tokens))
+    return fail(c->kv_heads < 1 || c->head_dim < 1 || c->page_tokens < 1 ? SPH_E_INVALID_ARG : SPH_E_UNSUPPORTED,
+                "%s: kv_heads=%d head_dim=%d page_tokens=%d (head_dim 64, 128 or 256, pages of 16 ... 256 tokens)",
+                fn, c->kv_heads, c->head_dim, c->page_tokens);
+  if (c->n_pages < 1 || c->n_pages > kMaxIds || c->layers < 1 || c->layers > kMaxIds)
+    return fail(SPH_E_INVALID_ARG, "%s: n_pages=%lld layers=%lld", fn, (long long)c->n_pages, (long long)c->layers);
+  if (c->max_pages < 1 || c->max_pages > kMaxIds || c->ld_table < c->max_pages || c->n_slots < 1 || c->n_slots > kMaxIds)
+    return fail(SPH_E_INVALID_ARG, "%s: max_pages=%lld ld_table=%lld n_slots=%lld", fn, (long long)c->max_pages,
+                (long long)c->ld_table, (long long)c->n_slots);
+  const int64_t need = sph_kv_page_bytes(c->kv_heads, c->head_dim, c->page_tokens);
+  if (c->page_stride < need || c->page_stride % 16 != 0 || (c->layers > 1 && c->layer_stride % 16 != 0))
+    return fail(SPH_E_INVALID_ARG, "%s: page_stride=%lld layer_stride=%lld for pages of %lld bytes", fn,
+                (long long)c->page_stride, (long long)c->layer_stride, (long long)need);
+  if (!c->pool || !c->table || !c->lens || (pages && !c->refs))
+    return fail(SPH_E_INVALID_ARG, "%s: pool, table, lens or refs is NULL", fn);
+  if (reinterpret_cast<uintptr_t>(c->pool) & 15)
+    return fail(SPH_E_INVALID_ARG, "%s: pool is not 16-byte aligned", fn);
+  return SPH_OK;
+}
+
+int log2_of(int x) {
+  int n = 0;
+  while ((1 << n) < x) ++n;
+  return n;
+}
+
+// The arguments that the layer calls share.
+int kv_call(const char* fn, const sph_kv_cache* c, int64_t layer, int64_t n_sessions, int64_t R,
+            const int32_t* rows, const int32_t* slots, sph::KvArgs* a) {
+  const int e = kv_check(fn, c, false);
+  if (e != SPH_OK) return e;
+  if (layer < 0 || layer >= c->layers)
+    return fail(SPH_E_INVALID_ARG, "%s: layer=%lld of %lld", fn, (long long)layer, (long long)c->layers);
+  if (n_sessions < 0 || n_sessions > kMaxSessions || R < 0 || R > sph::kKvMost)
+    return fail(SPH_E_INVALID_ARG, "%s: n_sessions=%lld R=%lld", fn, (long long)n_sessions, (long long)R);
+  if (!slots && n_sessions > c->n_slots)
+    return fail(SPH_E_INVALID_ARG, "%s: n_sessions=%lld beyond n_slots=%lld", fn, (long long)n_sessions,
+                (long long)c->n_slots);
+  a->pool = static_cast<uint8_t*>(c->pool) + layer * c->layer_stride;
+  a->page_stride = c->page_stride;
+  a->n_pages = (int)c->n_pages;
+  a->table = c->table;
+  a->ld_table = c->ld_table;
+  a->max_pages = (int)c->max_pages;
+  a->lens = c->lens;
+  a->rows = rows;
+  a->slots = slots;
+  a->n_slots = (int)c->n_slots;
+  a->n_sessions = (int)n_sessions;
+  a->R = (int)R;
+  a->heads = c->kv_heads;
+  a->page_shift = log2_of(c->page_tokens);
+  return SPH_OK;
+}
+
+sph::PagesArgs pages_args(const sph_kv_cache* c) {
+  sph::PagesArgs a;
+  a.pool = static_cast<uint8_t*>(c->pool);
+  a.layer_stride = c->layer_stride;
+  a.page_stride = c->page_stride;
+  a.page_bytes = sph_kv_page_bytes(c->kv_heads, c->head_dim, c->page_tokens);
+  a.layers = (int)c->layers;
+  a.n_pages = (int)c->n_pages;
+  a.table = c->table;
+  a.ld_table = c->ld_table;
+  a.max_pages = (int)c->max_pages;
+  a.lens = c->lens;
+  a.refs = c->refs;
+  a.n_slots = (int)c->n_slots;
+  a.page_shift = log2_of(c->page_tokens);
+  return a;
+}
+
+// Row and head strides of a [rows][heads][d] tensor, in either order.
+bool kv_strides_ok(int64_t row, int64_t head, int64_t heads, int64_t d) {
+  return row >= d && (head >= d || (heads == 1 && head >= 0));
+}
+
+int kv_rows(const char* fn, bool append, const sph_kv_cache* c, int64_t layer, const void* k, int64_t k_row,
+            int64_t k_head, const void* v, int64_t v_row, int64_t v_head, int64_t n_sessions, int64_t R,
+            const int32_t* rows, const int32_t* slots, void* stream) {
+  sph::KvArgs a;
+  const int e = kv_call(fn, c, layer, n_sessions, R, rows, slots, &a);
+  if (e != SPH_OK) return e;
+  if (!kv_strides_ok(k_row, k_head, c->kv_heads, c->head_dim) || !kv_strides_ok(v_row, v_head, c->kv_heads, c->head_dim))
+    return fail(SPH_E_INVALID_ARG, "%s: row and head strides %lld, %lld and %lld, %lld for %d heads of %d", fn,
+                (long long)k_row, (long long)k_head, (long long)v_row, (long long)v_head, c->kv_heads, c->head_dim);
+  if (n_sessions == 0 || R == 0) return ok();
+  if (!k || !v) return fail(SPH_E_INVALID_ARG, "%s: k or v is NULL", fn);
+  hipStream_t s = (hipStream_t)stream;
+  const hipError_t he = traced(append ? "kv_append" : "kv_read", s, [&] {
+    return sph::launch_kv_rows(append, c->head_dim, a, k, k_row, k_head, v, v_row, v_head, s);
+  });
+  if (he != hipSuccess) return hip_fail(he, "cache rows launch");
+  return ok();
+}
+
+// The longest session that the caller vouches for, or that a page row can hold.
+int64_t kv_most(const sph_kv_cache* c, int64_t max_len) {
+  const int64_t most = std::min<int64_t>(c->max_pages * c->page_tokens, sph::kKvMost);
+  return max_len > 0 && max_len < most ? max_len : most;
+}
+
+int pages_ws(const char* fn, const void* workspace, size_t have, size_t need) {
+  if (have < need || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))
+    return fail(SPH_E_WORKSPACE, "%s: workspace %p of %zu bytes, need %zu (aligned)", fn, workspace, have, need);
+  return SPH_OK;
+}
+
+}  // namespace
+
+int64_t sph_kv_page_bytes(int kv_heads, int head_dim, int page_tokens) {
+  if (!kv_sizes_ok(kv_heads, head_dim, page_tokens)) return -1;
+  return (int64_t)kv_heads * page_tokens * head_dim * 17 / 16;
+}
+
+int sph_kv_append(const sph_kv_cache* cache, int64_t layer, const void* k, int64_t k_row,
+                  int64_t k_head, const void* v, int64_t v_row, int64_t v_head,
+                  int64_t n_sessions, int64_t R, const int32_t* rows, const int32_t* slots,
+                  void* stream) {
+  return kv_rows("sph_kv_append", true, cache, layer, k, k_row, k_head, v, v_row, v_head, n_sessions, R, rows,
+                 slots, stream);
+}
+
+int sph_kv_read(const sph_kv_cache* cache, int64_t layer, void* k, int64_t k_row, int64_t k_head,
+                void* v, int64_t v_row, int64_t v_head, int64_t n_sessions, int64_t R,
+                const int32_t* rows, const int32_t* slots, void* stream) {
+  return kv_rows("sph_kv_read", false, cache, layer, k, k_row, k_head, v, v_row, v_head, n_sessions, R, rows,
+                 slots, stream);
+}
+
+size_t sph_kv_attend_workspace(const sph_kv_cache* cache, int64_t q_heads, int64_t n_sessions,
+                               int64_t R, int64_t window, int64_t max_len) {
+  if (!cache || !kv_sizes_ok(cache->kv_heads, cache->head_dim, cache->page_tokens) || q_heads < 1 ||
+      q_heads % cache->kv_heads != 0 || n_sessions < 1 || R < 1 || window < 0 || max_len < 0 || cache->max_pages < 1)
+    return 0;
+  return sph::kv_attend_scratch(cache->head_dim, n_sessions, R, cache->kv_heads, q_heads,
+                                kv_most(cache, max_len), window);
+}
+
+int sph_kv_attend(const sph_kv_cache* cache, int64_t layer, const void* q, int64_t q_row,
+                  int64_t q_head, int64_t q_heads, int64_t n_sessions, int64_t R,
+                  const int32_t* rows, const int32_t* slots, float scale, int64_t window,
+                  int64_t max_len, void* out, int64_t o_row, int64_t o_head, float* lse_out,
+                  void* workspace, size_t ws_bytes, void* stream) {
+  const char* fn = "sph_kv_attend";
+  sph::KvArgs a;
+  const int e = kv_call(fn, cache, layer, n_sessions, R, rows, slots, &a);
+  if (e != SPH_OK) return e;
+  const int64_t d = cache->head_dim;
+  if (q_heads < 1 || q_heads > 65535 || q_heads % cache->kv_heads != 0)
+    return fail(SPH_E_INVALID_ARG, "%s: q_heads=%lld is no multiple of kv_heads=%d", fn, (long long)q_heads,
+                cache->kv_heads);
+  if (!(scale > 0.0f && scale <= 1e6f)) return fail(SPH_E_INVALID_ARG, "%s: scale=%g not in (0, 1e6]", fn, scale);
+  if (window < 0 || max_len < 0)
+    return fail(SPH_E_INVALID_ARG, "%s: window=%lld max_len=%lld", fn, (long long)window, (long long)max_len);
+  if (!kv_strides_ok(q_row, q_head, q_heads, d) || !kv_strides_ok(o_row, o_head, q_heads, d))
+    return fail(SPH_E_INVALID_ARG, "%s: row and head strides %lld, %lld and %lld, %lld for %lld heads of %lld", fn,
+                (long long)q_row, (long long)q_head, (long long)o_row, (long long)o_head, (long long)q_heads,
+                (long long)d);
+  if (n_sessions == 0 || R == 0) return ok();
+  if (R * (q_heads / cache->kv_heads) > sph::kKvMost)
+    return fail(SPH_E_UNSUPPORTED, "%s: %lld rows of %lld heads each", fn, (long long)R,
+                (long long)(q_heads / cache->kv_heads));
+  if (!q || !out) return fail(SPH_E_INVALID_ARG, "%s: q or out is NULL", fn);
+  if (window > kMaxIds) window = 0;  // every length is below it
+  max_len = kv_most(cache, max_len);
+  const size_t need = sph::kv_attend_scratch((int)d, n_sessions, R, cache->kv_heads, q_heads, max_len, window);
+  if (need > 0) {
+    const int we = pages_ws(fn, workspace, ws_bytes, need);
+    if (we != SPH_OK) return we;
+  }
+  const sph::AttendCall c{q, q_row, q_head, (int)q_heads, scale, (int)window, max_len, out, o_row, o_head, lse_out};
+  hipStream_t s = (hipStream_t)stream;
+  const hipError_t he = traced("kv_attend", s, [&] { return sph::launch_kv_attend((int)d, a, c, workspace, s); });
+  if (he != hipSuccess) return hip_fail(he, "attention launch");
+  return ok();
+}
+
+size_t sph_pages_grow_workspace(const sph_kv_cache* cache) {
+  if (!cache || cache->n_pages < 1 || cache->n_pages > kMaxIds || cache->n_slots < 1 || cache->n_slots > kMaxIds) return 0;
+  return sph::pages_grow_scratch(cache->n_pages, cache->n_slots);
+}
+
+int sph_pages_grow(const sph_kv_cache* cache, const int32_t* add, int32_t* status_out,
+                   void* workspace, size_t ws_bytes, void* stream) {
+  const char* fn = "sph_pages_grow";
+  int e = kv_check(fn, cache, true);
+  if (e != SPH_OK) return e;
+  if (!add || !status_out) return fail(SPH_E_INVALID_ARG, "%s: add or status_out is NULL", fn);
+  e = pages_ws(fn, workspace, ws_bytes, sph_pages_grow_workspace(cache));
+  if (e != SPH_OK) return e;
+  hipStream_t s = (hipStream_t)stream;
+  const hipError_t he =
+      traced("pages_grow", s, [&] { return sph::launch_pages_grow(pages_args(cache), add, status_out, workspace, s); });
+  if (he != hipSuccess) return hip_fail(he, "page growth launch");
+  return ok();
+}
+
+int sph_pages_trim(const sph_kv_cache* cache, const int32_t* kept, void* stream) {
+  const char* fn = "sph_pages_trim";
+  const int e = kv_check(fn, cache, true);
+  if (e != SPH_OK) return e;
+  if (!kept) return fail(SPH_E_INVALID_ARG, "%s: kept is NULL", fn);
+  hipStream_t s = (hipStream_t)stream;
+  const hipError_t he = traced("pages_trim", s, [&] { return sph::launch_pages_trim(pages_args(cache), kept, s); });
+  if (he != hipSuccess) return hip_fail(he, "page trim launch");
+  return ok();
+}
+
+int sph_pages_fork(const sph_kv_cache* cache, const int32_t* parents, const int32_t* children,
+                   int64_t n, void* stream) {
+  const char* fn = "sph_pages_fork";
+  const int e = kv_check(fn, cache, true);
+  if (e != SPH_OK) return e;
+  if (n < 0 || n > cache->n_slots)
+    return fail(SPH_E_INVALID_ARG, "%s: n=%lld of n_slots=%lld", fn, (long long)n, (long long)cache->n_slots);
+  if (n == 0) return ok();
+  if (!parents || !children) return fail(SPH_E_INVALID_ARG, "%s: parents or children is NULL", fn);
+  hipStream_t s = (hipStream_t)stream;
+  const hipError_t he = traced("pages_fork", s, [&] {
+    return sph::launch_pages_fork(pages_args(cache), parents, children, (int)n, s);
+  });
+  if (he != hipSuccess) return hip_fail(he, "page fork launch");
+  return ok();
+}
+
+int sph_pages_copy(const sph_kv_cache* cache, const int32_t* src, const int32_t* dst, int64_t n,
+                   void* stream) {
+  const char* fn = "sph_pages_copy";
+  const int e = kv_check(fn, cache, true);
+  if (e != SPH_OK) return e;
+  if (n < 0 || n > cache->n_pages)
+    return fail(SPH_E_INVALID_ARG, "%s: n=%lld of n_pages=%lld", fn, (long long)n, (long long)cache->n_pages);
+  if (n == 0) return ok();
+  if (!src || !dst) return fail(SPH_E_INVALID_ARG, "%s: src or dst is NULL", fn);
+  hipStream_t s = (hipStream_t)stream;
+  const hipError_t he = traced("pages_copy", s, [&] { return sph::launch_pages_copy(pages_args(cache), src, dst, n, s); });
+  if (he != hipSuccess) return hip_fail(he, "page copy launch");
+  return ok();
+}
+
+size_t sph_pages_compact_workspace(const sph_kv_cache* cache) {
+  if (!cache || cache->n_pages < 1 || cache->n_pages > kMaxIds) return 0;
+  return sph::pages_compact_scratch(cache->n_pages);
+}
+
+int sph_pages_compact(const sph_kv_cache* cache, int32_t* table_out, int64_t ld_out,
+                      int32_t* refs_out, int32_t* live_out, void* workspace, size_t ws_bytes,
+                      void* stream) {
+  const char* fn = "sph_pages_compact";
+  int e = kv_check(fn, cache, true);
+  if (e != SPH_OK) return e;
+  if (!table_out || !refs_out || !live_out) return fail(SPH_E_INVALID_ARG, "%s: an output is NULL", fn);
+  if (ld_out < cache->max_pages)
+    return fail(SPH_E_INVALID_ARG, "%s: ld_out=%lld below max_pages=%lld", fn, (long long)ld_out,
+                (long long)cache->max_pages);
+  e = pages_ws(fn, workspace, ws_bytes, sph_pages_compact_workspace(cache));
+  if (e != SPH_OK) return e;
+  hipStream_t s = (hipStream_t)stream;
+  const hipError_t he = traced("pages_compact", s, [&] {
+    return sph::launch_pages_compact(pages_args(cache), table_out, ld_out, refs_out, live_out, workspace, s);
+  });
+  if (he != hipSuccess) return hip_fail(he, "page compaction launch");
+  return ok();
 }
 
 int sph_trace_start(int capacity) {
