@@ -144,4 +144,14 @@ __device__ __forceinline__ uint32_t fp4_pair(uint32_t codes, float scale) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, BYTE));
 }
 
+// The same for a byte number that unrolling makes a constant.
+__device__ __forceinline__ uint32_t fp4_pair_at(uint32_t codes, float scale, int byte) {
+  switch (byte) {
+    case 0: return fp4_pair<0>(codes, scale);
+    case 1: return fp4_pair<1>(codes, scale);
+    case 2: return fp4_pair<2>(codes, scale);
+    default: return fp4_pair<3>(codes, scale);
+  }
+}
+
 }  // namespace sph
