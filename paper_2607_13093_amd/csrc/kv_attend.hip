@@ -40,15 +40,32 @@ struct AttendArgs {
 };
 
 constexpr float kNoScore = -1.0e30f;  // finite, also times a scale: differences with it are no NaN
+constexpr int kQueriesInLds = 512;  // head size times tiles
 constexpr float kLate = 8.0f;
 constexpr float kLn2 = 0.693147180559945f;
 
-// A lane's share of 32 tokens: codes, the scale bytes of its keys (one, two for D
+// Tiles of 32 tokens go from memory straight into a ring of LDS stages that is the
+// wave's own: as many as the ring holds are in flight at no cost in registers, and
+// no wave waits for another.  A stage is the codes of both blocks as they are
+// stored, then the scales of both.
+template <int D>
+struct Stage {
+  static constexpr int kCodes = 32 * D;                               // bytes
+  static constexpr int kBytes = (34 * D + 255) / 256 * 256;
+  static constexpr int kCodeCopies = kCodes / 1024;                   // a wave copies 64 x 16 bytes,
+  static constexpr int kScaleCopies = (2 * D + 255) / 256;            // scales 64 x 4
+  static constexpr int kCopies = kCodeCopies + kScaleCopies;
+};
+
+// A lane's share of a stage: codes, and the scale bytes of its keys (one, two for D
 // 256) and of its values (four tokens).
 template <int D>
-struct KvTile {
-  uint32_t k[2][D / 32], v[2][D / 32];
-  uint32_t ks[2], vs[2];
+struct KvKeys {
+  uint32_t c[2][D / 32], s[2];
+};
+template <int D>
+struct KvValues {
+  uint32_t c[2][D / 32], s[2];
 };
 
 // Pages of a tile's two blocks, -1 for one that no row of the wave sees or the
@@ -59,41 +76,102 @@ struct KvPages {
 __device__ __forceinline__ KvPages tile_pages(const KvArgs& a, const KvSession& ses, int pos, int end) {
   KvPages p;
 #pragma unroll
-  for (int b = 0; b < 2; ++b) p.page[b] = pos + b * kKvBlock < end ? kv_page(a, ses, pos + b * kKvBlock) : -1;
+  for (int b = 0; b < 2; ++b) {
+    const int at = pos + b * kKvBlock;
+    const int i = at >> a.page_shift;
+    // (the constant address space makes it a scalar load)
+    const int page = at < end && i < a.max_pages ? ((const __attribute__((address_space(4))) int32_t*)ses.table)[i] : -1;
+    p.page[b] = (unsigned)page < (unsigned)a.n_pages ? page : -1;
+  }
   return p;
 }
 
-template <int N>
-__device__ __forceinline__ void load_words(uint32_t (&r)[N], const uint8_t* p) {
-  if constexpr (N == 2) {
-    const u32x2_t x = *reinterpret_cast<const u32x2_t*>(p);
-    r[0] = x[0], r[1] = x[1];
-  } else {
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i) {
-      const u32x4_t x = *reinterpret_cast<const u32x4_t*>(p + 16 * i);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) r[4 * i + e] = x[e];
-    }
-  }
-}
-
-// A block that does not exist is read from page 0 and not used.
+// Copies of one tile into the stage `to`.  A block that does not exist is copied
+// from page 0 and not used.  lane16: the lane's 16 bytes (kept apart from the base,
+// which stays scalar); the offset operand counts for both sides.
 template <int D>
-__device__ __forceinline__ void load_tile(KvTile<D>& t, const KvArgs& a, int head, int pos, const KvPages& pages,
-                                          uint32_t lane) {
-  const uint32_t g = lane >> 4, n = lane & 15;
+__device__ __forceinline__ void copy_tile(uint8_t* to, const KvArgs& a, int head, int pos, const KvPages& pages,
+                                          uint32_t& lane16, uint32_t lane) {
+  const uint8_t* blk[2];
+  asm volatile("" : "+v"(lane16));
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     const int page = pages.page[b];
-    const uint8_t* blk = scalar_ptr(kv_block<D>(a, page < 0 ? 0 : page, head, page < 0 ? 0 : pos + b * kKvBlock));
-    load_words(t.k[b], blk + (n * (D / 2) + g * (D / 8)));
-    load_words(t.v[b], blk + (KvLayout<D>::kValues + lane * (D / 8)));
-    constexpr uint32_t KS = KvLayout<D>::kKeyScales;
-    if constexpr (D == 64) t.ks[b] = blk[KS + (g >> 1) * kKvBlock + n];
-    else if constexpr (D == 128) t.ks[b] = blk[KS + g * kKvBlock + n];
-    else t.ks[b] = blk[KS + 2 * g * kKvBlock + n] | ((uint32_t)blk[KS + (2 * g + 1) * kKvBlock + n] << 8);
-    t.vs[b] = *reinterpret_cast<const uint32_t*>(blk + (KvLayout<D>::kValueScales + n * D / 512 * kKvBlock + 4 * g));
+    blk[b] = scalar_ptr(kv_block<D>(a, page < 0 ? 0 : page, head, page < 0 ? 0 : pos + b * kKvBlock));
+    lds_void_t* at = (lds_void_t*)(to + b * 16 * D);
+    __builtin_amdgcn_global_load_lds(blk[b] + lane16, at, 16, 0, 0);
+    if constexpr (D >= 128) __builtin_amdgcn_global_load_lds(blk[b] + lane16, at, 16, 1024, 0);
+    if constexpr (D >= 256) {
+      __builtin_amdgcn_global_load_lds(blk[b] + lane16, at, 16, 2048, 0);
+      __builtin_amdgcn_global_load_lds(blk[b] + lane16, at, 16, 3072, 0);
+    }
+  }
+  lds_void_t* at = (lds_void_t*)(to + Stage<D>::kCodes);
+  if constexpr (D == 256) {  // 256 bytes of either block
+    const uint32_t lane4 = lane16 / 4 + 16 * D;
+    __builtin_amdgcn_global_load_lds(blk[0] + lane4, at, 4, 0, 0);
+    __builtin_amdgcn_global_load_lds(blk[1] + lane4, (lds_void_t*)(to + Stage<D>::kCodes + 256), 4, 0, 0);
+  } else {                   // D bytes of either; for D 64 the last half of the lanes repeat the first
+    const uint32_t in = lane * 4 % (2 * D);
+    const uint64_t b0 = reinterpret_cast<uint64_t>(blk[0]), b1 = reinterpret_cast<uint64_t>(blk[1]);
+    const uint64_t base = in < D ? b0 : b1;
+    __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint8_t*>(base) + (16 * D + in % D), at, 4, 0, 0);
+  }
+}
+
+// At most N of the wave's newest copies may still be on their way.
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory");
+}
+
+// Reads of a stage end with their own wait: the compiler would make them wait for
+// every copy in flight.  at_c, at_s: LDS addresses of the lane's codes and scales.
+template <int D>
+__device__ __forceinline__ void read_codes(uint32_t (&c)[2][D / 32], uint32_t& s0, uint32_t& s1, uint32_t at_c,
+                                           uint32_t at_s, bool bytes) {
+  if constexpr (D == 64) {
+    u32x2_t x, y;
+    if (bytes)
+      asm volatile("ds_read_b64 %0, %4\n ds_read_b64 %1, %4 offset:1024\n ds_read_u8 %2, %5\n"
+                   "ds_read_u8 %3, %5 offset:64\n s_waitcnt lgkmcnt(0)"
+                   : "=&v"(x), "=&v"(y), "=&v"(s0), "=&v"(s1) : "v"(at_c), "v"(at_s) : "memory");
+    else
+      asm volatile("ds_read_b64 %0, %4\n ds_read_b64 %1, %4 offset:1024\n ds_read_b32 %2, %5\n"
+                   "ds_read_b32 %3, %5 offset:64\n s_waitcnt lgkmcnt(0)"
+                   : "=&v"(x), "=&v"(y), "=&v"(s0), "=&v"(s1) : "v"(at_c), "v"(at_s) : "memory");
+    c[0][0] = x[0], c[0][1] = x[1], c[1][0] = y[0], c[1][1] = y[1];
+  } else if constexpr (D == 128) {
+    u32x4_t x, y;
+    if (bytes)
+      asm volatile("ds_read_b128 %0, %4\n ds_read_b128 %1, %4 offset:2048\n ds_read_u8 %2, %5\n"
+                   "ds_read_u8 %3, %5 offset:128\n s_waitcnt lgkmcnt(0)"
+                   : "=&v"(x), "=&v"(y), "=&v"(s0), "=&v"(s1) : "v"(at_c), "v"(at_s) : "memory");
+    else
+      asm volatile("ds_read_b128 %0, %4\n ds_read_b128 %1, %4 offset:2048\n ds_read_b32 %2, %5\n"
+                   "ds_read_b32 %3, %5 offset:128\n s_waitcnt lgkmcnt(0)"
+                   : "=&v"(x), "=&v"(y), "=&v"(s0), "=&v"(s1) : "v"(at_c), "v"(at_s) : "memory");
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[0][e] = x[e], c[1][e] = y[e];
+  } else {
+    u32x4_t x, y, z, w;
+    if (bytes) {
+      uint32_t t0, t1;  // the second group's bytes
+      asm volatile("ds_read_b128 %0, %8\n ds_read_b128 %1, %8 offset:16\n ds_read_b128 %2, %8 offset:4096\n"
+                   "ds_read_b128 %3, %8 offset:4112\n ds_read_u8 %4, %9\n ds_read_u8 %5, %9 offset:256\n"
+                   "ds_read_u8 %6, %9 offset:16\n ds_read_u8 %7, %9 offset:272\n s_waitcnt lgkmcnt(0)"
+                   : "=&v"(x), "=&v"(y), "=&v"(z), "=&v"(w), "=&v"(s0), "=&v"(s1), "=&v"(t0), "=&v"(t1)
+                   : "v"(at_c), "v"(at_s) : "memory");
+      s0 |= t0 << 8;
+      s1 |= t1 << 8;
+    } else {
+      asm volatile("ds_read_b128 %0, %6\n ds_read_b128 %1, %6 offset:16\n ds_read_b128 %2, %6 offset:4096\n"
+                   "ds_read_b128 %3, %6 offset:4112\n ds_read_b32 %4, %7\n ds_read_b32 %5, %7 offset:256\n"
+                   "s_waitcnt lgkmcnt(0)"
+                   : "=&v"(x), "=&v"(y), "=&v"(z), "=&v"(w), "=&v"(s0), "=&v"(s1) : "v"(at_c), "v"(at_s) : "memory");
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[0][e] = x[e], c[0][4 + e] = y[e], c[1][e] = z[e], c[1][4 + e] = w[e];
   }
 }
 
@@ -125,64 +203,88 @@ struct Rows {
   float top[MT], sum[MT];  // sums of the lane's own tokens
 };
 
-// 32 tokens from position t0.  MASK: some of them are not for all of the rows:
-// held[b] tokens of either block exist, row n of tile m stands at pos[m].
-template <int D, int MT, bool MASK>
-__device__ __forceinline__ void take_tile(Rows<D, MT>& w, KvTile<D>& cur, const bf16x8_t (&q)[MT][D / 32],
-                                          const AttendArgs& a, int t0, const int (&held)[2], const int (&pos)[MT],
-                                          int g) {
-  constexpr int KJ = D / 32;  // steps of the first product
-  constexpr int VC = D / 16;  // products of the second
-  if constexpr (MASK) {
-    // tokens that do not exist: what their bytes say is anything, and zero times
-    // it has to be zero
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (4 * g + i >= held[b]) {
-          cur.vs[b] &= ~(0xFFu << (8 * i));
-          if constexpr (D == 64) cur.v[b][i >> 1] &= ~(0xFFFFu << (16 * (i & 1)));
-          else if constexpr (D == 128) cur.v[b][i] = 0u;
-          else cur.v[b][2 * i] = cur.v[b][2 * i + 1] = 0u;
-        }
+// Queries as the second operand of the first product: tile m, step j.  Where the
+// outputs alone are 128 registers they come from LDS.
+template <int D, int MT, bool LDS>
+struct Queries {
+  bf16x8_t r[LDS ? 1 : MT][LDS ? 1 : D / 32];
+  const u32x4_t* l;  // LDS [row groups][MT][D / 32][64 lanes]
+  uint32_t own;      // the lane's first
+  __device__ __forceinline__ bf16x8_t at(int m, int j) const {
+    if constexpr (LDS) return __builtin_bit_cast(bf16x8_t, l[own + (m * (D / 32) + j) * 64]);
+    else return r[m][j];
   }
+};
 
-  // scores: lane l has row n against tokens 4 g + e of both blocks
-  f32x4_t sc[MT][2];
+// Scores of 32 tokens: lane l has row n against tokens 4 g + e of both blocks.
+template <int D, int MT, bool LDS>
+__device__ __forceinline__ void take_keys(f32x4_t (&sc)[MT][2], const KvKeys<D>& k, Queries<D, MT, LDS>& q) {
+  // (read again for every tile: kept in registers they would cost what LDS saves)
+  if constexpr (LDS) asm volatile("" : "+v"(q.own));
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
+  for (int m = 0; m < MT; ++m) sc[m][0] = sc[m][1] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int m = 0; m < MT; ++m) sc[m][b] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int j = 0; j < D / 32; ++j) {
+    bf16x8_t kf[2];
 #pragma unroll
-    for (int j = 0; j < KJ; ++j) {
-      const float ks = e8m0_operand(D == 256 ? (cur.ks[b] >> (8 * (j / 4))) & 0xFFu : cur.ks[b]);
-      const uint32_t c = cur.k[b][j];
-      const u32x4_t x{fp4_pair<0>(c, ks), fp4_pair<1>(c, ks), fp4_pair<2>(c, ks), fp4_pair<3>(c, ks)};
-      const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, x);
+    for (int b = 0; b < 2; ++b) {
+      const float s = e8m0_operand(D == 256 ? (k.s[b] >> (8 * (j / 4))) & 0xFFu : k.s[b]);
+      const uint32_t c = k.c[b][j];
+      const u32x4_t x{fp4_pair<0>(c, s), fp4_pair<1>(c, s), fp4_pair<2>(c, s), fp4_pair<3>(c, s)};
+      kf[b] = __builtin_bit_cast(bf16x8_t, x);
+    }
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-        sc[m][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[m][j], sc[m][b], 0, 0, 0);
+    for (int m = 0; m < MT; ++m) {
+      const bf16x8_t qf = q.at(m, j);
+      sc[m][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[0], qf, sc[m][0], 0, 0, 0);
+      sc[m][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[1], qf, sc[m][1], 0, 0, 0);
     }
   }
-  if constexpr (MASK) {
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int in = 4 * g + e, j = t0 + b * kKvBlock + in;
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          const bool sees = in < held[b] && j <= pos[m] && (a.window <= 0 || j > pos[m] - a.window);
-          sc[m][b][e] = sees ? sc[m][b][e] : -INFINITY;
-        }
-      }
-  }
+}
 
-  // Weights are taken against a reference that is at most kLate binades below the
-  // row's largest score so far (so that weights stay below 2^kLate): lanes look
-  // at their own scores and exchange them only when one goes past that, which is
-  // rare after the first tiles.
+// What row n of tile m, at position pos[m], does not see of 32 tokens from t0, of
+// which held[b] exist in either block.
+template <int MT>
+__device__ __forceinline__ void mask_scores(f32x4_t (&sc)[MT][2], const int (&pos)[MT], int window, int t0,
+                                            const int (&held)[2], int g) {
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int in = 4 * g + e, j = t0 + b * kKvBlock + in;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const bool sees = in < held[b] && j <= pos[m] && (window <= 0 || j > pos[m] - window);
+        sc[m][b][e] = sees ? sc[m][b][e] : -INFINITY;
+      }
+    }
+}
+
+// Tokens that do not exist: what their bytes say is anything, and zero times it
+// has to be zero.
+template <int D>
+__device__ __forceinline__ void clear_values(KvValues<D>& v, const int (&held)[2], int g) {
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (4 * g + i >= held[b]) {
+        v.s[b] &= ~(0xFFu << (8 * i));
+        if constexpr (D == 64) v.c[b][i >> 1] &= ~(0xFFFFu << (16 * (i & 1)));
+        else if constexpr (D == 128) v.c[b][i] = 0u;
+        else v.c[b][2 * i] = v.c[b][2 * i + 1] = 0u;
+      }
+}
+
+// Weights of 32 tokens as the second operand of the second product, in bf16 (its
+// sums stay in fp32: an output is off by about the rounding of a bf16).  They are
+// taken against a reference that is at most kLate binades below the row's largest
+// score so far, so that they stay below 2^kLate: lanes look at their own scores
+// and exchange them only when one goes past that, which is rare after the first
+// tiles.
+template <int D, int MT>
+__device__ __forceinline__ void take_weights(bf16x8_t (&p)[MT], Rows<D, MT>& w, const f32x4_t (&sc)[MT][2],
+                                             const AttendArgs& a) {
   float most[MT];
   bool late = false;
 #pragma unroll
@@ -199,13 +301,10 @@ __device__ __forceinline__ void take_tile(Rows<D, MT>& w, KvTile<D>& cur, const 
       const float f = __builtin_amdgcn_exp2f((w.top[m] - t) * a.scale_log2);
       w.sum[m] *= f;
 #pragma unroll
-      for (int c = 0; c < VC; ++c) w.o[m][c] *= f;
+      for (int c = 0; c < D / 16; ++c) w.o[m][c] *= f;
       w.top[m] = t;
     }
   }
-  // P rounded to bf16 for the second product (its sums stay in fp32: an output is
-  // off by about the rounding of a bf16)
-  bf16x8_t p[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     const float off = w.top[m] * a.scale_log2;
@@ -218,22 +317,26 @@ __device__ __forceinline__ void take_tile(Rows<D, MT>& w, KvTile<D>& cur, const 
     const u32x4_t x{pack_bf16(e8[0], e8[1]), pack_bf16(e8[2], e8[3]), pack_bf16(e8[4], e8[5]), pack_bf16(e8[6], e8[7])};
     p[m] = __builtin_bit_cast(bf16x8_t, x);
   }
+}
 
-  float vs[2][4];
+// The second product: columns 2 c, 2 c + 1 of the lane's part are a byte of each
+// of its eight tokens.
+template <int D, int MT>
+__device__ __forceinline__ void take_values(Rows<D, MT>& w, const KvValues<D>& v, const bf16x8_t (&p)[MT]) {
+  float s[2][4];
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) vs[b][i] = e8m0_operand((cur.vs[b] >> (8 * i)) & 0xFFu);
-  // columns 2 c, 2 c + 1 of the lane's part: a byte of each of its eight tokens
+    for (int i = 0; i < 4; ++i) s[b][i] = e8m0_operand((v.s[b] >> (8 * i)) & 0xFFu);
 #pragma unroll
-  for (int c = 0; c < VC / 2; ++c) {
+  for (int c = 0; c < D / 32; ++c) {
     uint32_t x8[8];
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int at = i * (D / 32) + c;  // byte of the lane's D/8
-        x8[4 * b + i] = fp4_pair_at(cur.v[b][at / 4], vs[b][i], at % 4);
+        x8[4 * b + i] = fp4_pair_at(v.c[b][at / 4], s[b][i], at % 4);
       }
     u32x4_t x, y;
 #pragma unroll
@@ -251,14 +354,34 @@ __device__ __forceinline__ void take_tile(Rows<D, MT>& w, KvTile<D>& cur, const 
 
 // A workgroup is 4 waves: WT of them share the tokens of the same rows, 4 / WT
 // have rows of their own.
-#ifndef WPE
-#define WPE(D, MT) ((D) * (MT) <= 128 ? 3 : (D) * (MT) <= 256 ? 2 : 1)
-#endif
+// Waves of a SIMD (workgroups of a CU) that the registers leave room for, and the
+// stages of a ring.
+constexpr int waves_of(int d, int mt) { return d * mt <= 128 ? 4 : (mt < 4 && d * mt <= 256 ? 3 : 2); }
+constexpr int stages_of(int d) { return d == 64 ? 4 : (d == 128 ? 3 : 2); }
+// LDS of a workgroup: rings and queries, in their place the waves' outputs.
+constexpr int attend_lds(int d, int mt, int wt) {
+  const int run = 4 * stages_of(d) * ((34 * d + 255) / 256 * 256) + (d * mt >= kQueriesInLds ? 4 / wt * mt * (d / 32) * 1024 : 0);
+  const int end = wt > 1 ? 256 * d + 512 * mt : 0;
+  return run > end ? run : end;
+}
+constexpr int resident(int d, int mt, int wt) {  // workgroups of a CU
+  const int by_lds = 160 * 1024 / attend_lds(d, mt, wt);
+  return by_lds < waves_of(d, mt) ? by_lds : waves_of(d, mt);
+}
+// Tiles of a wave for so many rows of a head.
+constexpr int rows_tiles(int d, int64_t rows) {
+  if (rows <= 16 || d == 256) return 1;
+  if (rows <= 32) return 2;
+  return d == 64 || rows <= 64 ? 4 : 2;
+}
+
 template <int D, int MT, int WT>
-__global__ __launch_bounds__(256, WPE(D, MT)) void k_kv_attend(AttendArgs a) {
+__global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a) {
+  constexpr int NS = stages_of(D);
   constexpr int WR = 4 / WT;
   constexpr int KJ = D / 32;   // steps of the first product
   constexpr int VC = D / 16;   // products of the second
+  constexpr bool QL = D * MT >= kQueriesInLds;
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int wt = wave % WT, wr = wave / WT;
@@ -275,7 +398,11 @@ __global__ __launch_bounds__(256, WPE(D, MT)) void k_kv_attend(AttendArgs a) {
   const int row0 = (tile * WR + wr) * 16 * MT;     // the wave's first of total rows
 
   // rows: fq = r G + query head; those past the session's see nothing
-  bf16x8_t q[MT][KJ];
+  extern __shared__ __align__(16) uint8_t smem[];  // rings, then queries of each group of rows
+  u32x4_t* s_q = reinterpret_cast<u32x4_t*>(smem + 4 * NS * Stage<D>::kBytes);
+  Queries<D, MT, QL> q;
+  q.l = s_q;
+  q.own = wr * (MT * KJ * 64) + lane;
   int pos[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
@@ -286,7 +413,8 @@ __global__ __launch_bounds__(256, WPE(D, MT)) void k_kv_attend(AttendArgs a) {
 #pragma unroll
     for (int j = 0; j < KJ; ++j) {
       u32x4_t x{0u, 0u, 0u, 0u};
-      if (fq < live) {
+      // (waves that share rows share the work of it)
+      if (fq < live && (!QL || j % WT == wt)) {
         if (a.q_aligned) {
           x = *reinterpret_cast<const u32x4_t*>(p + 8 * j);
         } else {
@@ -294,10 +422,10 @@ __global__ __launch_bounds__(256, WPE(D, MT)) void k_kv_attend(AttendArgs a) {
           for (int i = 0; i < 4; ++i) x[i] = (uint32_t)p[8 * j + 2 * i] | ((uint32_t)p[8 * j + 2 * i + 1] << 16);
         }
       }
-      q[m][j] = __builtin_bit_cast(bf16x8_t, x);
+      if constexpr (!QL) q.r[m][j] = __builtin_bit_cast(bf16x8_t, x);
+      else if (j % WT == wt) s_q[((wr * MT + m) * KJ + j) * 64 + lane] = x;
     }
   }
-
   // tokens that the wave's rows see, and those that all of them see
   const int last_row = (row0 + 16 * MT < live ? row0 + 16 * MT : live) - 1;
   int lo = 0, hi = 0, all_lo = 0, all_hi = 0;
@@ -345,43 +473,78 @@ __global__ __launch_bounds__(256, WPE(D, MT)) void k_kv_attend(AttendArgs a) {
     return k < n_whole ? whole + k * STEP : (k < n_whole + n_head ? start : part - n_head * STEP) + (k - n_whole) * STEP;
   };
 
-  // codes are asked for one tile ahead, pages two
-  KvTile<D> next;
-  KvPages here = tile_pages(a.kv, ses, place(0), to);
-  if (n_tiles > 0) load_tile<D>(next, a.kv, head, place(0), here, lane);
-  KvPages ahead = tile_pages(a.kv, ses, place(1), to);
-  int k = 0;
-  for (; k < n_whole; ++k) {
-    KvTile<D> cur = next;
-    const KvPages after = tile_pages(a.kv, ses, place(k + 2), to);
-    if (k + 1 < n_tiles) load_tile<D>(next, a.kv, head, place(k + 1), ahead, lane);
-    const int held[2] = {kKvBlock, kKvBlock};
-    take_tile<D, MT, false>(w, cur, q, a, 0, held, pos, g);
-    here = ahead;
+  uint8_t* ring = smem + wave * (NS * Stage<D>::kBytes);
+  uint32_t lane16 = lane * 16;
+  const uint32_t ring_at = (uint32_t)(uintptr_t)(lds_void_t*)ring;
+  // the lane's places in a stage: keys token n of a block, values as they lie
+  const uint32_t key_at = n * (D / 2) + g * (D / 8), value_at = KvLayout<D>::kValues + lane * (D / 8);
+  const uint32_t ks_at = Stage<D>::kCodes + (D == 64 ? g >> 1 : D == 128 ? g : 2 * g) * kKvBlock + n;
+  const uint32_t vs_at = Stage<D>::kCodes + D / 2 + n * D / 512 * kKvBlock + 4 * g;
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i)
+    if (i < n_tiles) copy_tile<D>(ring + i * Stage<D>::kBytes, a.kv, head, place(i), tile_pages(a.kv, ses, place(i), to), lane16, lane);
+  if constexpr (QL) __syncthreads();
+  else  // here, not in the loop: the compiler's wait would be for all copies in flight
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int j = 0; j < KJ; ++j) asm volatile("" : "+v"(q.r[m][j]));
+  KvPages ahead = tile_pages(a.kv, ses, place(NS - 1), to);
+  int k = 0, stage = 0, fill = NS - 1;  // stages read and written next
+  KvKeys<D> keys;
+  KvValues<D> values;
+  f32x4_t sc[MT][2];
+  bf16x8_t p[MT];
+  // asks for the tile NS - 1 ahead, waits for this one, and scores it
+  auto begin = [&] {
+    const KvPages after = tile_pages(a.kv, ses, place(k + NS), to);
+    if (k + NS - 1 < n_tiles) {
+      copy_tile<D>(ring + fill * Stage<D>::kBytes, a.kv, head, place(k + NS - 1), ahead, lane16, lane);
+      wait_copies<(NS - 1) * Stage<D>::kCopies>();
+    } else if (NS > 2 && k + 2 == n_tiles) {
+      wait_copies<Stage<D>::kCopies>();
+    } else if (NS > 3 && k + 3 == n_tiles) {
+      wait_copies<2 * Stage<D>::kCopies>();
+    } else {
+      wait_copies<0>();
+    }
     ahead = after;
+    const uint32_t at = ring_at + stage * Stage<D>::kBytes;
+    read_codes<D>(keys.c, keys.s[0], keys.s[1], at + key_at, at + ks_at, true);
+    take_keys(sc, keys, q);
+    read_codes<D>(values.c, values.s[0], values.s[1], at + value_at, at + vs_at, false);
+    stage = stage + 1 == NS ? 0 : stage + 1;
+    fill = fill + 1 == NS ? 0 : fill + 1;
+  };
+  for (; k < n_whole; ++k) {
+    begin();
+    take_weights(p, w, sc, a);
+    take_values(w, values, p);
   }
   for (; k < n_tiles; ++k) {
-    KvTile<D> cur = next;
     const int t0 = place(k);
-    const KvPages after = tile_pages(a.kv, ses, place(k + 2), to);
-    if (k + 1 < n_tiles) load_tile<D>(next, a.kv, head, place(k + 1), ahead, lane);
+    const KvPages here = tile_pages(a.kv, ses, t0, to);
     int held[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const int left = to - t0 - b * kKvBlock;
       held[b] = here.page[b] < 0 ? 0 : (left < kKvBlock ? left : kKvBlock);
     }
-    take_tile<D, MT, true>(w, cur, q, a, t0, held, pos, g);
-    here = ahead;
-    ahead = after;
+    begin();
+    mask_scores(sc, pos, a.window, t0, held, g);
+    take_weights(p, w, sc, a);
+    clear_values(values, held, g);
+    take_values(w, values, p);
   }
 #pragma unroll
   for (int m = 0; m < MT; ++m) w.sum[m] = sum_over_groups(w.sum[m]);
 
   // lane l holds row n, dimensions (4 g + e) D/16 + c = w.o[m][c][e]
-  __shared__ float s_ml[WT > 1 ? 4 * MT * 16 * 2 : 1];
-  __shared__ float s_o[WT > 1 ? 4 * D * 16 : 1];
+  // (in what were rings)
+  float* s_o = reinterpret_cast<float*>(smem);       // 4 x 16 D
+  float* s_ml = reinterpret_cast<float*>(smem) + 64 * D;
   if constexpr (WT > 1) {
+    __syncthreads();
     if (g == 0)
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
@@ -462,92 +625,142 @@ __global__ __launch_bounds__(256, WPE(D, MT)) void k_kv_attend(AttendArgs a) {
   }
 }
 
-// The shares of a row joined: a workgroup a row and head, D/4 lanes for a share,
-// the shares in turns; sums in an order that is always the same.
-template <int D>
-__global__ __launch_bounds__(256) void k_kv_join(AttendArgs a) {
-  constexpr int LPS = D / 4, TURNS = 256 / LPS;  // 16, 32 or 64 lanes
-  __shared__ float s_l[TURNS];
-  __shared__ f32x4_t s_o[256];
-  const int d4 = threadIdx.x % LPS, turn = threadIdx.x / LPS;
-  const int64_t i = blockIdx.x;
+// The shares of a row joined.  D/4 lanes take a share, TURNS groups of them the
+// shares of one row and head in turns, each eight at a time so that all their
+// loads are on their way together; sums in an order that is always the same.
+template <int D, int TURNS>
+__global__ __launch_bounds__(256) void k_kv_join(AttendArgs a, int64_t rows) {
+  constexpr int LPS = D / 4, PER = 256 / LPS / TURNS;  // rows of a workgroup
+  __shared__ float s_l[256 / LPS];
+  __shared__ f32x4_t s_o[TURNS > 1 ? 256 : 1];
+  const int d4 = threadIdx.x % LPS, turn = threadIdx.x / LPS % TURNS;
+  const int64_t want = (int64_t)blockIdx.x * PER + threadIdx.x / (LPS * TURNS);
+  const int64_t i = want < rows ? want : rows - 1;
+  const float2* ml = a.part_ml + i * a.splits;
+  const float* part = a.part_o + i * a.splits * D + d4 * 4;
+  float top = kNoScore, l = 0.0f;
+  f32x4_t y{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int k0 = turn; k0 < a.splits; k0 += 8 * TURNS) {
+    float2 x[8];
+    f32x4_t o[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int k = k0 + u * TURNS;
+      const bool in = k < a.splits;
+      x[u] = in ? ml[k] : make_float2(kNoScore, 0.0f);
+      // shares without a token left their place unwritten: read, not used
+      if (in) o[u] = *reinterpret_cast<const f32x4_t*>(part + (int64_t)k * D);
+    }
+    float t = top;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) t = fmaxf(t, x[u].x);
+    const float f = __builtin_amdgcn_exp2f((top - t) * a.scale_log2);
+    l *= f;
+    y *= f;
+    top = t;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (x[u].y == 0.0f) continue;
+      const float e = __builtin_amdgcn_exp2f((x[u].x - top) * a.scale_log2);
+      l += x[u].y * e;
+      y += o[u] * e;
+    }
+  }
+  if constexpr (TURNS > 1) {
+    __shared__ float s_top[256 / LPS];
+    s_o[threadIdx.x] = y;
+    if (d4 == 0) {
+      s_l[turn] = l;
+      s_top[turn] = top;
+    }
+    __syncthreads();
+    if (turn != 0) return;
+    float t = top;
+#pragma unroll
+    for (int k = 1; k < TURNS; ++k) t = fmaxf(t, s_top[k]);
+    y = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    l = 0.0f;
+#pragma unroll
+    for (int k = 0; k < TURNS; ++k) {
+      const float e = __builtin_amdgcn_exp2f((s_top[k] - t) * a.scale_log2);
+      y += s_o[k * LPS + d4] * e;
+      l += s_l[k] * e;
+    }
+    top = t;
+  }
+  if (want >= rows) return;
   const int heads = a.kv.heads * a.group;
   const int64_t row = i / heads;
   const int hq = (int)(i - row * heads);
-  const float2* ml = a.part_ml + i * a.splits;
-  const float* part = a.part_o + i * a.splits * D + d4 * 4;
-  float t = kNoScore;
-  for (int k = threadIdx.x & 63; k < a.splits; k += 64) t = fmaxf(t, ml[k].x);
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) t = fmaxf(t, __shfl_xor(t, o, 64));
-  float l = 0.0f;
-  f32x4_t y{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-  for (int k = turn; k < a.splits; k += TURNS) {
-    const float2 x = ml[k];
-    const bool some = !(x.y == 0.0f);  // shares without a token left their place unwritten
-    const float f = some ? __builtin_amdgcn_exp2f((x.x - t) * a.scale_log2) : 0.0f;
-    f32x4_t o{0.0f, 0.0f, 0.0f, 0.0f};
-    if (some) o = *reinterpret_cast<const f32x4_t*>(part + (int64_t)k * D);
-    l += some ? x.y * f : 0.0f;
-    y += o * f;
-  }
-  s_o[threadIdx.x] = y;
-  if (d4 == 0) s_l[turn] = l;
-  __syncthreads();
-  if (turn != 0) return;
-#pragma unroll
-  for (int k = 1; k < TURNS; ++k) {
-    y += s_o[k * LPS + d4];
-    l += s_l[k];
-  }
   const float f = l == 0.0f ? 0.0f : 1.0f / l;
   uint16_t* dst = a.out + row * a.o_row + hq * a.o_head + d4 * 4;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) dst[e] = (uint16_t)pack_bf16(l == 0.0f ? 0.0f : y[e] * f, 0.0f);
+  const uint32_t lo = l == 0.0f ? 0u : pack_bf16(y[0] * f, y[1] * f), hi = l == 0.0f ? 0u : pack_bf16(y[2] * f, y[3] * f);
+  if (a.o_aligned) {
+    *reinterpret_cast<uint32_t*>(dst) = lo;
+    *reinterpret_cast<uint32_t*>(dst + 2) = hi;
+  } else {
+    dst[0] = (uint16_t)lo, dst[1] = (uint16_t)(lo >> 16);
+    dst[2] = (uint16_t)hi, dst[3] = (uint16_t)(hi >> 16);
+  }
   if (a.lse && d4 == 0)
-    a.lse[i] = l == 0.0f ? -INFINITY : fmaf(t, a.scale, __builtin_amdgcn_logf(l) * kLn2);
+    a.lse[i] = l == 0.0f ? -INFINITY : fmaf(top, a.scale, __builtin_amdgcn_logf(l) * kLn2);
+}
+
+template <int D>
+void launch_join(const AttendArgs& a, int64_t rows, hipStream_t s) {
+  constexpr int ALL = 256 / (D / 4);
+  if (a.splits <= 8)
+    launch_kernel(k_kv_join<D, 1>, dim3((unsigned)((rows + ALL - 1) / ALL)), dim3(256), 0, s, a, rows);
+  else
+    launch_kernel(k_kv_join<D, ALL>, dim3((unsigned)rows), dim3(256), 0, s, a, rows);
 }
 
 namespace {
 
+// How the rows of one head and the tokens of a session are shared out.
 struct Plan {
-  int mt, wt, tiles, splits, chunk;
+  int mt, wt;          // tiles of 16 rows of a wave, waves that share the tokens of the same rows
+  int tiles;           // workgroups for all rows of a head
+  int splits, chunk;   // shares of the tokens, tokens of one
 };
 
-// How rows and tokens are shared out.  R G rows of one head: up to 16 MT in a
-// workgroup whose four waves share the tokens, or 64 MT with rows a wave.
+// units: sessions times key/value heads; rows: of one head; span: tokens that a
+// row sees at most.
 Plan plan_of(int d, int64_t units, int64_t rows, int64_t span) {
   Plan p;
-#ifndef M64
-#define M64 4
-#endif
-#ifndef M128
-#define M128 2
-#endif
-#ifndef M256
-#define M256 1
-#endif
-  const int most = d == 64 ? M64 : (d == 128 ? M128 : M256);
-  p.mt = 1;
-  while (p.mt < most && rows > 16 * p.mt) p.mt *= 2;
+  p.mt = rows_tiles(d, rows);
   p.wt = 4;
   while (p.wt > 1 && rows > 16 * p.mt * (4 / p.wt)) p.wt /= 2;
   const int per = 16 * p.mt * (4 / p.wt);
   p.tiles = (int)((rows + per - 1) / per);
-#ifndef BLOCKS
-#define BLOCKS 512
-#endif
-  // as many workgroups as the chip holds at a time, with 256 tokens at least
-  int64_t splits = 1;
-  if (units * p.tiles > 0) splits = BLOCKS / (units * p.tiles);
-  const int64_t least = 256;
-  if (splits > (span + least - 1) / least) splits = (span + least - 1) / least;
-  if (splits < 1) splits = 1;
-  int64_t chunk = ((span + splits - 1) / splits + 127) / 128 * 128;
-  if (chunk < 128) chunk = 128;
-  p.chunk = (int)chunk;
-  p.splits = (int)((span + chunk - 1) / chunk);
+
+  // Shares: as few as keep the chip busy, by a rough account in microseconds.  A
+  // workgroup starts and ends in about 5; a tile of a wave is the issue of its
+  // instructions (a third more for what does not overlap) times the waves that
+  // share a SIMD, or a wave's own latencies; joining costs a launch and the
+  // partial outputs' way out and back.
+  const double issue = (4.0 * (0.9 * d + 20 + 36 * p.mt) + (32.0 + d / 2.0) * p.mt) * 1.35 / 2100;
+  const int64_t slots = (int64_t)kCUs * resident(d, p.mt, p.wt);
+  const int64_t blocks = units * p.tiles, step = 32 * p.wt;
+  auto workgroup = [&](int64_t n, int64_t tokens) {  // n of them at a time
+    const double beside = (double)((n + kCUs - 1) / kCUs);
+    const double tile = beside * issue > issue + 0.7 ? beside * issue : issue + 0.7;
+    return 5.0 + (double)((tokens + step - 1) / step) * tile;
+  };
+  p.splits = 1;
+  p.chunk = (int)((span + step - 1) / step * step);
+  double best = 0;
+  for (int64_t n = 1; n <= 128 && (n == 1 || n * step <= span + step - 1); n += n < 8 ? 1 : n / 4) {
+    const int64_t chunk = ((span + n - 1) / n + step - 1) / step * step;
+    const int64_t all = blocks * n, last = all % slots;
+    double t = (double)(all / slots) * workgroup(slots, chunk) + (last > 0 ? workgroup(last, chunk) : 0.0);
+    if (n > 1) t += 4.0 + (double)(units * rows * n) * (d * 8 + 16) / 4e6;
+    if (n == 1 || t < 0.97 * best) {
+      best = t;
+      p.splits = (int)((span + chunk - 1) / chunk);
+      p.chunk = (int)chunk;
+    }
+  }
   if (p.splits < 1) p.splits = 1;
   return p;
 }
@@ -557,25 +770,28 @@ int64_t span_of(int64_t max_len, int64_t rows, int64_t window) {
 }
 
 template <int D, int MT, int WT>
-void launch_one(const AttendArgs& a, int64_t blocks, hipStream_t s) {
-  launch_kernel(k_kv_attend<D, MT, WT>, dim3((unsigned)blocks), dim3(256), 0, s, a);
+hipError_t launch_one(const AttendArgs& a, int64_t blocks, hipStream_t s) {
+  constexpr size_t lds = attend_lds(D, MT, WT);
+  static std::atomic<uint64_t> done{0};
+  const hipError_t e = set_lds_limit_once(done, reinterpret_cast<const void*>(k_kv_attend<D, MT, WT>), lds);
+  if (e != hipSuccess) return e;
+  launch_kernel(k_kv_attend<D, MT, WT>, dim3((unsigned)blocks), dim3(256), (uint32_t)lds, s, a);
+  return hipGetLastError();
 }
 
 template <int D, int MT>
-void launch_waves(const Plan& p, const AttendArgs& a, int64_t blocks, hipStream_t s) {
-  if (p.wt == 4) launch_one<D, MT, 4>(a, blocks, s);
-  else if (p.wt == 2) launch_one<D, MT, 2>(a, blocks, s);
-  else launch_one<D, MT, 1>(a, blocks, s);
+hipError_t launch_waves(const Plan& p, const AttendArgs& a, int64_t blocks, hipStream_t s) {
+  if (p.wt == 4) return launch_one<D, MT, 4>(a, blocks, s);
+  if (p.wt == 2) return launch_one<D, MT, 2>(a, blocks, s);
+  return launch_one<D, MT, 1>(a, blocks, s);
 }
 
 template <int D>
-void launch_tiles(const Plan& p, const AttendArgs& a, int64_t blocks, hipStream_t s) {
-  constexpr int M = D == 64 ? M64 : (D == 128 ? M128 : M256);
-  if (p.mt == M) launch_waves<D, M>(p, a, blocks, s);
-  else if constexpr (M > 1) {
-    if (p.mt == 1) launch_one<D, 1, 4>(a, blocks, s);
-    else if constexpr (M > 2) launch_one<D, 2, 4>(a, blocks, s);
-  }
+hipError_t launch_tiles(const Plan& p, const AttendArgs& a, int64_t blocks, hipStream_t s) {
+  if (p.mt == 1) return launch_waves<D, 1>(p, a, blocks, s);
+  if (p.mt == 2) return launch_waves<D, 2>(p, a, blocks, s);
+  if constexpr (D < 256) return launch_waves<D, 4>(p, a, blocks, s);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -619,15 +835,15 @@ hipError_t launch_kv_attend(int d, const KvArgs& kv, const AttendCall& c, void* 
   }
   const int64_t blocks = units * p.tiles * p.splits;
   if (blocks > 0x7FFFFFFF || rows > 0x7FFFFFFF) return hipErrorInvalidValue;
-  if (d == 64) launch_tiles<64>(p, a, blocks, s);
-  else if (d == 128) launch_tiles<128>(p, a, blocks, s);
-  else if (d == 256) launch_tiles<256>(p, a, blocks, s);
-  else return hipErrorInvalidValue;
+  const hipError_t e = d == 64    ? launch_tiles<64>(p, a, blocks, s)
+                       : d == 128 ? launch_tiles<128>(p, a, blocks, s)
+                       : d == 256 ? launch_tiles<256>(p, a, blocks, s)
+                                  : hipErrorInvalidValue;
+  if (e != hipSuccess) return e;
   if (p.splits > 1) {
-    const dim3 grid((unsigned)rows);
-    if (d == 64) launch_kernel(k_kv_join<64>, grid, dim3(256), 0, s, a);
-    else if (d == 128) launch_kernel(k_kv_join<128>, grid, dim3(256), 0, s, a);
-    else launch_kernel(k_kv_join<256>, grid, dim3(256), 0, s, a);
+    if (d == 64) launch_join<64>(a, rows, s);
+    else if (d == 128) launch_join<128>(a, rows, s);
+    else launch_join<256>(a, rows, s);
   }
   return hipGetLastError();
 }
