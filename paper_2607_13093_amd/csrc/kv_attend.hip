@@ -78,10 +78,11 @@ __device__ __forceinline__ KvPages tile_pages(const KvArgs& a, const KvSession& 
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     const int at = pos + b * kKvBlock;
-    const int i = at >> a.page_shift;
-    // (the constant address space makes it a scalar load)
-    const int page = at < end && i < a.max_pages ? ((const __attribute__((address_space(4))) int32_t*)ses.table)[i] : -1;
-    p.page[b] = (unsigned)page < (unsigned)a.n_pages ? page : -1;
+    const int i = at >> a.page_shift, last = a.max_pages - 1;
+    // (read wherever it is, so that the load need not wait for the session's length;
+    // the constant address space makes it a scalar one)
+    const int page = ((const __attribute__((address_space(4))) int32_t*)ses.table)[i < last ? i : last];
+    p.page[b] = at < end && i <= last && (unsigned)page < (unsigned)a.n_pages ? page : -1;
   }
   return p;
 }
@@ -89,7 +90,7 @@ __device__ __forceinline__ KvPages tile_pages(const KvArgs& a, const KvSession& 
 // Copies of one tile into the stage `to`.  A block that does not exist is copied
 // from page 0 and not used.  lane16: the lane's 16 bytes (kept apart from the base,
 // which stays scalar); the offset operand counts for both sides.
-template <int D>
+template <int D, int AUX>
 __device__ __forceinline__ void copy_tile(uint8_t* to, const KvArgs& a, int head, int pos, const KvPages& pages,
                                           uint32_t& lane16, uint32_t lane) {
   const uint8_t* blk[2];
@@ -99,23 +100,23 @@ __device__ __forceinline__ void copy_tile(uint8_t* to, const KvArgs& a, int head
     const int page = pages.page[b];
     blk[b] = scalar_ptr(kv_block<D>(a, page < 0 ? 0 : page, head, page < 0 ? 0 : pos + b * kKvBlock));
     lds_void_t* at = (lds_void_t*)(to + b * 16 * D);
-    __builtin_amdgcn_global_load_lds(blk[b] + lane16, at, 16, 0, 0);
-    if constexpr (D >= 128) __builtin_amdgcn_global_load_lds(blk[b] + lane16, at, 16, 1024, 0);
+    __builtin_amdgcn_global_load_lds(blk[b] + lane16, at, 16, 0, AUX);
+    if constexpr (D >= 128) __builtin_amdgcn_global_load_lds(blk[b] + lane16, at, 16, 1024, AUX);
     if constexpr (D >= 256) {
-      __builtin_amdgcn_global_load_lds(blk[b] + lane16, at, 16, 2048, 0);
-      __builtin_amdgcn_global_load_lds(blk[b] + lane16, at, 16, 3072, 0);
+      __builtin_amdgcn_global_load_lds(blk[b] + lane16, at, 16, 2048, AUX);
+      __builtin_amdgcn_global_load_lds(blk[b] + lane16, at, 16, 3072, AUX);
     }
   }
   lds_void_t* at = (lds_void_t*)(to + Stage<D>::kCodes);
   if constexpr (D == 256) {  // 256 bytes of either block
     const uint32_t lane4 = lane16 / 4 + 16 * D;
-    __builtin_amdgcn_global_load_lds(blk[0] + lane4, at, 4, 0, 0);
-    __builtin_amdgcn_global_load_lds(blk[1] + lane4, (lds_void_t*)(to + Stage<D>::kCodes + 256), 4, 0, 0);
+    __builtin_amdgcn_global_load_lds(blk[0] + lane4, at, 4, 0, AUX);
+    __builtin_amdgcn_global_load_lds(blk[1] + lane4, (lds_void_t*)(to + Stage<D>::kCodes + 256), 4, 0, AUX);
   } else {                   // D bytes of either; for D 64 the last half of the lanes repeat the first
     const uint32_t in = lane * 4 % (2 * D);
     const uint64_t b0 = reinterpret_cast<uint64_t>(blk[0]), b1 = reinterpret_cast<uint64_t>(blk[1]);
     const uint64_t base = in < D ? b0 : b1;
-    __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint8_t*>(base) + (16 * D + in % D), at, 4, 0, 0);
+    __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint8_t*>(base) + (16 * D + in % D), at, 4, 0, AUX);
   }
 }
 
@@ -378,6 +379,9 @@ constexpr int rows_tiles(int d, int64_t rows) {
 template <int D, int MT, int WT>
 __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a) {
   constexpr int NS = stages_of(D);
+  // Waves that share all of a head's rows read each byte once: as a stream (one long
+  // session a head of 16 rows 166 -> 148 us, 20 rows 183 -> 169); others meet in L2.
+  constexpr int AUX = WT == 4 ? 2 : 0;
   constexpr int WR = 4 / WT;
   constexpr int KJ = D / 32;   // steps of the first product
   constexpr int VC = D / 16;   // products of the second
@@ -454,17 +458,11 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
 
   // The wave's tiles from `start` on, STEP tokens apart.  Those that all its rows
   // see whole, from `whole` to `part`, come first, then the others: the order of
-  // tokens is free.  A wave that finds a page missing takes all as the latter.
+  // tokens is free.
   constexpr int STEP = 32 * WT;
   const int start = from + 32 * wt;
   int whole = start + (all_lo > start ? (all_lo - start + STEP - 1) / STEP * STEP : 0);
   int part = whole + ((all_hi < to ? all_hi : to) - whole + STEP - 32) / STEP * STEP;
-  if (part > whole) {
-    bool missing = false;
-    for (int c = (whole >> a.kv.page_shift) + lane; c <= (part - STEP + 31) >> a.kv.page_shift; c += 64)
-      missing = missing || kv_page(a.kv, ses, c << a.kv.page_shift) < 0;
-    if (__any(missing)) part = whole;
-  }
   if (part <= whole) whole = part = start;
   const int n_whole = (part - whole) / STEP, n_head = (whole - start) / STEP;
   const int n_tiles = n_whole + n_head + (to > part ? (to - part + STEP - 1) / STEP : 0);
@@ -480,9 +478,15 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
   const uint32_t key_at = n * (D / 2) + g * (D / 8), value_at = KvLayout<D>::kValues + lane * (D / 8);
   const uint32_t ks_at = Stage<D>::kCodes + (D == 64 ? g >> 1 : D == 128 ? g : 2 * g) * kKvBlock + n;
   const uint32_t vs_at = Stage<D>::kCodes + D / 2 + n * D / 512 * kKvBlock + 4 * g;
+  uint32_t none = 0;  // of the tiles in flight, the next in the low bits: blocks without a page
+  auto none_of = [](const KvPages& p) { return (uint32_t)(p.page[0] < 0) | ((uint32_t)(p.page[1] < 0) << 1); };
 #pragma unroll
   for (int i = 0; i < NS - 1; ++i)
-    if (i < n_tiles) copy_tile<D>(ring + i * Stage<D>::kBytes, a.kv, head, place(i), tile_pages(a.kv, ses, place(i), to), lane16, lane);
+    if (i < n_tiles) {
+      const KvPages pages = tile_pages(a.kv, ses, place(i), to);
+      none |= none_of(pages) << (2 * i);
+      copy_tile<D, AUX>(ring + i * Stage<D>::kBytes, a.kv, head, place(i), pages, lane16, lane);
+    }
   if constexpr (QL) __syncthreads();
   else  // here, not in the loop: the compiler's wait would be for all copies in flight
 #pragma unroll
@@ -499,7 +503,8 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
   auto begin = [&] {
     const KvPages after = tile_pages(a.kv, ses, place(k + NS), to);
     if (k + NS - 1 < n_tiles) {
-      copy_tile<D>(ring + fill * Stage<D>::kBytes, a.kv, head, place(k + NS - 1), ahead, lane16, lane);
+      none |= none_of(ahead) << (2 * (NS - 1));
+      copy_tile<D, AUX>(ring + fill * Stage<D>::kBytes, a.kv, head, place(k + NS - 1), ahead, lane16, lane);
       wait_copies<(NS - 1) * Stage<D>::kCopies>();
     } else if (NS > 2 && k + 2 == n_tiles) {
       wait_copies<Stage<D>::kCopies>();
@@ -518,19 +523,29 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
   };
   for (; k < n_whole; ++k) {
     begin();
+    if (none & 3) {  // no such tokens: no weight, and values that zero times is zero
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        if ((none >> b) & 1) {
+          values.s[b] = 0u;
+#pragma unroll
+          for (int m = 0; m < MT; ++m) sc[m][b] = f32x4_t{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        }
+    }
+    none >>= 2;
     take_weights(p, w, sc, a);
     take_values(w, values, p);
   }
   for (; k < n_tiles; ++k) {
     const int t0 = place(k);
-    const KvPages here = tile_pages(a.kv, ses, t0, to);
+    begin();
     int held[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const int left = to - t0 - b * kKvBlock;
-      held[b] = here.page[b] < 0 ? 0 : (left < kKvBlock ? left : kKvBlock);
+      held[b] = (none >> b) & 1 ? 0 : (left < kKvBlock ? left : kKvBlock);
     }
-    begin();
+    none >>= 2;
     mask_scores(sc, pos, a.window, t0, held, g);
     take_weights(p, w, sc, a);
     clear_values(values, held, g);
@@ -762,6 +777,9 @@ Plan plan_of(int d, int64_t units, int64_t rows, int64_t span) {
     }
   }
   if (p.splits < 1) p.splits = 1;
+#ifdef FORCE
+  p.chunk = (int)(((span + FORCE - 1) / FORCE + step - 1) / step * step); p.splits = (int)((span + p.chunk - 1) / p.chunk);
+#endif
   return p;
 }
 
