@@ -243,22 +243,20 @@ __device__ __forceinline__ void take_keys(f32x4_t (&sc)[MT][2], const KvKeys<D>&
   }
 }
 
-// What row n of tile m, at position pos[m], does not see of 32 tokens from t0, of
-// which held[b] exist in either block.
+// What the lane's rows do not see of 32 tokens from t0: row n of tile m sees
+// span[m] tokens from first[m] on.
 template <int MT>
-__device__ __forceinline__ void mask_scores(f32x4_t (&sc)[MT][2], const int (&pos)[MT], int window, int t0,
-                                            const int (&held)[2], int g) {
+__device__ __forceinline__ void mask_scores(f32x4_t (&sc)[MT][2], const int (&first)[MT], const int (&span)[MT], int t0,
+                                            int g) {
 #pragma unroll
-  for (int b = 0; b < 2; ++b)
+  for (int m = 0; m < MT; ++m) {
+    const int from = t0 + 4 * g - first[m];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int in = 4 * g + e, j = t0 + b * kKvBlock + in;
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const bool sees = in < held[b] && j <= pos[m] && (window <= 0 || j > pos[m] - window);
-        sc[m][b][e] = sees ? sc[m][b][e] : -INFINITY;
-      }
-    }
+      for (int e = 0; e < 4; ++e)
+        sc[m][b][e] = (uint32_t)(from + b * kKvBlock + e) < (uint32_t)span[m] ? sc[m][b][e] : -INFINITY;
+  }
 }
 
 // Tokens that do not exist: what their bytes say is anything, and zero times it
@@ -373,6 +371,9 @@ constexpr int resident(int d, int mt, int wt) {  // workgroups of a CU
 constexpr int rows_tiles(int d, int64_t rows) {
   if (rows <= 16 || d == 256) return 1;
   if (rows <= 32) return 2;
+#ifdef T64
+  if (d == 64) return T64;
+#endif
   return d == 64 || rows <= 64 ? 4 : 2;
 }
 
@@ -407,12 +408,14 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
   Queries<D, MT, QL> q;
   q.l = s_q;
   q.own = wr * (MT * KJ * 64) + lane;
-  int pos[MT];
+  int first[MT], span[MT];  // the tokens that the lane's rows see
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     const int fq = row0 + m * 16 + n;
     const int r = fq / G;
-    pos[m] = fq < live ? base + r : -1;
+    const int pos = fq < live ? base + r : -1;
+    first[m] = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
+    span[m] = pos - first[m] + 1 > 0 ? pos - first[m] + 1 : 0;
     const uint16_t* p = a.q + ((int64_t)s * a.kv.R + r) * a.q_row + (int64_t)(head * G + fq - r * G) * a.q_head + g * (D / 4);
 #pragma unroll
     for (int j = 0; j < KJ; ++j) {
@@ -518,11 +521,6 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
     read_codes<D>(keys.c, keys.s[0], keys.s[1], at + key_at, at + ks_at, true);
     take_keys(sc, keys, q);
     read_codes<D>(values.c, values.s[0], values.s[1], at + value_at, at + vs_at, false);
-    stage = stage + 1 == NS ? 0 : stage + 1;
-    fill = fill + 1 == NS ? 0 : fill + 1;
-  };
-  for (; k < n_whole; ++k) {
-    begin();
     if (none & 3) {  // no such tokens: no weight, and values that zero times is zero
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -533,22 +531,23 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
         }
     }
     none >>= 2;
+    stage = stage + 1 == NS ? 0 : stage + 1;
+    fill = fill + 1 == NS ? 0 : fill + 1;
+  };
+  for (; k < n_whole; ++k) {
+    begin();
     take_weights(p, w, sc, a);
     take_values(w, values, p);
   }
   for (; k < n_tiles; ++k) {
     const int t0 = place(k);
     begin();
-    int held[2];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int left = to - t0 - b * kKvBlock;
-      held[b] = (none >> b) & 1 ? 0 : (left < kKvBlock ? left : kKvBlock);
-    }
-    none >>= 2;
-    mask_scores(sc, pos, a.window, t0, held, g);
+    mask_scores(sc, first, span, t0, g);
     take_weights(p, w, sc, a);
-    clear_values(values, held, g);
+    if (t0 + 32 > ses.len) {
+      const int held[2] = {ses.len - t0, ses.len - t0 - kKvBlock};
+      clear_values(values, held, g);
+    }
     take_values(w, values, p);
   }
 #pragma unroll
