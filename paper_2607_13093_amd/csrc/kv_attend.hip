@@ -91,7 +91,7 @@ __device__ __forceinline__ KvPages tile_pages(const KvArgs& a, const KvSession& 
 // from page 0 and not used.  lane16: the lane's 16 bytes (kept apart from the base,
 // which stays scalar); the offset operand counts for both sides.
 template <int D, int AUX>
-__device__ __forceinline__ void copy_tile(uint8_t* to, const KvArgs& a, int head, int pos, const KvPages& pages,
+__device__ __forceinline__ void copy_with(uint8_t* to, const KvArgs& a, int head, int pos, const KvPages& pages,
                                           uint32_t& lane16, uint32_t lane) {
   const uint8_t* blk[2];
   asm volatile("" : "+v"(lane16));
@@ -118,6 +118,16 @@ __device__ __forceinline__ void copy_tile(uint8_t* to, const KvArgs& a, int head
     const uint64_t base = in < D ? b0 : b1;
     __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint8_t*>(base) + (16 * D + in % D), at, 4, 0, AUX);
   }
+}
+
+// Codes that one workgroup alone reads go past the caches as a stream (192 sessions
+// with 16 rows of a head 166 -> 148 us, with 20 rows 183 -> 169); where tiles of
+// rows read the same ones they meet in L2.
+template <int D>
+__device__ __forceinline__ void copy_tile(uint8_t* to, const KvArgs& a, int head, int pos, const KvPages& pages,
+                                          uint32_t& lane16, uint32_t lane, bool alone) {
+  if (alone) copy_with<D, 2>(to, a, head, pos, pages, lane16, lane);
+  else copy_with<D, 0>(to, a, head, pos, pages, lane16, lane);
 }
 
 // At most N of the wave's newest copies may still be on their way.
@@ -367,22 +377,9 @@ constexpr int resident(int d, int mt, int wt) {  // workgroups of a CU
   const int by_lds = 160 * 1024 / attend_lds(d, mt, wt);
   return by_lds < waves_of(d, mt) ? by_lds : waves_of(d, mt);
 }
-// Tiles of a wave for so many rows of a head.
-constexpr int rows_tiles(int d, int64_t rows) {
-  if (rows <= 16 || d == 256) return 1;
-  if (rows <= 32) return 2;
-#ifdef T64
-  if (d == 64) return T64;
-#endif
-  return d == 64 || rows <= 64 ? 4 : 2;
-}
-
 template <int D, int MT, int WT>
 __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a) {
   constexpr int NS = stages_of(D);
-  // Waves that share all of a head's rows read each byte once: as a stream (one long
-  // session a head of 16 rows 166 -> 148 us, 20 rows 183 -> 169); others meet in L2.
-  constexpr int AUX = WT == 4 ? 2 : 0;
   constexpr int WR = 4 / WT;
   constexpr int KJ = D / 32;   // steps of the first product
   constexpr int VC = D / 16;   // products of the second
@@ -476,6 +473,7 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
 
   uint8_t* ring = smem + wave * (NS * Stage<D>::kBytes);
   uint32_t lane16 = lane * 16;
+  const bool alone = WT == 4 && a.tiles == 1;
   const uint32_t ring_at = (uint32_t)(uintptr_t)(lds_void_t*)ring;
   // the lane's places in a stage: keys token n of a block, values as they lie
   const uint32_t key_at = n * (D / 2) + g * (D / 8), value_at = KvLayout<D>::kValues + lane * (D / 8);
@@ -488,7 +486,7 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
     if (i < n_tiles) {
       const KvPages pages = tile_pages(a.kv, ses, place(i), to);
       none |= none_of(pages) << (2 * i);
-      copy_tile<D, AUX>(ring + i * Stage<D>::kBytes, a.kv, head, place(i), pages, lane16, lane);
+      copy_tile<D>(ring + i * Stage<D>::kBytes, a.kv, head, place(i), pages, lane16, lane, alone);
     }
   if constexpr (QL) __syncthreads();
   else  // here, not in the loop: the compiler's wait would be for all copies in flight
@@ -507,7 +505,7 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
     const KvPages after = tile_pages(a.kv, ses, place(k + NS), to);
     if (k + NS - 1 < n_tiles) {
       none |= none_of(ahead) << (2 * (NS - 1));
-      copy_tile<D, AUX>(ring + fill * Stage<D>::kBytes, a.kv, head, place(k + NS - 1), ahead, lane16, lane);
+      copy_tile<D>(ring + fill * Stage<D>::kBytes, a.kv, head, place(k + NS - 1), ahead, lane16, lane, alone);
       wait_copies<(NS - 1) * Stage<D>::kCopies>();
     } else if (NS > 2 && k + 2 == n_tiles) {
       wait_copies<Stage<D>::kCopies>();
@@ -741,45 +739,44 @@ struct Plan {
 // units: sessions times key/value heads; rows: of one head; span: tokens that a
 // row sees at most.
 Plan plan_of(int d, int64_t units, int64_t rows, int64_t span) {
-  Plan p;
-  p.mt = rows_tiles(d, rows);
-  p.wt = 4;
-  while (p.wt > 1 && rows > 16 * p.mt * (4 / p.wt)) p.wt /= 2;
-  const int per = 16 * p.mt * (4 / p.wt);
-  p.tiles = (int)((rows + per - 1) / per);
-
-  // Shares: as few as keep the chip busy, by a rough account in microseconds.  A
-  // workgroup starts and ends in about 5; a tile of a wave is the issue of its
-  // instructions (a third more for what does not overlap) times the waves that
-  // share a SIMD, or a wave's own latencies; joining costs a launch and the
-  // partial outputs' way out and back.
-  const double issue = (4.0 * (0.9 * d + 20 + 36 * p.mt) + (32.0 + d / 2.0) * p.mt) * 1.35 / 2100;
-  const int64_t slots = (int64_t)kCUs * resident(d, p.mt, p.wt);
-  const int64_t blocks = units * p.tiles, step = 32 * p.wt;
-  auto workgroup = [&](int64_t n, int64_t tokens) {  // n of them at a time
-    const double beside = (double)((n + kCUs - 1) / kCUs);
-    const double tile = beside * issue > issue + 0.7 ? beside * issue : issue + 0.7;
-    return 5.0 + (double)((tokens + step - 1) / step) * tile;
-  };
-  p.splits = 1;
-  p.chunk = (int)((span + step - 1) / step * step);
-  double best = 0;
-  for (int64_t n = 1; n <= 128 && (n == 1 || n * step <= span + step - 1); n += n < 8 ? 1 : n / 4) {
-    const int64_t chunk = ((span + n - 1) / n + step - 1) / step * step;
-    const int64_t all = blocks * n, last = all % slots;
-    double t = (double)(all / slots) * workgroup(slots, chunk) + (last > 0 ? workgroup(last, chunk) : 0.0);
-    if (n > 1) t += 4.0 + (double)(units * rows * n) * (d * 8 + 16) / 4e6;
-    if (n == 1 || t < 0.97 * best) {
-      best = t;
-      p.splits = (int)((span + chunk - 1) / chunk);
-      p.chunk = (int)chunk;
+  // Row tiles and waves by head size: many rows a wave share the conversion of the
+  // codes, waves that share rows make more workgroups of them.
+  static constexpr int kShapes[3][5][2] = {{{1, 4}, {2, 4}, {4, 4}, {4, 2}, {4, 1}},
+                                           {{1, 4}, {2, 4}, {4, 4}, {2, 2}, {2, 1}},
+                                           {{1, 4}, {1, 2}, {1, 1}, {0, 0}, {0, 0}}};
+  Plan best{};
+  double least = 0;
+  for (const auto& shape : kShapes[d / 128]) {
+    const int mt = shape[0], wt = shape[1];
+    if (mt == 0) break;
+    const int per = 16 * mt * (4 / wt);
+    const int64_t tiles = (rows + per - 1) / per, blocks = units * tiles, step = 32 * wt;
+    const int64_t slots = (int64_t)kCUs * resident(d, mt, wt);
+    // A rough account in microseconds.  A workgroup starts and ends in about 5 (more
+    // where its waves join many outputs); a tile of a wave is the issue of its instructions (a third more for what does not
+    // overlap) times the waves that share a SIMD, or a wave's own latencies; joining
+    // shares costs a launch and the partial outputs' way out and back.
+    const double issue = (4.0 * (0.9 * d + 20 + 36 * mt) + (32.0 + d / 2.0) * mt) * 1.35 / 2100;
+    auto workgroup = [&](int64_t n, int64_t tokens) {  // n of them at a time
+      const double beside = (double)((n + kCUs - 1) / kCUs);
+      const double tile = beside * issue > issue + 0.7 ? beside * issue : issue + 0.7;
+      return (wt > 1 ? 5.0 + 1.5 * mt : 5.0) + (double)((tokens + step - 1) / step) * tile;
+    };
+    for (int64_t n = 1; n <= 128 && (n == 1 || n * step <= span + step - 1); n += n < 8 ? 1 : n / 4) {
+      const int64_t chunk = ((span + n - 1) / n + step - 1) / step * step;
+      const int64_t all = blocks * n, last = all % slots;
+      double t = (double)(all / slots) * workgroup(slots, chunk) + (last > 0 ? workgroup(last, chunk) : 0.0);
+      // (tiles of rows see less and less: the last ones fill the gaps)
+      if (tiles > 1 && all > slots) t = ((double)all / (double)slots + 0.1) * workgroup(slots, chunk);
+      if (n > 1) t += 4.0 + (double)(units * rows * n) * (d * 8 + 16) / 4e6;
+      if (best.mt == 0 || t < 0.97 * least) {
+        least = t;
+        best = Plan{mt, wt, (int)tiles, (int)((span + chunk - 1) / chunk), (int)chunk};
+      }
     }
   }
-  if (p.splits < 1) p.splits = 1;
-#ifdef FORCE
-  p.chunk = (int)(((span + FORCE - 1) / FORCE + step - 1) / step * step); p.splits = (int)((span + p.chunk - 1) / p.chunk);
-#endif
-  return p;
+  if (best.splits < 1) best.splits = 1;
+  return best;
 }
 
 int64_t span_of(int64_t max_len, int64_t rows, int64_t window) {
@@ -796,19 +793,19 @@ hipError_t launch_one(const AttendArgs& a, int64_t blocks, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int D, int MT>
-hipError_t launch_waves(const Plan& p, const AttendArgs& a, int64_t blocks, hipStream_t s) {
-  if (p.wt == 4) return launch_one<D, MT, 4>(a, blocks, s);
-  if (p.wt == 2) return launch_one<D, MT, 2>(a, blocks, s);
-  return launch_one<D, MT, 1>(a, blocks, s);
-}
-
 template <int D>
 hipError_t launch_tiles(const Plan& p, const AttendArgs& a, int64_t blocks, hipStream_t s) {
-  if (p.mt == 1) return launch_waves<D, 1>(p, a, blocks, s);
-  if (p.mt == 2) return launch_waves<D, 2>(p, a, blocks, s);
-  if constexpr (D < 256) return launch_waves<D, 4>(p, a, blocks, s);
-  return hipErrorInvalidValue;
+  if (p.mt == 1 && p.wt == 4) return launch_one<D, 1, 4>(a, blocks, s);
+  if constexpr (D == 256) {
+    if (p.wt == 2) return launch_one<D, 1, 2>(a, blocks, s);
+    return launch_one<D, 1, 1>(a, blocks, s);
+  } else {
+    if (p.mt == 2 && p.wt == 4) return launch_one<D, 2, 4>(a, blocks, s);
+    if (p.mt == 4 && p.wt == 4) return launch_one<D, 4, 4>(a, blocks, s);
+    constexpr int M = D == 64 ? 4 : 2;
+    if (p.wt == 2) return launch_one<D, M, 2>(a, blocks, s);
+    return launch_one<D, M, 1>(a, blocks, s);
+  }
 }
 
 }  // namespace
