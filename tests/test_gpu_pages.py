@@ -66,6 +66,8 @@ class Both:
 @pytest.mark.parametrize("page", [16, 64])
 @pytest.mark.parametrize("n_pages,n_slots,max_pages,layers,heads", [
     (40, 5, 9, 1, 1), (300, 17, 40, 3, 2), (5000, 40, 200, 2, 1), (9000, 3, 4000, 1, 1),
+    # past what one workgroup takes: pages, slots
+    (140000, 6, 30000, 1, 1), (6000, 4500, 5, 1, 1),
 ])
 def test_random_walk(n_pages, n_slots, max_pages, layers, heads, page):
     rng = np.random.default_rng(n_pages + page)
@@ -85,6 +87,20 @@ def test_random_walk(n_pages, n_slots, max_pages, layers, heads, page):
             b.fork(order[:1].tolist() * k if step < 6 else order[:k].tolist(), order[k:2 * k].tolist())
         else:
             b.compact(apart=step > 6)
+        b.same()
+
+
+def test_growth_finds_pages_far_back():
+    # free pages only at the end of the pool, as many as are needed
+    for n_pages in (100, 20000, 131072, 131073):
+        say("far back", n_pages)
+        b = Both(n_pages, 3, n_pages, 16, layers=1)
+        b.grow([(n_pages - 5) * 16, 0, 0])
+        b.grow([0, 33, 32])
+        b.same()
+        b.grow([1, 0, 0])
+        b.trim([0, 33, 32])
+        b.grow([5, 5, 5])
         b.same()
 
 
