@@ -336,7 +336,7 @@ __device__ __forceinline__ void take_values(Rows<D, MT>& w, const KvValues<D>& v
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[b][i] = e8m0_operand((v.s[b] >> (8 * i)) & 0xFFu);
+    for (int i = 0; i < 4; ++i) s[b][i] = e8m0_operand_at(v.s[b], i);
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) {
     uint32_t x8[8];
@@ -762,7 +762,9 @@ Plan plan_of(int d, int64_t units, int64_t rows, int64_t span) {
       const double tile = beside * issue > issue + 0.7 ? beside * issue : issue + 0.7;
       return (wt > 1 ? 5.0 + 1.5 * mt : 5.0) + (double)((tokens + step - 1) / step) * tile;
     };
-    for (int64_t n = 1; n <= 128 && (n == 1 || n * step <= span + step - 1); n += n < 8 ? 1 : n / 4) {
+    static constexpr int kShares[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80, 96, 128};
+    for (const int64_t n : kShares) {
+      if (n > 1 && n * step > span + step - 1) break;
       const int64_t chunk = ((span + n - 1) / n + step - 1) / step * step;
       const int64_t all = blocks * n, last = all % slots;
       double t = (double)(all / slots) * workgroup(slots, chunk) + (last > 0 ? workgroup(last, chunk) : 0.0);

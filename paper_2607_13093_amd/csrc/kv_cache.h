@@ -137,6 +137,24 @@ __device__ __forceinline__ uint8_t* kv_block(const KvArgs& a, int page, int head
 // 2^-127, byte 255 NaN).
 __device__ __forceinline__ float e8m0_operand(uint32_t byte) { return __uint_as_float(byte << 23); }
 
+// The same for a byte of a word, number a constant: one instruction with the byte
+// selected by its operand (the compiler makes two of three of them a shift and a mask).
+__device__ __forceinline__ float e8m0_operand_at(uint32_t word, int byte) {
+  uint32_t r;
+  const uint32_t by = 23;
+#define SPH_BYTE(N)                                                                                  \
+  asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_" #N \
+      : "=v"(r) : "v"(by), "v"(word))
+  switch (byte) {
+    case 0: SPH_BYTE(0); break;
+    case 1: SPH_BYTE(1); break;
+    case 2: SPH_BYTE(2); break;
+    default: SPH_BYTE(3); break;
+  }
+#undef SPH_BYTE
+  return __uint_as_float(r);
+}
+
 // Two E2M1 codes of a byte as bf16, exact (but for scales near the ends of the
 // exponent range).
 template <int BYTE>

@@ -204,7 +204,7 @@ __global__ __launch_bounds__(256) void k_grow_apply(PagesArgs a, const int32_t* 
 // All of that by one workgroup, for pools and tables that fit its LDS: it looks at
 // pages from the lowest on until there are enough free ones, which a pool that is
 // not nearly full has among its first.  (One launch less, 3.7 us of the host's time:
-// 256 sessions giving back and taking 8 rows in 65536 pages 18.3 -> 15.9 us.)
+// 256 sessions giving back and taking 8 rows in 65536 pages 18.3 -> 14.8 us.)
 constexpr int kOnePages = 131072, kOneSlots = 4096;
 __global__ __launch_bounds__(1024) void k_grow_one(PagesArgs a, const int32_t* add, GrowScratch w, int32_t* status) {
   constexpr int kWords = kOnePages / 64, kLook = 16;  // words of 64 pages; pages a thread looks at in a turn
