@@ -253,19 +253,20 @@ __device__ __forceinline__ void take_keys(f32x4_t (&sc)[MT][2], const KvKeys<D>&
   }
 }
 
-// What the lane's rows do not see of 32 tokens from t0: row n of tile m sees
-// span[m] tokens from first[m] on.
+// What the lane's rows do not see of 32 tokens from t0: row n of tile m, at
+// position pos[m], sees `window` tokens up to its own.
 template <int MT>
-__device__ __forceinline__ void mask_scores(f32x4_t (&sc)[MT][2], const int (&first)[MT], const int (&span)[MT], int t0,
-                                            int g) {
+__device__ __forceinline__ void mask_scores(f32x4_t (&sc)[MT][2], const int (&pos)[MT], int window, int t0, int g) {
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    const int from = t0 + 4 * g - first[m];
+    const int most = pos[m] < 0 ? 0 : pos[m] + 1;
+    const int span = window > 0 && window < most ? window : most;  // its tokens, up to pos
+    const int from = t0 + 4 * g - (pos[m] - span + 1);
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        sc[m][b][e] = (uint32_t)(from + b * kKvBlock + e) < (uint32_t)span[m] ? sc[m][b][e] : -INFINITY;
+        sc[m][b][e] = (uint32_t)(from + b * kKvBlock + e) < (uint32_t)span ? sc[m][b][e] : -INFINITY;
   }
 }
 
@@ -361,8 +362,8 @@ __device__ __forceinline__ void take_values(Rows<D, MT>& w, const KvValues<D>& v
   }
 }
 
-// A workgroup is 4 waves: WT of them share the tokens of the same rows, 4 / WT
-// have rows of their own.
+// A workgroup is 4 waves: WT of them (4 or 2) share the tokens of the same rows,
+// 4 / WT have rows of their own.
 // Waves of a SIMD (workgroups of a CU) that the registers leave room for, and the
 // stages of a ring.
 constexpr int waves_of(int d, int mt) { return d * mt <= 128 ? 4 : (mt < 4 && d * mt <= 256 ? 3 : 2); }
@@ -370,7 +371,7 @@ constexpr int stages_of(int d) { return d == 64 ? 4 : (d == 128 ? 3 : 2); }
 // LDS of a workgroup: rings and queries, in their place the waves' outputs.
 constexpr int attend_lds(int d, int mt, int wt) {
   const int run = 4 * stages_of(d) * ((34 * d + 255) / 256 * 256) + (d * mt >= kQueriesInLds ? 4 / wt * mt * (d / 32) * 1024 : 0);
-  const int end = wt > 1 ? 256 * d + 512 * mt : 0;
+  const int end = 256 * d + 512 * mt;
   return run > end ? run : end;
 }
 constexpr int resident(int d, int mt, int wt) {  // workgroups of a CU
@@ -405,14 +406,12 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
   Queries<D, MT, QL> q;
   q.l = s_q;
   q.own = wr * (MT * KJ * 64) + lane;
-  int first[MT], span[MT];  // the tokens that the lane's rows see
+  int pos[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     const int fq = row0 + m * 16 + n;
     const int r = fq / G;
-    const int pos = fq < live ? base + r : -1;
-    first[m] = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
-    span[m] = pos - first[m] + 1 > 0 ? pos - first[m] + 1 : 0;
+    pos[m] = fq < live ? base + r : -1;
     const uint16_t* p = a.q + ((int64_t)s * a.kv.R + r) * a.q_row + (int64_t)(head * G + fq - r * G) * a.q_head + g * (D / 4);
 #pragma unroll
     for (int j = 0; j < KJ; ++j) {
@@ -540,7 +539,7 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
   for (; k < n_tiles; ++k) {
     const int t0 = place(k);
     begin();
-    mask_scores(sc, first, span, t0, g);
+    mask_scores(sc, pos, a.window, t0, g);
     take_weights(p, w, sc, a);
     if (t0 + 32 > ses.len) {
       const int held[2] = {ses.len - t0, ses.len - t0 - kKvBlock};
@@ -552,62 +551,53 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
   for (int m = 0; m < MT; ++m) w.sum[m] = sum_over_groups(w.sum[m]);
 
   // lane l holds row n, dimensions (4 g + e) D/16 + c = w.o[m][c][e]
+  // (what the rows are is worked out again: kept since the start it would be spilled
+  // around the loop, and waited for here; 192 sessions with 20 rows of a head 175 -> 163 us)
+  int heads_of = G, row_first = row0;
+  asm volatile("" : "+s"(heads_of), "+s"(row_first));
   // (in what were rings)
   float* s_o = reinterpret_cast<float*>(smem);       // 4 x 16 D
   float* s_ml = reinterpret_cast<float*>(smem) + 64 * D;
-  if constexpr (WT > 1) {
-    __syncthreads();
-    if (g == 0)
+  __syncthreads();
+  if (g == 0)
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        s_ml[((wave * MT + m) * 16 + n) * 2] = w.top[m];
-        s_ml[((wave * MT + m) * 16 + n) * 2 + 1] = w.sum[m];
-      }
-    __syncthreads();
-  }
+    for (int m = 0; m < MT; ++m) {
+      s_ml[((wave * MT + m) * 16 + n) * 2] = w.top[m];
+      s_ml[((wave * MT + m) * 16 + n) * 2 + 1] = w.sum[m];
+    }
+  __syncthreads();
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    float t = w.top[m], l = w.sum[m];
-    constexpr int PER = WT > 1 ? (D / 4) / WT : D / 4;  // values a lane ends with
-    float y[PER];
-    int d0;  // its first dimension
-    if constexpr (WT > 1) {
-      t = kNoScore;
+    constexpr int PER = D / 4 / WT;  // values a lane ends with
+    float t = kNoScore, l = 0.0f;
 #pragma unroll
-      for (int k = 0; k < WT; ++k) t = fmaxf(t, s_ml[(((wr * WT + k) * MT + m) * 16 + n) * 2]);
-      l = 0.0f;
+    for (int k = 0; k < WT; ++k) t = fmaxf(t, s_ml[(((wr * WT + k) * MT + m) * 16 + n) * 2]);
 #pragma unroll
-      for (int k = 0; k < WT; ++k) {
-        const float* ml = &s_ml[(((wr * WT + k) * MT + m) * 16 + n) * 2];
-        l += ml[1] * __builtin_amdgcn_exp2f((ml[0] - t) * a.scale_log2);
-      }
-      const float f = __builtin_amdgcn_exp2f((w.top[m] - t) * a.scale_log2);
-      if (m > 0) __syncthreads();
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int c = 0; c < VC; ++c) s_o[((wave * 4 + e) * VC + c) * 64 + lane] = w.o[m][c][e] * f;
-      __syncthreads();
-      // wave wt of WT sums its share of the (e, c) pairs over the WT waves
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        float x = 0.0f;
-#pragma unroll
-        for (int k = 0; k < WT; ++k) x += s_o[((wr * WT + k) * 4 * VC + wt * PER + i) * 64 + lane];
-        y[i] = x;
-      }
-      d0 = g * (D / 4) + wt * PER;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int c = 0; c < VC; ++c) y[e * VC + c] = w.o[m][c][e];
-      d0 = g * (D / 4);
+    for (int k = 0; k < WT; ++k) {
+      const float* ml = &s_ml[(((wr * WT + k) * MT + m) * 16 + n) * 2];
+      l += ml[1] * __builtin_amdgcn_exp2f((ml[0] - t) * a.scale_log2);
     }
-    const int fq = row0 + m * 16 + n;
+    const float f = __builtin_amdgcn_exp2f((w.top[m] - t) * a.scale_log2);
+    if (m > 0) __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int c = 0; c < VC; ++c) s_o[((wave * 4 + e) * VC + c) * 64 + lane] = w.o[m][c][e] * f;
+    __syncthreads();
+    // wave wt of WT sums its share of the (e, c) pairs over the WT waves
+    float y[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      float x = 0.0f;
+#pragma unroll
+      for (int k = 0; k < WT; ++k) x += s_o[((wr * WT + k) * 4 * VC + wt * PER + i) * 64 + lane];
+      y[i] = x;
+    }
+    const int d0 = g * (D / 4) + wt * PER;  // the first of them
+    const int fq = row_first + m * 16 + n;
     if (fq >= live) l = 0.0f;  // rows that are none
     if (fq < total) {
-      const int r = fq / G, hq = head * G + fq - r * G;
+      const int r = fq / heads_of, hq = head * heads_of + fq - r * heads_of;
       const int64_t row = (int64_t)s * a.kv.R + r;
       if (a.splits == 1) {
         const float f = l == 0.0f ? 0.0f : 1.0f / l;
@@ -622,11 +612,11 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
             dst[i + 1] = (uint16_t)(w >> 16);
           }
         }
-        if (a.lse && g == 0 && (WT == 1 || wt == 0))
+        if (a.lse && g == 0 && wt == 0)
           a.lse[row * (a.kv.heads * G) + hq] = l == 0.0f ? -INFINITY : fmaf(t, a.scale, __builtin_amdgcn_logf(l) * kLn2);
       } else {
         const int64_t at = (row * (a.kv.heads * G) + hq) * a.splits + split;
-        if (g == 0 && (WT == 1 || wt == 0)) a.part_ml[at] = make_float2(t, l);
+        if (g == 0 && wt == 0) a.part_ml[at] = make_float2(t, l);
         if (!(l == 0.0f)) {
 #pragma unroll
           for (int i = 0; i < PER; i += 4)
@@ -736,31 +726,34 @@ struct Plan {
   int splits, chunk;   // shares of the tokens, tokens of one
 };
 
-// units: sessions times key/value heads; rows: of one head; span: tokens that a
-// row sees at most.
-Plan plan_of(int d, int64_t units, int64_t rows, int64_t span) {
-  // Row tiles and waves by head size: many rows a wave share the conversion of the
-  // codes, waves that share rows make more workgroups of them.
-  static constexpr int kShapes[3][5][2] = {{{1, 4}, {2, 4}, {4, 4}, {4, 2}, {4, 1}},
-                                           {{1, 4}, {2, 4}, {4, 4}, {2, 2}, {2, 1}},
-                                           {{1, 4}, {1, 2}, {1, 1}, {0, 0}, {0, 0}}};
+// units: sessions times key/value heads; group: query heads of one of those; R rows
+// of a session, which has max_len tokens at most.
+Plan plan_of(int d, int64_t units, int64_t R, int64_t group, int64_t max_len, int64_t window) {
+  const int64_t rows = R * group;
+  // Row tiles of a wave and waves that share its rows: many rows share the conversion
+  // of the codes (a long prompt of 128 dimensions, us: 1450 with {2, 1}, 1215 with
+  // {4, 4}), few make more workgroups (sliding window, 64 dimensions: 82 and 67).
+  static constexpr int kShapes[4][2] = {{1, 4}, {2, 4}, {4, 4}, {2, 2}}, kWide[2][2] = {{1, 4}, {1, 2}};
   Plan best{};
   double least = 0;
-  for (const auto& shape : kShapes[d / 128]) {
-    const int mt = shape[0], wt = shape[1];
-    if (mt == 0) break;
+  for (int i = 0; i < (d == 256 ? 2 : 4); ++i) {
+    const int mt = d == 256 ? kWide[i][0] : kShapes[i][0], wt = d == 256 ? kWide[i][1] : kShapes[i][1];
     const int per = 16 * mt * (4 / wt);
     const int64_t tiles = (rows + per - 1) / per, blocks = units * tiles, step = 32 * wt;
     const int64_t slots = (int64_t)kCUs * resident(d, mt, wt);
-    // A rough account in microseconds.  A workgroup starts and ends in about 5 (more
-    // where its waves join many outputs); a tile of a wave is the issue of its instructions (a third more for what does not
-    // overlap) times the waves that share a SIMD, or a wave's own latencies; joining
-    // shares costs a launch and the partial outputs' way out and back.
+    // tokens that a workgroup's rows see
+    const int64_t wide = window + (per < rows ? per : rows) / group + 32;
+    const int64_t span = window > 0 && wide < max_len ? wide : max_len;
+    // A rough account in microseconds.  A workgroup starts and ends in about 5 and
+    // joins its waves' outputs; a tile of a wave is the issue of its instructions (a
+    // third more for what does not overlap) times the waves that share a SIMD, or a
+    // wave's own latencies; joining shares costs a launch and the partial outputs'
+    // way out and back.
     const double issue = (4.0 * (0.9 * d + 20 + 36 * mt) + (32.0 + d / 2.0) * mt) * 1.35 / 2100;
     auto workgroup = [&](int64_t n, int64_t tokens) {  // n of them at a time
       const double beside = (double)((n + kCUs - 1) / kCUs);
       const double tile = beside * issue > issue + 0.7 ? beside * issue : issue + 0.7;
-      return (wt > 1 ? 5.0 + 1.5 * mt : 5.0) + (double)((tokens + step - 1) / step) * tile;
+      return 5.0 + 1.5 * mt + (double)((tokens + step - 1) / step) * tile;
     };
     static constexpr int kShares[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80, 96, 128};
     for (const int64_t n : kShares) {
@@ -781,10 +774,6 @@ Plan plan_of(int d, int64_t units, int64_t rows, int64_t span) {
   return best;
 }
 
-int64_t span_of(int64_t max_len, int64_t rows, int64_t window) {
-  return window > 0 && window + rows + 31 < max_len ? window + rows + 31 : max_len;
-}
-
 template <int D, int MT, int WT>
 hipError_t launch_one(const AttendArgs& a, int64_t blocks, hipStream_t s) {
   constexpr size_t lds = attend_lds(D, MT, WT);
@@ -798,16 +787,10 @@ hipError_t launch_one(const AttendArgs& a, int64_t blocks, hipStream_t s) {
 template <int D>
 hipError_t launch_tiles(const Plan& p, const AttendArgs& a, int64_t blocks, hipStream_t s) {
   if (p.mt == 1 && p.wt == 4) return launch_one<D, 1, 4>(a, blocks, s);
-  if constexpr (D == 256) {
-    if (p.wt == 2) return launch_one<D, 1, 2>(a, blocks, s);
-    return launch_one<D, 1, 1>(a, blocks, s);
-  } else {
-    if (p.mt == 2 && p.wt == 4) return launch_one<D, 2, 4>(a, blocks, s);
-    if (p.mt == 4 && p.wt == 4) return launch_one<D, 4, 4>(a, blocks, s);
-    constexpr int M = D == 64 ? 4 : 2;
-    if (p.wt == 2) return launch_one<D, M, 2>(a, blocks, s);
-    return launch_one<D, M, 1>(a, blocks, s);
-  }
+  if constexpr (D == 256) return launch_one<D, 1, 2>(a, blocks, s);
+  else if (p.wt == 2) return launch_one<D, 2, 2>(a, blocks, s);
+  else if (p.mt == 2) return launch_one<D, 2, 4>(a, blocks, s);
+  else return launch_one<D, 4, 4>(a, blocks, s);
 }
 
 }  // namespace
@@ -815,7 +798,7 @@ hipError_t launch_tiles(const Plan& p, const AttendArgs& a, int64_t blocks, hipS
 // Workspace: the shares' maxima and sums, then their outputs.
 size_t kv_attend_scratch(int d, int64_t n_sessions, int64_t R, int64_t heads, int64_t q_heads,
                          int64_t max_len, int64_t window) {
-  const Plan p = plan_of(d, n_sessions * heads, R * (q_heads / heads), span_of(max_len, R, window));
+  const Plan p = plan_of(d, n_sessions * heads, R, q_heads / heads, max_len, window);
   if (p.splits <= 1) return 0;
   const size_t n = (size_t)n_sessions * R * q_heads * p.splits;
   return (n * 8 + 255) / 256 * 256 + n * d * 4;
@@ -840,7 +823,7 @@ hipError_t launch_kv_attend(int d, const KvArgs& kv, const AttendCall& c, void* 
   a.q_aligned = c.q_row % 8 == 0 && c.q_head % 8 == 0 && (reinterpret_cast<uintptr_t>(c.q) & 15) == 0;
   a.o_aligned = c.o_row % 2 == 0 && c.o_head % 2 == 0 && (reinterpret_cast<uintptr_t>(c.out) & 3) == 0;
   const int64_t units = (int64_t)kv.n_sessions * kv.heads;
-  const Plan p = plan_of(d, units, (int64_t)kv.R * a.group, span_of(c.max_len, kv.R, c.window));
+  const Plan p = plan_of(d, units, kv.R, a.group, c.max_len, c.window);
   a.tiles = p.tiles;
   a.splits = p.splits;
   a.chunk = p.chunk;
