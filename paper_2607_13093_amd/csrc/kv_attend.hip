@@ -763,7 +763,7 @@ Plan plan_of(int d, int64_t units, int64_t R, int64_t group, int64_t max_len, in
       double t = (double)(all / slots) * workgroup(slots, chunk) + (last > 0 ? workgroup(last, chunk) : 0.0);
       // (tiles of rows see less and less: the last ones fill the gaps)
       if (tiles > 1 && all > slots) t = ((double)all / (double)slots + 0.1) * workgroup(slots, chunk);
-      if (n > 1) t += 4.0 + (double)(units * rows * n) * (d * 8 + 16) / 4e6;
+      if (n > 1) t += 6.0 + (double)(units * rows * n) * (d * 8 + 16) / 4e6;
       if (best.mt == 0 || t < 0.97 * least) {
         least = t;
         best = Plan{mt, wt, (int)tiles, (int)((span + chunk - 1) / chunk), (int)chunk};
@@ -802,6 +802,13 @@ size_t kv_attend_scratch(int d, int64_t n_sessions, int64_t R, int64_t heads, in
   if (p.splits <= 1) return 0;
   const size_t n = (size_t)n_sessions * R * q_heads * p.splits;
   return (n * 8 + 255) / 256 * 256 + n * d * 4;
+}
+
+void kv_attend_shape(int d, int64_t n_sessions, int64_t R, int64_t heads, int64_t q_heads, int64_t max_len,
+                     int64_t window, int shape[5]) {
+  const Plan p = plan_of(d, n_sessions * heads, R, q_heads / heads, max_len, window);
+  const int out[5] = {p.mt, p.wt, p.tiles, p.splits, p.chunk};
+  for (int i = 0; i < 5; ++i) shape[i] = out[i];
 }
 
 hipError_t launch_kv_attend(int d, const KvArgs& kv, const AttendCall& c, void* workspace, hipStream_t s) {

@@ -87,6 +87,10 @@ hipError_t launch_kv_rows(bool append, int d, const KvArgs& a, const void* k, in
                           hipStream_t s);
 size_t kv_attend_scratch(int d, int64_t n_sessions, int64_t R, int64_t heads, int64_t q_heads,
                          int64_t max_len, int64_t window);
+// How such a call is shared out: row tiles of a wave, waves that share its rows,
+// workgroups for the rows of a head, shares of the tokens, tokens of a share.
+void kv_attend_shape(int d, int64_t n_sessions, int64_t R, int64_t heads, int64_t q_heads, int64_t max_len,
+                     int64_t window, int shape[5]);
 hipError_t launch_kv_attend(int d, const KvArgs& kv, const AttendCall& c, void* workspace, hipStream_t s);
 
 size_t pages_grow_scratch(int64_t n_pages, int64_t n_slots);
