@@ -441,6 +441,7 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
       all_lo = base + r_hi - a.window + 1;
     }
     lo = lo > 0 ? lo & ~31 : 0;
+    hi = hi > 0 ? hi : 0;  // rows before the first token see none, and name no page
   }
   // the share of this workgroup; the last takes what is left
   const int from = lo + split * a.chunk;

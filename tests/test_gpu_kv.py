@@ -198,6 +198,19 @@ def test_attend_prompts(hq, hkv, d, page, R, lens, rows, window):
     _check(c, q, q64, k, v, R, d ** -0.5, lens, rows=rows, window=window)
 
 
+@pytest.mark.parametrize("hq,d,R,lens,window", [
+    (1, 128, 400, [3, 0, 40], 0),                  # whole tiles of rows stand before the first token
+    (3, 64, 77, [0, 1], 5),
+    (8, 256, 130, [2, 129, 16], 0),
+])
+def test_more_rows_than_tokens(hq, d, R, lens, window):
+    rng = np.random.default_rng(R + d)
+    say("more rows than tokens", hq, d, R, lens, window)
+    c, k, v = filled(rng, lens, 1, d, 16)
+    q, q64 = bf16(rng, len(lens) * R, hq, d, scale=2.0)
+    _check(c, q, q64, k, v, R, d ** -0.5, lens, window=window)
+
+
 def test_wrong_hints_change_nothing_but_the_sharing():
     rng = np.random.default_rng(21)
     lens = [3000, 10, 2000]
