@@ -619,7 +619,7 @@ def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, rows_per_session: int
     M, heads = q.shape[0], q.shape[1]
     n = _kv_sessions(M, R)
     if out is None:
-        out = (torch.empty((M, heads, cache.head_dim), dtype=torch.bfloat16, device=dev),
+        out = (torch.empty_like(q) if q.is_contiguous() else q.new_empty((M, heads, cache.head_dim)),
                torch.empty((M, heads), dtype=torch.float32, device=dev) if want_lse else None)
     o, lse = out
     os = _kv_rows("out", o, heads, cache.head_dim, dev)

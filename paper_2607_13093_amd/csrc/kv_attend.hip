@@ -16,6 +16,8 @@
 // and the scores that lane l receives, row n of the tile against tokens
 // 4 g ... 4 g + 3 of both blocks, are its operand of the second product.  A
 // lane's outputs are D/4 neighbouring values of one row.
+#include <array>
+
 #include "kv_cache.h"
 #include "mfma_tile.h"
 
@@ -33,6 +35,7 @@ struct AttendArgs {
   float scale, scale_log2;
   float late;            // kLate binades of weight, as a difference of raw scores
   bool q_aligned, o_aligned;
+  int order;             // sessions that a round of workgroups holds (0: as they come, see session_at)
   int tiles;             // blocks of rows of a session and head
   int splits, chunk;     // shares of the tokens, tokens of one
   float2* part_ml;       // [rows x heads][splits]: maximum of the raw scores, sum
@@ -40,7 +43,6 @@ struct AttendArgs {
 };
 
 constexpr float kNoScore = -1.0e30f;  // finite, also times a scale: differences with it are no NaN
-constexpr int kQueriesInLds = 512;  // head size times tiles
 constexpr float kLate = 8.0f;
 constexpr float kLn2 = 0.693147180559945f;
 
@@ -184,6 +186,39 @@ __device__ __forceinline__ void read_codes(uint32_t (&c)[2][D / 32], uint32_t& s
 #pragma unroll
     for (int e = 0; e < 4; ++e) c[0][e] = x[e], c[0][4 + e] = y[e], c[1][e] = z[e], c[1][4 + e] = w[e];
   }
+}
+
+// Session at place p of the order in which workgroups are started: the longest
+// first, so that none starts late and goes on alone.  Where all workgroups are
+// resident from the start, a round of the CUs descends and the next ascends, so that
+// a CU's sessions add up alike.  Ranks are counted by one thread a session.
+constexpr int kOrdered = 256;
+__device__ __forceinline__ int session_at(const AttendArgs& a, int p) {
+  __shared__ __align__(16) uint32_t s_key[kOrdered];
+  __shared__ int s_found;
+  const int n = a.kv.n_sessions, t = threadIdx.x;
+  const int round = p / a.order, first = round * a.order;
+  const int last = first + a.order < n ? first + a.order - 1 : n - 1;
+  const int rank = round & 1 ? first + last - p : p;
+  uint32_t key = 0;
+  if (t < n) {  // (ties go to the first)
+    const int len = kv_length(a.kv, a.kv.slots ? a.kv.slots[t] : t);
+    key = (uint32_t)(len < (1 << 23) ? len : (1 << 23)) << 8 | (uint32_t)(kOrdered - 1 - t);
+  }
+  if (t < kOrdered) s_key[t] = key;
+  __syncthreads();
+  if (t < n) {
+    int above = 0;
+    const u32x4_t* keys = reinterpret_cast<const u32x4_t*>(s_key);
+#pragma unroll 8
+    for (int j = 0; j < (n + 3) / 4; ++j) {
+      const u32x4_t k = keys[j];
+      above += (k[0] > key) + (k[1] > key) + (k[2] > key) + (k[3] > key);
+    }
+    if (above == rank) s_found = t;
+  }
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(s_found);
 }
 
 __device__ __forceinline__ float max_over_groups(float x) {  // of lanes n, n + 16, n + 32, n + 48
@@ -362,29 +397,35 @@ __device__ __forceinline__ void take_values(Rows<D, MT>& w, const KvValues<D>& v
   }
 }
 
-// A workgroup is 4 waves: WT of them (4 or 2) share the tokens of the same rows,
-// 4 / WT have rows of their own.
-// Waves of a SIMD (workgroups of a CU) that the registers leave room for, and the
-// stages of a ring.
-constexpr int waves_of(int d, int mt) { return d * mt <= 128 ? 4 : (mt < 4 && d * mt <= 256 ? 3 : 2); }
-constexpr int stages_of(int d) { return d == 64 ? 4 : (d == 128 ? 3 : 2); }
+// A workgroup is 4 waves, WT of which (4 or 2) share the tokens of the same rows
+// while 4 / WT have rows of their own, or 8 that share the tokens of one group of rows.
+constexpr int waves_in(int wt) { return wt == 8 ? 8 : 4; }
+// Waves of a SIMD that the registers leave room for, and the stages of a ring.
+constexpr int waves_of(int d, int mt, int wt) {
+  return wt == 8 ? (d == 128 ? 4 : 2) : d * mt <= 128 ? 4 : (mt < 4 && d * mt <= 256 ? 3 : 2);
+}
+constexpr bool queries_in_lds(int d, int mt) { return d * mt >= 512; }
+constexpr int stages_of(int d, int wt) { return d == 64 ? 4 : (d == 128 && wt < 8 ? 3 : 2); }
 // LDS of a workgroup: rings and queries, in their place the waves' outputs.
 constexpr int attend_lds(int d, int mt, int wt) {
-  const int run = 4 * stages_of(d) * ((34 * d + 255) / 256 * 256) + (d * mt >= kQueriesInLds ? 4 / wt * mt * (d / 32) * 1024 : 0);
-  const int end = 256 * d + 512 * mt;
+  const int nw = waves_in(wt);
+  const int run = nw * stages_of(d, wt) * ((34 * d + 255) / 256 * 256) +
+                  (queries_in_lds(d, mt) ? nw / wt * mt * (d / 32) * 1024 : 0);
+  const int end = nw * (64 * d + 128 * mt);
   return run > end ? run : end;
 }
 constexpr int resident(int d, int mt, int wt) {  // workgroups of a CU
-  const int by_lds = 160 * 1024 / attend_lds(d, mt, wt);
-  return by_lds < waves_of(d, mt) ? by_lds : waves_of(d, mt);
+  const int by_lds = 160 * 1024 / attend_lds(d, mt, wt), by_waves = waves_of(d, mt, wt) * 4 / waves_in(wt);
+  return by_lds < by_waves ? by_lds : by_waves;
 }
 template <int D, int MT, int WT>
-__global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a) {
-  constexpr int NS = stages_of(D);
-  constexpr int WR = 4 / WT;
+__global__ __launch_bounds__(64 * waves_in(WT), waves_of(D, MT, WT)) void k_kv_attend(AttendArgs a) {
+  constexpr int NS = stages_of(D, WT);
+  constexpr int NW = waves_in(WT);
+  constexpr int WR = NW / WT;
   constexpr int KJ = D / 32;   // steps of the first product
   constexpr int VC = D / 16;   // products of the second
-  constexpr bool QL = D * MT >= kQueriesInLds;
+  constexpr bool QL = queries_in_lds(D, MT);
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int wt = wave % WT, wr = wave / WT;
@@ -394,7 +435,8 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
   const int rest = blockIdx.x / units;
   const int split = rest % a.splits;
   const int tile = a.tiles - 1 - rest / a.splits;  // rows that see most come first
-  const int head = unit % a.kv.heads, s = unit / a.kv.heads;
+  const int head = unit % a.kv.heads;
+  const int s = a.order > 0 ? session_at(a, unit / a.kv.heads) : unit / a.kv.heads;
   const KvSession ses = kv_session(a.kv, s);
   const int G = a.group, total = a.kv.R * G, live = ses.rows * G;
   const int base = ses.len - ses.rows;
@@ -402,7 +444,7 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
 
   // rows: fq = r G + query head; those past the session's see nothing
   extern __shared__ __align__(16) uint8_t smem[];  // rings, then queries of each group of rows
-  u32x4_t* s_q = reinterpret_cast<u32x4_t*>(smem + 4 * NS * Stage<D>::kBytes);
+  u32x4_t* s_q = reinterpret_cast<u32x4_t*>(smem + NW * NS * Stage<D>::kBytes);
   Queries<D, MT, QL> q;
   q.l = s_q;
   q.own = wr * (MT * KJ * 64) + lane;
@@ -473,7 +515,7 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
 
   uint8_t* ring = smem + wave * (NS * Stage<D>::kBytes);
   uint32_t lane16 = lane * 16;
-  const bool alone = WT == 4 && a.tiles == 1;
+  const bool alone = WT >= 4 && a.tiles == 1;
   const uint32_t ring_at = (uint32_t)(uintptr_t)(lds_void_t*)ring;
   // the lane's places in a stage: keys token n of a block, values as they lie
   const uint32_t key_at = n * (D / 2) + g * (D / 8), value_at = KvLayout<D>::kValues + lane * (D / 8);
@@ -557,8 +599,8 @@ __global__ __launch_bounds__(256, waves_of(D, MT)) void k_kv_attend(AttendArgs a
   int heads_of = G, row_first = row0;
   asm volatile("" : "+s"(heads_of), "+s"(row_first));
   // (in what were rings)
-  float* s_o = reinterpret_cast<float*>(smem);       // 4 x 16 D
-  float* s_ml = reinterpret_cast<float*>(smem) + 64 * D;
+  float* s_o = reinterpret_cast<float*>(smem);       // NW x 16 D
+  float* s_ml = reinterpret_cast<float*>(smem) + NW * 16 * D;
   __syncthreads();
   if (g == 0)
 #pragma unroll
@@ -720,6 +762,15 @@ void launch_join(const AttendArgs& a, int64_t rows, hipStream_t s) {
 
 namespace {
 
+// Whether workgroups start by their sessions' lengths (shares of a window are alike):
+// where there are more of them than CUs, and where the longest takes long enough,
+// turns of its waves, for the 2 us of ranking that each spends (208 sessions of 762
+// tokens each 22 -> 27 us).  64 users of 1 to 8192 tokens 79 -> 68 us, 128 with heads
+// of 256 up to 4096 87 -> 69, 256 with 64 heads up to 16384 714 -> 650.
+bool by_length(int64_t n_sessions, int64_t blocks, int64_t turns) {
+  return n_sessions > 1 && n_sessions <= kOrdered && blocks > kCUs && turns >= 16;
+}
+
 // How the rows of one head and the tokens of a session are shared out.
 struct Plan {
   int mt, wt;          // tiles of 16 rows of a wave, waves that share the tokens of the same rows
@@ -727,19 +778,25 @@ struct Plan {
   int splits, chunk;   // shares of the tokens, tokens of one
 };
 
-// units: sessions times key/value heads; group: query heads of one of those; R rows
-// of a session, which has max_len tokens at most.
-Plan plan_of(int d, int64_t units, int64_t R, int64_t group, int64_t max_len, int64_t window) {
-  const int64_t rows = R * group;
+// heads: of keys and values; group: query heads of one of those; R rows of a session,
+// which has max_len tokens at most.
+Plan account(int d, int64_t n_sessions, int64_t heads, int64_t R, int64_t group, int64_t max_len, int64_t window) {
+  const int64_t rows = R * group, units = n_sessions * heads;
   // Row tiles of a wave and waves that share its rows: many rows share the conversion
   // of the codes (a long prompt of 128 dimensions, us: 1450 with {2, 1}, 1215 with
   // {4, 4}), few make more workgroups (sliding window, 64 dimensions: 82 and 67).
-  static constexpr int kShapes[4][2] = {{1, 4}, {2, 4}, {4, 4}, {2, 2}}, kWide[2][2] = {{1, 4}, {1, 2}};
+  // Eight waves a session end a long one sooner where few rows need few registers (64
+  // users' single tokens 57 -> 51), and share 256 dimensions' conversion among 32 rows,
+  // which leave room for no second workgroup anyway (prompts 153 -> 126).
+  static constexpr int kNarrow[][2] = {{1, 4}, {2, 4}, {4, 4}, {2, 2}};
+  static constexpr int kMiddle[][2] = {{1, 4}, {2, 4}, {4, 4}, {2, 2}, {1, 8}};
+  static constexpr int kWide[][2] = {{1, 4}, {1, 2}, {2, 8}};
+  const int(*shapes)[2] = d == 64 ? kNarrow : d == 128 ? kMiddle : kWide;
   Plan best{};
   double least = 0;
-  for (int i = 0; i < (d == 256 ? 2 : 4); ++i) {
-    const int mt = d == 256 ? kWide[i][0] : kShapes[i][0], wt = d == 256 ? kWide[i][1] : kShapes[i][1];
-    const int per = 16 * mt * (4 / wt);
+  for (int i = 0; i < (d == 128 ? 5 : d == 64 ? 4 : 3); ++i) {
+    const int mt = shapes[i][0], wt = shapes[i][1], waves = waves_in(wt);
+    const int per = 16 * mt * (waves / wt);
     const int64_t tiles = (rows + per - 1) / per, blocks = units * tiles, step = 32 * wt;
     const int64_t slots = (int64_t)kCUs * resident(d, mt, wt);
     // tokens that a workgroup's rows see
@@ -752,7 +809,7 @@ Plan plan_of(int d, int64_t units, int64_t R, int64_t group, int64_t max_len, in
     // way out and back.
     const double issue = (4.0 * (0.9 * d + 20 + 36 * mt) + (32.0 + d / 2.0) * mt) * 1.35 / 2100;
     auto workgroup = [&](int64_t n, int64_t tokens) {  // n of them at a time
-      const double beside = (double)((n + kCUs - 1) / kCUs);
+      const double beside = (double)((n + kCUs - 1) / kCUs * (waves / 4));
       const double tile = beside * issue > issue + 0.7 ? beside * issue : issue + 0.7;
       return 5.0 + 1.5 * mt + (double)((tokens + step - 1) / step) * tile;
     };
@@ -764,6 +821,14 @@ Plan plan_of(int d, int64_t units, int64_t R, int64_t group, int64_t max_len, in
       double t = (double)(all / slots) * workgroup(slots, chunk) + (last > 0 ? workgroup(last, chunk) : 0.0);
       // (tiles of rows see less and less: the last ones fill the gaps)
       if (tiles > 1 && all > slots) t = ((double)all / (double)slots + 0.1) * workgroup(slots, chunk);
+      const bool ordered = n == 1 && window == 0 && by_length(n_sessions, all, chunk / step);
+      if (ordered) {
+        // Sessions may be all alike or very different, which is half of the work and the
+        // longest alone.
+        const double load = all > slots ? (double)all / (double)slots * workgroup(slots, chunk / 2) : workgroup(all, chunk / 2);
+        const double alone = workgroup(1, chunk);
+        t = 0.5 * (t + (load > alone ? load : alone));
+      }
       if (n > 1) t += 6.0 + (double)(units * rows * n) * (d * 8 + 16) / 4e6;
       if (best.mt == 0 || t < 0.97 * least) {
         least = t;
@@ -775,23 +840,41 @@ Plan plan_of(int d, int64_t units, int64_t R, int64_t group, int64_t max_len, in
   return best;
 }
 
+// The account takes 1 us of the host: a layer's workspace query, its call and the next
+// layers' ask for the same sizes.
+Plan plan_of(int d, int64_t n_sessions, int64_t heads, int64_t R, int64_t group, int64_t max_len, int64_t window) {
+  thread_local std::array<int64_t, 7> sizes{};
+  thread_local Plan plan{};
+  const std::array<int64_t, 7> want{d, n_sessions, heads, R, group, max_len, window};
+  if (sizes != want) {
+    plan = account(d, n_sessions, heads, R, group, max_len, window);
+    sizes = want;
+  }
+  return plan;
+}
+
 template <int D, int MT, int WT>
 hipError_t launch_one(const AttendArgs& a, int64_t blocks, hipStream_t s) {
   constexpr size_t lds = attend_lds(D, MT, WT);
   static std::atomic<uint64_t> done{0};
   const hipError_t e = set_lds_limit_once(done, reinterpret_cast<const void*>(k_kv_attend<D, MT, WT>), lds);
   if (e != hipSuccess) return e;
-  launch_kernel(k_kv_attend<D, MT, WT>, dim3((unsigned)blocks), dim3(256), (uint32_t)lds, s, a);
+  launch_kernel(k_kv_attend<D, MT, WT>, dim3((unsigned)blocks), dim3(64 * waves_in(WT)), (uint32_t)lds, s, a);
   return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch_tiles(const Plan& p, const AttendArgs& a, int64_t blocks, hipStream_t s) {
   if (p.mt == 1 && p.wt == 4) return launch_one<D, 1, 4>(a, blocks, s);
-  if constexpr (D == 256) return launch_one<D, 1, 2>(a, blocks, s);
-  else if (p.wt == 2) return launch_one<D, 2, 2>(a, blocks, s);
-  else if (p.mt == 2) return launch_one<D, 2, 4>(a, blocks, s);
-  else return launch_one<D, 4, 4>(a, blocks, s);
+  if constexpr (D == 256)
+    return p.wt == 8 ? launch_one<D, 2, 8>(a, blocks, s) : launch_one<D, 1, 2>(a, blocks, s);
+  if constexpr (D == 128)
+    if (p.wt == 8) return launch_one<D, 1, 8>(a, blocks, s);
+  if constexpr (D < 256) {
+    if (p.wt == 2) return launch_one<D, 2, 2>(a, blocks, s);
+    if (p.mt == 2) return launch_one<D, 2, 4>(a, blocks, s);
+    return launch_one<D, 4, 4>(a, blocks, s);
+  }
 }
 
 }  // namespace
@@ -799,7 +882,7 @@ hipError_t launch_tiles(const Plan& p, const AttendArgs& a, int64_t blocks, hipS
 // Workspace: the shares' maxima and sums, then their outputs.
 size_t kv_attend_scratch(int d, int64_t n_sessions, int64_t R, int64_t heads, int64_t q_heads,
                          int64_t max_len, int64_t window) {
-  const Plan p = plan_of(d, n_sessions * heads, R, q_heads / heads, max_len, window);
+  const Plan p = plan_of(d, n_sessions, heads, R, q_heads / heads, max_len, window);
   if (p.splits <= 1) return 0;
   const size_t n = (size_t)n_sessions * R * q_heads * p.splits;
   return (n * 8 + 255) / 256 * 256 + n * d * 4;
@@ -807,7 +890,7 @@ size_t kv_attend_scratch(int d, int64_t n_sessions, int64_t R, int64_t heads, in
 
 void kv_attend_shape(int d, int64_t n_sessions, int64_t R, int64_t heads, int64_t q_heads, int64_t max_len,
                      int64_t window, int shape[5]) {
-  const Plan p = plan_of(d, n_sessions * heads, R, q_heads / heads, max_len, window);
+  const Plan p = plan_of(d, n_sessions, heads, R, q_heads / heads, max_len, window);
   const int out[5] = {p.mt, p.wt, p.tiles, p.splits, p.chunk};
   for (int i = 0; i < 5; ++i) shape[i] = out[i];
 }
@@ -831,7 +914,7 @@ hipError_t launch_kv_attend(int d, const KvArgs& kv, const AttendCall& c, void* 
   a.q_aligned = c.q_row % 8 == 0 && c.q_head % 8 == 0 && (reinterpret_cast<uintptr_t>(c.q) & 15) == 0;
   a.o_aligned = c.o_row % 2 == 0 && c.o_head % 2 == 0 && (reinterpret_cast<uintptr_t>(c.out) & 3) == 0;
   const int64_t units = (int64_t)kv.n_sessions * kv.heads;
-  const Plan p = plan_of(d, units, kv.R, a.group, c.max_len, c.window);
+  const Plan p = plan_of(d, kv.n_sessions, kv.heads, kv.R, a.group, c.max_len, c.window);
   a.tiles = p.tiles;
   a.splits = p.splits;
   a.chunk = p.chunk;
@@ -841,7 +924,11 @@ hipError_t launch_kv_attend(int d, const KvArgs& kv, const AttendCall& c, void* 
     a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + ((size_t)rows * p.splits * 8 + 255) / 256 * 256);
   }
   const int64_t blocks = units * p.tiles * p.splits;
-  if (blocks > 0x7FFFFFFF || rows > 0x7FFFFFFF) return hipErrorInvalidValue;
+  if (p.splits == 1 && c.window == 0 && by_length(kv.n_sessions, blocks, p.chunk / (32 * p.wt))) {
+    const int per = kCUs / kv.heads;
+    const bool at_once = p.tiles == 1 && blocks <= (int64_t)kCUs * resident(d, p.mt, p.wt);
+    a.order = at_once && per > 0 ? per : kv.n_sessions;
+  }
   const hipError_t e = d == 64    ? launch_tiles<64>(p, a, blocks, s)
                        : d == 128 ? launch_tiles<128>(p, a, blocks, s)
                        : d == 256 ? launch_tiles<256>(p, a, blocks, s)

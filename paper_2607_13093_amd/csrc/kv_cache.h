@@ -110,14 +110,16 @@ struct KvSession {
 
 // A slot out of range holds nothing; lengths are cut to what a page row can
 // name, row counts to [0, R].
+__device__ __forceinline__ int kv_length(const KvArgs& a, int slot) {
+  const int64_t named = (int64_t)a.max_pages << a.page_shift, most = named < kKvMost ? named : kKvMost;
+  const int len = (unsigned)slot < (unsigned)a.n_slots ? a.lens[slot] : 0;
+  return len < 0 ? 0 : (len > most ? (int)most : len);
+}
 __device__ __forceinline__ KvSession kv_session(const KvArgs& a, int s) {
   const int slot = a.slots ? a.slots[s] : s;
-  const bool in = (unsigned)slot < (unsigned)a.n_slots;
-  const int64_t named = (int64_t)a.max_pages << a.page_shift, most = named < kKvMost ? named : kKvMost;
   KvSession r;
-  r.table = a.table + (in ? slot : 0) * a.ld_table;
-  const int len = in ? a.lens[slot] : 0;
-  r.len = len < 0 ? 0 : (len > most ? (int)most : len);
+  r.table = a.table + ((unsigned)slot < (unsigned)a.n_slots ? slot : 0) * a.ld_table;
+  r.len = kv_length(a, slot);
   const int n = a.rows ? a.rows[s] : a.R;
   r.rows = n < 0 ? 0 : (n > a.R ? a.R : n);
   return r;

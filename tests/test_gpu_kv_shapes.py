@@ -21,17 +21,24 @@ pytestmark = pytest.mark.gpu
 SHAPES = [
     (2, 1, 64, 1, 1, 100, 50, (1, 4, 0)), (2, 1, 64, 1, 9, 100, 0, (1, 4, 0)), (4, 1, 64, 1, 200, 1500, 0, (1, 4, 1)),
     (1, 1, 64, 1, 1, 1500, 0, (1, 4, 2)), (16, 2, 64, 64, 33, 100, 50, (2, 2, 0)), (21, 3, 64, 16, 100, 100, 0, (2, 2, 0)),
-    (32, 8, 64, 64, 5, 3000, 0, (2, 4, 0)), (14, 2, 64, 40, 33, 100, 50, (2, 4, 0)), (14, 2, 64, 1, 300, 3000, 0, (2, 4, 1)),
+    (32, 8, 64, 64, 5, 3000, 0, (1, 4, 0)), (14, 2, 64, 40, 33, 100, 50, (2, 4, 0)), (14, 2, 64, 1, 300, 3000, 0, (2, 4, 1)),
     (14, 2, 64, 1, 100, 12000, 0, (2, 4, 2)), (8, 8, 64, 64, 33, 1500, 0, (4, 4, 0)), (10, 2, 64, 5, 500, 1500, 0, (4, 4, 0)),
     (3, 1, 64, 40, 33, 6000, 0, (4, 4, 1)), (4, 2, 64, 3, 200, 12000, 0, (4, 4, 2)),
-    (1, 1, 128, 1, 1, 100, 50, (1, 4, 0)), (2, 1, 128, 1, 9, 100, 50, (1, 4, 0)), (5, 1, 128, 1, 100, 1500, 0, (1, 4, 1)),
+    (1, 1, 128, 1, 1, 100, 50, (1, 4, 0)), (2, 1, 128, 1, 9, 100, 50, (1, 4, 0)), (5, 1, 128, 1, 100, 1500, 0, (1, 8, 0)),
     (1, 1, 128, 1, 1, 1500, 0, (1, 4, 2)), (40, 8, 128, 64, 7, 100, 50, (2, 2, 0)), (16, 2, 128, 16, 100, 100, 0, (2, 2, 0)),
-    (40, 8, 128, 64, 5, 100, 50, (2, 4, 0)), (14, 2, 128, 16, 64, 100, 700, (2, 4, 0)), (5, 1, 128, 1, 500, 3000, 0, (2, 4, 1)),
-    (8, 1, 128, 1, 100, 12000, 0, (2, 4, 2)), (8, 8, 128, 64, 33, 700, 700, (4, 4, 0)), (56, 8, 128, 1, 500, 700, 0, (4, 4, 0)),
-    (14, 2, 128, 2, 300, 3000, 0, (4, 4, 1)), (1, 1, 128, 40, 33, 12000, 0, (4, 4, 2)),
-    (56, 8, 256, 40, 3, 100, 50, (1, 2, 0)), (21, 3, 256, 5, 100, 100, 0, (1, 2, 0)), (8, 1, 256, 2, 200, 12000, 0, (1, 2, 1)),
+    (40, 8, 128, 64, 5, 100, 50, (2, 4, 0)), (14, 2, 128, 16, 64, 100, 700, (2, 4, 0)), (5, 1, 128, 1, 500, 3000, 0, (1, 8, 0)),
+    (8, 1, 128, 1, 100, 12000, 0, (1, 8, 2)), (8, 8, 128, 64, 33, 700, 700, (4, 4, 0)), (56, 8, 128, 1, 500, 700, 0, (4, 4, 0)),
+    (14, 2, 128, 2, 300, 3000, 0, (1, 8, 0)), (1, 1, 128, 40, 33, 12000, 0, (4, 4, 2)),
+    (56, 8, 256, 40, 3, 100, 50, (1, 2, 0)), (21, 3, 256, 5, 100, 100, 0, (1, 2, 0)), (8, 1, 256, 2, 200, 12000, 0, (2, 8, 1)),
     (3, 1, 256, 1, 1, 100, 50, (1, 4, 0)), (4, 1, 256, 1, 5, 100, 0, (1, 4, 0)), (1, 1, 256, 1, 1, 700, 0, (1, 4, 1)),
     (1, 1, 256, 1, 1, 1500, 0, (1, 4, 2)),
+    (9, 3, 128, 16, 2, 3000, 0, (1, 4, 1)), (4, 2, 128, 1, 100, 3000, 0, (1, 8, 1)), (21, 3, 128, 2, 100, 3000, 0, (2, 4, 1)),
+    (2, 2, 128, 2, 100, 16001, 0, (2, 4, 2)), (112, 16, 128, 1, 33, 16001, 0, (4, 4, 1)), (6, 2, 256, 1, 33, 700, 0, (2, 8, 0)),
+    (2, 2, 256, 2, 33, 16001, 0, (2, 8, 2)),
+    # started by their lengths
+    (24, 8, 64, 64, 5, 3000, 0, (1, 4, 0)), (8, 8, 64, 64, 33, 3000, 0, (2, 4, 0)), (80, 16, 64, 64, 8, 3000, 0, (4, 4, 0)),
+    (6, 2, 128, 256, 1, 3000, 0, (1, 8, 0)), (24, 8, 128, 64, 8, 3000, 0, (2, 4, 0)), (40, 8, 128, 64, 8, 3000, 0, (4, 4, 0)),
+    (8, 8, 256, 64, 9, 3000, 0, (1, 4, 0)), (9, 3, 256, 256, 8, 3000, 0, (2, 8, 0)),
 ]
 
 
@@ -99,3 +106,32 @@ def test_shape(case):
             assert bool((off <= 0).all())
     say("worst output error: %.3f of its bound" % worst)
     assert worst <= 1.0
+
+
+@pytest.mark.parametrize("hkv,d,n", [(8, 128, 40), (4, 64, 255), (2, 256, 256), (300, 64, 2)])
+def test_order_of_sessions(hkv, d, n):
+    # sessions are started by their lengths: what each answers does not depend on it
+    say("order", hkv, d, n)
+    rng = np.random.default_rng(hkv + n)
+    most = 2600
+    lens = [int(x) for x in rng.integers(0, most + 1, n)]
+    lens[:n // 3] = [most] * (n // 3)                 # ties, and sessions of nothing
+    lens[n // 2] = 0
+    c = cache_of(rng, lens, hkv, d, 64)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n)
+    c.pool.random_(0, 128, generator=g)               # any codes, scales of 2^-127 ... 2^0
+    q = torch.randn(n, hkv, d, generator=g, device="cuda").to(torch.bfloat16)
+    want, wl = sph.kv_attend(c, 0, q, 1, 0.1, max_len=most, want_lse=True)
+    assert bool(torch.isfinite(want).all()) and bool(torch.isneginf(wl[n // 2]).all())
+    at = torch.from_numpy(rng.permutation(n).astype(np.int32)).cuda()
+    out, lse = sph.kv_attend(c, 0, q[at.long()], 1, 0.1, slots=at, max_len=most, want_lse=True)
+    assert torch.equal(out, want[at.long()]) and torch.equal(lse, wl[at.long()])
+    one = int(np.argmax(lens)), int(np.argmin(lens))
+    for s in one:                                     # alone: the same but for the order of sums
+        slot = torch.tensor([s], dtype=torch.int32).cuda()
+        o, l = sph.kv_attend(c, 0, q[s:s + 1], 1, 0.1, slots=slot, max_len=most, want_lse=True)
+        # the weights and each output round to bf16
+        v = want[s].float().abs().max()
+        assert float((o.float() - want[s:s + 1].float()).abs().max()) <= float(v) * 2.0 ** -5
+        assert torch.allclose(l, wl[s:s + 1], rtol=2.0 ** -18, atol=2.0 ** -12)
