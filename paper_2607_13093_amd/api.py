@@ -503,6 +503,9 @@ class KvCache:
             table.data_ptr(), table.stride(0), table.shape[1], lens.data_ptr(), refs.data_ptr(),
             table.shape[0], self.kv_heads, self.head_dim, self.page_tokens)
         self.ptr = ctypes.addressof(self._struct)
+        lib = _lib.load()
+        self._grow_bytes, self._compact_bytes = (lib.sph_pages_grow_workspace(self.ptr),
+                                                 lib.sph_pages_compact_workspace(self.ptr))
 
     @classmethod
     def empty(cls, layers: int, n_pages: int, n_slots: int, max_pages: int, kv_heads: int,
@@ -585,8 +588,8 @@ def kv_read(cache: KvCache, layer: int, rows_per_session: int, rows: Optional[to
         n = cache.n_slots if given is None else given.shape[0]
     if out is None:
         shape = (int(n) * R, cache.kv_heads, cache.head_dim)
-        out = (torch.empty(shape, dtype=torch.bfloat16, device=dev),
-               torch.empty(shape, dtype=torch.bfloat16, device=dev))
+        k = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+        out = k, torch.empty_like(k)
     k, v = out
     ks = _kv_rows("k", k, cache.kv_heads, cache.head_dim, dev)
     vs = _kv_rows("v", v, cache.kv_heads, cache.head_dim, dev)
@@ -650,7 +653,7 @@ def pages_grow(cache: KvCache, add: torch.Tensor, workspace: Optional[torch.Tens
     dev = cache.device
     status = torch.empty(2, dtype=torch.int32, device=dev) if out is None else out
     if workspace is None:
-        workspace = torch.empty(lib.sph_pages_grow_workspace(cache.ptr), dtype=torch.uint8, device=dev)
+        workspace = torch.empty(cache._grow_bytes, dtype=torch.uint8, device=dev)
     check(lib.sph_pages_grow(cache.ptr, _kv_ints("add", add, cache.n_slots, dev), _kv_ints("out", status, 2, dev),
                              workspace.data_ptr(), workspace.numel(), _stream_handle(dev)))
     return status
@@ -688,7 +691,7 @@ def pages_compact(cache: KvCache, out=None, workspace: Optional[torch.Tensor] = 
         raise ValueError(f"table: expected int32 {tuple(cache.table.shape)} on {dev}")
     live = torch.empty(1, dtype=torch.int32, device=dev)
     if workspace is None:
-        workspace = torch.empty(lib.sph_pages_compact_workspace(cache.ptr), dtype=torch.uint8, device=dev)
+        workspace = torch.empty(cache._compact_bytes, dtype=torch.uint8, device=dev)
     check(lib.sph_pages_compact(cache.ptr, table.data_ptr(), table.stride(0), _kv_ints("refs", refs, cache.n_pages, dev),
                                 live.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_handle(dev)))
     return table, refs, live
