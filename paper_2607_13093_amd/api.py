@@ -586,15 +586,16 @@ def kv_read(cache: KvCache, layer: int, rows_per_session: int, rows: Optional[to
     if n is None:
         given = rows if rows is not None else slots
         n = cache.n_slots if given is None else given.shape[0]
+    heads, d = cache.kv_heads, cache.head_dim
     if out is None:
-        shape = (int(n) * R, cache.kv_heads, cache.head_dim)
-        k = torch.empty(shape, dtype=torch.bfloat16, device=dev)
-        out = k, torch.empty_like(k)
-    k, v = out
-    ks = _kv_rows("k", k, cache.kv_heads, cache.head_dim, dev)
-    vs = _kv_rows("v", v, cache.kv_heads, cache.head_dim, dev)
-    if k.shape[0] != n * R or v.shape[0] != n * R:
-        raise ValueError(f"out: expected {n * R} rows, got {k.shape[0]} and {v.shape[0]}")
+        k = torch.empty((int(n) * R, heads, d), dtype=torch.bfloat16, device=dev)
+        v = torch.empty_like(k)
+        ks = vs = heads * d, d
+    else:
+        k, v = out
+        ks, vs = _kv_rows("k", k, heads, d, dev), _kv_rows("v", v, heads, d, dev)
+        if k.shape[0] != n * R or v.shape[0] != n * R:
+            raise ValueError(f"out: expected {n * R} rows, got {k.shape[0]} and {v.shape[0]}")
     check(_lib.load().sph_kv_read(cache.ptr, int(layer), k.data_ptr(), *ks, v.data_ptr(), *vs, int(n), R,
                                   _kv_ints("rows", rows, n, dev), _kv_ints("slots", slots, n, dev),
                                   _stream_handle(dev)))
@@ -621,16 +622,19 @@ def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, rows_per_session: int
     qs = _kv_rows("q", q, None, cache.head_dim, dev)
     M, heads = q.shape[0], q.shape[1]
     n = _kv_sessions(M, R)
+    d = cache.head_dim
     if out is None:
-        out = (torch.empty_like(q) if q.is_contiguous() else q.new_empty((M, heads, cache.head_dim)),
-               torch.empty((M, heads), dtype=torch.float32, device=dev) if want_lse else None)
-    o, lse = out
-    os = _kv_rows("out", o, heads, cache.head_dim, dev)
-    if o.shape[0] != M:
-        raise ValueError(f"out: expected {M} rows, got {o.shape[0]}")
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (M, heads) or not lse.is_contiguous()
-                            or lse.device != dev):
-        raise ValueError(f"lse: expected contiguous float32 ({M}, {heads}) on {dev}")
+        o = torch.empty_like(q) if q.is_contiguous() else q.new_empty((M, heads, d))
+        lse = torch.empty((M, heads), dtype=torch.float32, device=dev) if want_lse else None
+        os = heads * d, d
+    else:
+        o, lse = out
+        os = _kv_rows("out", o, heads, d, dev)
+        if o.shape[0] != M:
+            raise ValueError(f"out: expected {M} rows, got {o.shape[0]}")
+        if lse is not None and (lse.dtype != torch.float32 or lse.shape != (M, heads) or not lse.is_contiguous()
+                                or lse.device != dev):
+            raise ValueError(f"lse: expected contiguous float32 ({M}, {heads}) on {dev}")
     if workspace is None:
         need = kv_attend_workspace(cache, heads, n, R, window, max_len)
         if need > 0:
