@@ -448,7 +448,7 @@ int sph_kv_read(const sph_kv_cache* cache, int64_t layer, void* k, int64_t k_row
  *             q_head (o_row, o_head) elements apart
  * q_heads     a multiple of kv_heads
  * scale       0 < scale <= 1e6
- * window      0: none
+ * window      0, or no less than a slot can hold: none
  * max_len     the largest of the sessions' lens, as far as the caller knows (0:
  *             max_pages * page_tokens).  It shares out the work; results are
  *             right for any, up to the order of sums.

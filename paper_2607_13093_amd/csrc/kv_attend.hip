@@ -86,7 +86,7 @@ __device__ __forceinline__ KvPages tile_pages(const KvArgs& a, const KvSession& 
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     const int at = pos + b * kKvBlock;
-    const int i = at >> a.page_shift, last = a.max_pages - 1;
+    const uint32_t i = (uint32_t)at >> a.page_shift, last = a.max_pages - 1;
     // (read wherever it is, so that the load need not wait for the session's length;
     // the constant address space makes it a scalar one)
     const int page = ((const __attribute__((address_space(4))) int32_t*)ses.table)[i < last ? i : last];
@@ -424,6 +424,34 @@ constexpr int resident(int d, int mt, int wt) {  // workgroups of a CU
   const int by_lds = 160 * 1024 / attend_lds(d, mt, wt), by_waves = waves_of(d, mt, wt) * 4 / waves_in(wt);
   return by_lds < by_waves ? by_lds : by_waves;
 }
+// Tokens that rows r_lo ... r_hi of a session see (lo ... hi - 1, lo down to a whole
+// tile) and those that all of them see.  base: position of row 0, from -kKvMost on;
+// window below kKvMost (kv_window), so that nothing passes 32 bits.
+struct KvSpan {
+  int lo, hi, all_lo, all_hi;
+};
+__host__ __device__ __forceinline__ KvSpan kv_span(int base, int r_lo, int r_hi, int window) {
+  KvSpan t{0, base + r_hi + 1, 0, base + r_lo + 1};
+  if (window > 0) {
+    t.lo = base + r_lo - window + 1;
+    t.all_lo = base + r_hi - window + 1;
+  }
+  t.lo = t.lo > 0 ? t.lo & ~31 : 0;
+  t.hi = t.hi > 0 ? t.hi : 0;  // rows before the first token see none, and name no page
+  t.all_hi = t.all_hi > 0 ? t.all_hi : 0;
+  return t;
+}
+// The tokens of one share of them; the last takes what is left.
+struct KvShare {
+  int from, to;
+};
+__host__ __device__ __forceinline__ KvShare kv_share(const KvSpan& t, int split, int splits, int chunk) {
+  KvShare r;
+  r.from = t.lo + split * chunk;
+  r.to = split == splits - 1 ? t.hi : (r.from + chunk < t.hi ? r.from + chunk : t.hi);
+  return r;
+}
+
 template <int D, int MT, int WT>
 __global__ __launch_bounds__(64 * waves_in(WT), waves_of(D, MT, WT)) void k_kv_attend(AttendArgs a) {
   constexpr int NS = stages_of(D, WT);
@@ -479,21 +507,11 @@ __global__ __launch_bounds__(64 * waves_in(WT), waves_of(D, MT, WT)) void k_kv_a
   }
   // tokens that the wave's rows see, and those that all of them see
   const int last_row = (row0 + 16 * MT < live ? row0 + 16 * MT : live) - 1;
-  int lo = 0, hi = 0, all_lo = 0, all_hi = 0;
-  if (row0 < live) {
-    const int r_lo = row0 / G, r_hi = last_row / G;
-    hi = base + r_hi + 1;
-    all_hi = base + r_lo + 1;
-    if (a.window > 0) {
-      lo = base + r_lo - a.window + 1;
-      all_lo = base + r_hi - a.window + 1;
-    }
-    lo = lo > 0 ? lo & ~31 : 0;
-    hi = hi > 0 ? hi : 0;  // rows before the first token see none, and name no page
-  }
-  // the share of this workgroup; the last takes what is left
-  const int from = lo + split * a.chunk;
-  const int to = split == a.splits - 1 ? hi : (from + a.chunk < hi ? from + a.chunk : hi);
+  KvSpan seen{0, 0, 0, 0};
+  if (row0 < live) seen = kv_span(base, row0 / G, last_row / G, a.window);
+  const int all_lo = seen.all_lo, all_hi = seen.all_hi;
+  const KvShare share = kv_share(seen, split, a.splits, a.chunk);
+  const int from = share.from, to = share.to;
 
   Rows<D, MT> w;
 #pragma unroll
@@ -884,6 +902,15 @@ hipError_t launch_tiles(const Plan& p, const AttendArgs& a, int64_t blocks, hipS
 }
 
 }  // namespace
+
+int64_t kv_window(int64_t window, int64_t most) { return window < most ? window : 0; }
+
+void kv_attend_span(int base, int r_lo, int r_hi, int window, int split, int splits, int chunk, int span[6]) {
+  const KvSpan t = kv_span(base, r_lo, r_hi, window);
+  const KvShare share = kv_share(t, split, splits, chunk);
+  const int out[6] = {t.lo, t.hi, t.all_lo, t.all_hi, share.from, share.to};
+  for (int i = 0; i < 6; ++i) span[i] = out[i];
+}
 
 // Workspace: the shares' maxima and sums, then their outputs.
 size_t kv_attend_scratch(int d, int64_t n_sessions, int64_t R, int64_t heads, int64_t q_heads,

@@ -91,6 +91,12 @@ size_t kv_attend_scratch(int d, int64_t n_sessions, int64_t R, int64_t heads, in
 // workgroups for the rows of a head, shares of the tokens, tokens of a share.
 void kv_attend_shape(int d, int64_t n_sessions, int64_t R, int64_t heads, int64_t q_heads, int64_t max_len,
                      int64_t window, int shape[5]);
+// What such a call's window comes to where no session holds more than `most` tokens:
+// one that leaves none of them out is none (0).
+int64_t kv_window(int64_t window, int64_t most);
+// Tokens that a wave's rows see (some, all of them) and those of one share: lo, hi,
+// all_lo, all_hi, from, to.
+void kv_attend_span(int base, int r_lo, int r_hi, int window, int split, int splits, int chunk, int span[6]);
 hipError_t launch_kv_attend(int d, const KvArgs& kv, const AttendCall& c, void* workspace, hipStream_t s);
 
 size_t pages_grow_scratch(int64_t n_pages, int64_t n_slots);

@@ -970,10 +970,6 @@ int64_t kv_most(const sph_kv_cache* c, int64_t max_len) {
   return max_len > 0 && max_len < most ? max_len : most;
 }
 
-// The window that a call works with, the same in its query: beyond every length it
-// is none.
-int64_t kv_window(int64_t window) { return window > kMaxIds ? 0 : window; }
-
 int pages_ws(const char* fn, const void* workspace, size_t have, size_t need) {
   if (have < need || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))
     return fail(SPH_E_WORKSPACE, "%s: workspace %p of %zu bytes, need %zu (aligned)", fn, workspace, have, need);
@@ -1008,7 +1004,7 @@ size_t sph_kv_attend_workspace(const sph_kv_cache* cache, int64_t q_heads, int64
       q_heads % cache->kv_heads != 0 || n_sessions < 1 || R < 1 || window < 0 || max_len < 0 || cache->max_pages < 1)
     return 0;
   return sph::kv_attend_scratch(cache->head_dim, n_sessions, R, cache->kv_heads, q_heads,
-                                kv_most(cache, max_len), kv_window(window));
+                                kv_most(cache, max_len), sph::kv_window(window, kv_most(cache, 0)));
 }
 
 int sph_kv_attend(const sph_kv_cache* cache, int64_t layer, const void* q, int64_t q_row,
@@ -1036,7 +1032,7 @@ int sph_kv_attend(const sph_kv_cache* cache, int64_t layer, const void* q, int64
     return fail(SPH_E_UNSUPPORTED, "%s: %lld rows of %lld heads each", fn, (long long)R,
                 (long long)(q_heads / cache->kv_heads));
   if (!q || !out) return fail(SPH_E_INVALID_ARG, "%s: q or out is NULL", fn);
-  window = kv_window(window);
+  window = sph::kv_window(window, kv_most(cache, 0));
   max_len = kv_most(cache, max_len);
   const size_t need = sph::kv_attend_scratch((int)d, n_sessions, R, cache->kv_heads, q_heads, max_len, window);
   if (need > 0) {
