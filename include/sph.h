@@ -456,7 +456,8 @@ int sph_kv_read(const sph_kv_cache* cache, int64_t layer, void* k, int64_t k_row
  * workspace   >= sph_kv_attend_workspace bytes for the same arguments, 256-byte
  *             aligned (NULL if that is 0)
  * Sums, maxima and the softmax are held in fp32; the weights softmax(x) enter
- * the second product as bf16.
+ * the second product as bf16.  Scores are fp32 too: a row with an x[j] above
+ * about 2e38 answers NaN, an x[j] below -2e38 has no weight.
  */
 size_t sph_kv_attend_workspace(const sph_kv_cache* cache, int64_t q_heads, int64_t n_sessions,
                                int64_t R, int64_t window, int64_t max_len);

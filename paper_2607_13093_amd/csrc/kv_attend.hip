@@ -38,17 +38,19 @@ struct AttendArgs {
   float* lse;            // fp32 [M][q_heads] or null
   int group;             // query heads of a key/value head
   int window;            // 0: none
-  float scale, scale_log2;
-  float late;            // kLate binades of weight, as a difference of raw scores
+  float scale_log2;      // of a raw score, to binades of weight
+  float binade;          // one of them as a difference of scores (ln 2, but for scale_log2's rounding)
   bool q_aligned, o_aligned;
   int order;             // sessions that a round of workgroups holds (0: as they come, see session_at)
   int tiles;             // blocks of rows of a session and head
   int splits, chunk;     // shares of the tokens, tokens of one
-  float2* part_ml;       // [rows x heads][splits]: maximum of the raw scores, sum
+  float2* part_ml;       // [rows x heads][splits]: reference of the weights, their sum
   float* part_o;         // [rows x heads][splits][D]
 };
 
-constexpr float kNoScore = -1.0e30f;  // finite, also times a scale: differences with it are no NaN
+// Where references start, in binades: finite, so that differences with it are no NaN,
+// and below any score that fp32 holds.
+constexpr float kNoScore = -3.402823466e38f;
 constexpr float kLate = 8.0f;
 constexpr float kLn2 = 0.693147180559945f;
 
@@ -332,7 +334,8 @@ __device__ __forceinline__ void clear_values(KvValues<D>& v, const int (&held)[2
 // taken against a reference that is at most kLate binades below the row's largest
 // score so far, so that they stay below 2^kLate: lanes look at their own scores
 // and exchange them only when one goes past that, which is rare after the first
-// tiles.
+// tiles.  A score past fp32 makes the row NaN (infinity less itself), one below it
+// weighs nothing.
 template <int D, int MT>
 __device__ __forceinline__ void take_weights(bf16x8_t (&p)[MT], Rows<D, MT>& w, const f32x4_t (&sc)[MT][2],
                                              const AttendArgs& a) {
@@ -343,13 +346,13 @@ __device__ __forceinline__ void take_weights(bf16x8_t (&p)[MT], Rows<D, MT>& w, 
     most[m] = sc[m][0][0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) most[m] = fmaxf(most[m], sc[m][i >> 2][i & 3]);
-    late = late || most[m] > w.top[m] + a.late;
+    late = late || fmaf(most[m], a.scale_log2, -w.top[m]) > kLate;
   }
   if (__any(late)) {
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      const float t = fmaxf(w.top[m], max_over_groups(most[m]));
-      const float f = __builtin_amdgcn_exp2f((w.top[m] - t) * a.scale_log2);
+      const float t = fmaxf(w.top[m], max_over_groups(most[m]) * a.scale_log2);
+      const float f = __builtin_amdgcn_exp2f(w.top[m] - t) + (t - t);
       w.sum[m] *= f;
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) w.o[m][c] *= f;
@@ -358,11 +361,10 @@ __device__ __forceinline__ void take_weights(bf16x8_t (&p)[MT], Rows<D, MT>& w, 
   }
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    const float off = w.top[m] * a.scale_log2;
     float e8[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      e8[i] = __builtin_amdgcn_exp2f(fmaf(sc[m][i >> 2][i & 3], a.scale_log2, -off));
+      e8[i] = __builtin_amdgcn_exp2f(fmaf(sc[m][i >> 2][i & 3], a.scale_log2, -w.top[m]));
       w.sum[m] += e8[i];
     }
     const u32x4_t x{pack_bf16(e8[0], e8[1]), pack_bf16(e8[2], e8[3]), pack_bf16(e8[4], e8[5]), pack_bf16(e8[6], e8[7])};
@@ -642,9 +644,9 @@ __global__ __launch_bounds__(64 * waves_in(WT), waves_of(D, MT, WT)) void k_kv_a
 #pragma unroll
     for (int k = 0; k < WT; ++k) {
       const float* ml = &s_ml[(((wr * WT + k) * MT + m) * 16 + n) * 2];
-      l += ml[1] * __builtin_amdgcn_exp2f((ml[0] - t) * a.scale_log2);
+      l += ml[1] * __builtin_amdgcn_exp2f(ml[0] - t);
     }
-    const float f = __builtin_amdgcn_exp2f((w.top[m] - t) * a.scale_log2);
+    const float f = __builtin_amdgcn_exp2f(w.top[m] - t);
     if (m > 0) __syncthreads();
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -680,7 +682,7 @@ __global__ __launch_bounds__(64 * waves_in(WT), waves_of(D, MT, WT)) void k_kv_a
           }
         }
         if (a.lse && g == 0 && wt == 0)
-          a.lse[row * (a.kv.heads * G) + hq] = l == 0.0f ? -INFINITY : fmaf(t, a.scale, __builtin_amdgcn_logf(l) * kLn2);
+          a.lse[row * (a.kv.heads * G) + hq] = l == 0.0f ? -INFINITY : fmaf(t, a.binade, __builtin_amdgcn_logf(l) * kLn2);
       } else {
         const int64_t at = (row * (a.kv.heads * G) + hq) * a.splits + split;
         if (g == 0 && wt == 0) a.part_ml[at] = make_float2(t, l);
@@ -723,14 +725,14 @@ __global__ __launch_bounds__(256) void k_kv_join(AttendArgs a, int64_t rows) {
     float t = top;
 #pragma unroll
     for (int u = 0; u < 8; ++u) t = fmaxf(t, x[u].x);
-    const float f = __builtin_amdgcn_exp2f((top - t) * a.scale_log2);
+    const float f = __builtin_amdgcn_exp2f(top - t);
     l *= f;
     y *= f;
     top = t;
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       if (x[u].y == 0.0f) continue;
-      const float e = __builtin_amdgcn_exp2f((x[u].x - top) * a.scale_log2);
+      const float e = __builtin_amdgcn_exp2f(x[u].x - top);
       l += x[u].y * e;
       y += o[u] * e;
     }
@@ -751,7 +753,7 @@ __global__ __launch_bounds__(256) void k_kv_join(AttendArgs a, int64_t rows) {
     l = 0.0f;
 #pragma unroll
     for (int k = 0; k < TURNS; ++k) {
-      const float e = __builtin_amdgcn_exp2f((s_top[k] - t) * a.scale_log2);
+      const float e = __builtin_amdgcn_exp2f(s_top[k] - t);
       y += s_o[k * LPS + d4] * e;
       l += s_l[k] * e;
     }
@@ -772,7 +774,7 @@ __global__ __launch_bounds__(256) void k_kv_join(AttendArgs a, int64_t rows) {
     dst[2] = (uint16_t)hi, dst[3] = (uint16_t)(hi >> 16);
   }
   if (a.lse && d4 == 0)
-    a.lse[i] = l == 0.0f ? -INFINITY : fmaf(top, a.scale, __builtin_amdgcn_logf(l) * kLn2);
+    a.lse[i] = l == 0.0f ? -INFINITY : fmaf(top, a.binade, __builtin_amdgcn_logf(l) * kLn2);
 }
 
 template <int D>
@@ -941,9 +943,8 @@ hipError_t launch_kv_attend(int d, const KvArgs& kv, const AttendCall& c, void* 
   a.lse = c.lse;
   a.group = c.q_heads / kv.heads;
   a.window = c.window;
-  a.scale = c.scale;
   a.scale_log2 = c.scale * 1.44269504088896f;
-  a.late = kLate / a.scale_log2;
+  a.binade = (float)((double)c.scale / a.scale_log2);
   a.q_aligned = c.q_row % 8 == 0 && c.q_head % 8 == 0 && (reinterpret_cast<uintptr_t>(c.q) & 15) == 0;
   a.o_aligned = c.o_row % 2 == 0 && c.o_head % 2 == 0 && (reinterpret_cast<uintptr_t>(c.out) & 3) == 0;
   const int64_t units = (int64_t)kv.n_sessions * kv.heads;
