@@ -477,7 +477,8 @@ class KvCache:
     table int32 [slots, max_pages], -1 where there is no page
     lens  int32 [slots] tokens held, refs int32 [pages] slots that hold a page
 
-    The tensors are kept alive, and changed in place by the calls below."""
+    The tensors are kept alive, and changed in place by the calls below, which go by
+    the addresses and sizes of when the cache was made: its attributes are fixed."""
 
     def __init__(self, pool: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, refs: torch.Tensor,
                  kv_heads: int, head_dim: int, page_tokens: int):
@@ -506,6 +507,12 @@ class KvCache:
         lib = _lib.load()
         self._grow_bytes, self._compact_bytes = (lib.sph_pages_grow_workspace(self.ptr),
                                                  lib.sph_pages_compact_workspace(self.ptr))
+        self._fixed = frozenset(self.__dict__)
+
+    def __setattr__(self, name, value):
+        if name in self.__dict__.get("_fixed", ()):
+            raise AttributeError(f"KvCache.{name} is fixed: make another cache, or change the tensor in place")
+        super().__setattr__(name, value)
 
     @classmethod
     def empty(cls, layers: int, n_pages: int, n_slots: int, max_pages: int, kv_heads: int,

@@ -1,0 +1,32 @@
+"""What the torch binding of the cache takes and gives back."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_13093_amd as sph
+
+from kv_build import bf16, cache_of, filled, host
+from test_gpu_kv import say
+
+pytestmark = pytest.mark.gpu
+
+
+def test_a_cache_is_fixed():
+    # another tensor in an attribute's place would not be the one that calls work on
+    rng = np.random.default_rng(1)
+    c = cache_of(rng, [20, 5], 2, 64, 16)
+    for name in ("pool", "table", "lens", "refs"):
+        was = getattr(c, name)
+        with pytest.raises(AttributeError, match=name):
+            setattr(c, name, was.clone())
+        assert getattr(c, name) is was
+    for name in ("kv_heads", "head_dim", "page_tokens", "layers", "n_pages", "n_slots", "device", "ptr"):
+        with pytest.raises(AttributeError, match=name):
+            setattr(c, name, getattr(c, name))
+    c.note = 1                                     # what is not the cache's is free
+    c.note = 2
+    say("in place")
+    c.lens.copy_(torch.tensor([3, 4], dtype=torch.int32))
+    sph.pages_trim(c, torch.tensor([2, 9], dtype=torch.int32).cuda())
+    assert host(c.lens).tolist() == [2, 4]
