@@ -623,7 +623,9 @@ def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, rows_per_session: int
     (rows and heads may be strided), q_heads a multiple of kv_heads.  Returns
     (out bf16 [sessions * R, q_heads, head_dim], log-sum-exp fp32 [sessions * R,
     q_heads] or None).  max_len: the longest session, if the caller knows it (the
-    work is shared out better); window: positions a row sees (0: all before it)."""
+    work is shared out better); window: positions a row sees (0: all before it).
+    out: (out, log-sum-exp or None) to write to; want_lse makes the second where it
+    is None."""
     lib = _lib.load()
     R, dev = int(rows_per_session), cache.device
     qs = _kv_rows("q", q, None, cache.head_dim, dev)
@@ -631,8 +633,7 @@ def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, rows_per_session: int
     n = _kv_sessions(M, R)
     d = cache.head_dim
     if out is None:
-        o = torch.empty_like(q) if q.is_contiguous() else q.new_empty((M, heads, d))
-        lse = torch.empty((M, heads), dtype=torch.float32, device=dev) if want_lse else None
+        o, lse = torch.empty_like(q) if q.is_contiguous() else q.new_empty((M, heads, d)), None
         os = heads * d, d
     else:
         o, lse = out
@@ -642,6 +643,8 @@ def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, rows_per_session: int
         if lse is not None and (lse.dtype != torch.float32 or lse.shape != (M, heads) or not lse.is_contiguous()
                                 or lse.device != dev):
             raise ValueError(f"lse: expected contiguous float32 ({M}, {heads}) on {dev}")
+    if lse is None and want_lse:
+        lse = torch.empty((M, heads), dtype=torch.float32, device=dev)
     if workspace is None:
         need = kv_attend_workspace(cache, heads, n, R, window, max_len)
         if need > 0:

@@ -30,3 +30,18 @@ def test_a_cache_is_fixed():
     c.lens.copy_(torch.tensor([3, 4], dtype=torch.int32))
     sph.pages_trim(c, torch.tensor([2, 9], dtype=torch.int32).cuda())
     assert host(c.lens).tolist() == [2, 4]
+
+
+def test_log_sum_exp_beside_an_output_of_the_caller():
+    rng = np.random.default_rng(2)
+    c, _, _ = filled(rng, [40, 7], 2, 64, 16)
+    q, _ = bf16(rng, 2 * 3, 4, 64)
+    want, wl = sph.kv_attend(c, 0, q, 3, 0.1, want_lse=True)
+    o = torch.empty_like(q)
+    say("lse wanted, none given")
+    got, lse = sph.kv_attend(c, 0, q, 3, 0.1, want_lse=True, out=(o, None))
+    assert got is o and torch.equal(o, want) and torch.equal(lse, wl)
+    say("not wanted, none given; given")
+    assert sph.kv_attend(c, 0, q, 3, 0.1, out=(o, None))[1] is None
+    mine = torch.empty_like(wl)
+    assert sph.kv_attend(c, 0, q, 3, 0.1, out=(o, mine))[1] is mine and torch.equal(mine, wl)
