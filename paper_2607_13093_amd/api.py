@@ -559,6 +559,14 @@ def _kv_ints(name: str, t: Optional[torch.Tensor], n: int, device) -> Optional[i
     return t.data_ptr()
 
 
+def _kv_workspace(t: torch.Tensor, device):
+    """Address and bytes of a workspace of the caller's."""
+    if t.device != device or not t.is_contiguous():
+        raise ValueError(f"workspace: expected a contiguous tensor on {device}, got one "
+                         f"on {t.device} with strides {t.stride()}")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def _kv_sessions(M: int, R: int) -> int:
     if R < 1 or M % R != 0:
         raise ValueError(f"{M} rows are no whole number of sessions of {R}")
@@ -647,13 +655,14 @@ def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, rows_per_session: int
         lse = torch.empty((M, heads), dtype=torch.float32, device=dev)
     if workspace is None:
         need = kv_attend_workspace(cache, heads, n, R, window, max_len)
-        if need > 0:
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need > 0 else None
+        ws = _ptr(workspace), need
+    else:
+        ws = _kv_workspace(workspace, dev)
     check(lib.sph_kv_attend(cache.ptr, int(layer), q.data_ptr(), *qs, heads, n, R,
                             _kv_ints("rows", rows, n, dev), _kv_ints("slots", slots, n, dev),
                             float(scale), int(window), int(max_len), o.data_ptr(), *os, _ptr(lse),
-                            _ptr(workspace), 0 if workspace is None else workspace.numel(),
-                            _stream_handle(dev)))
+                            *ws, _stream_handle(dev)))
     return o, lse
 
 
@@ -668,8 +677,11 @@ def pages_grow(cache: KvCache, add: torch.Tensor, workspace: Optional[torch.Tens
     status = torch.empty(2, dtype=torch.int32, device=dev) if out is None else out
     if workspace is None:
         workspace = torch.empty(cache._grow_bytes, dtype=torch.uint8, device=dev)
+        ws = workspace.data_ptr(), cache._grow_bytes
+    else:
+        ws = _kv_workspace(workspace, dev)
     check(lib.sph_pages_grow(cache.ptr, _kv_ints("add", add, cache.n_slots, dev), _kv_ints("out", status, 2, dev),
-                             workspace.data_ptr(), workspace.numel(), _stream_handle(dev)))
+                             *ws, _stream_handle(dev)))
     return status
 
 
@@ -706,8 +718,11 @@ def pages_compact(cache: KvCache, out=None, workspace: Optional[torch.Tensor] = 
     live = torch.empty(1, dtype=torch.int32, device=dev)
     if workspace is None:
         workspace = torch.empty(cache._compact_bytes, dtype=torch.uint8, device=dev)
+        ws = workspace.data_ptr(), cache._compact_bytes
+    else:
+        ws = _kv_workspace(workspace, dev)
     check(lib.sph_pages_compact(cache.ptr, table.data_ptr(), table.stride(0), _kv_ints("refs", refs, cache.n_pages, dev),
-                                live.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_handle(dev)))
+                                live.data_ptr(), *ws, _stream_handle(dev)))
     return table, refs, live
 
 

@@ -45,3 +45,27 @@ def test_log_sum_exp_beside_an_output_of_the_caller():
     assert sph.kv_attend(c, 0, q, 3, 0.1, out=(o, None))[1] is None
     mine = torch.empty_like(wl)
     assert sph.kv_attend(c, 0, q, 3, 0.1, out=(o, mine))[1] is mine and torch.equal(mine, wl)
+
+
+def test_workspaces_off_the_cache_s_device_are_refused():
+    # a kernel would write to host memory
+    rng = np.random.default_rng(3)
+    c, _, _ = filled(rng, [3000], 1, 128, 16)
+    q, _ = bf16(rng, 1, 8, 128)
+    want, _ = sph.kv_attend(c, 0, q, 1, 0.1)
+    need = sph.kv_attend_workspace(c, 8, 1, 1)
+    add = torch.zeros(1, dtype=torch.int32, device="cuda")
+    assert need > 0
+    big = torch.empty(1 << 22, dtype=torch.uint8)
+    for bad, what in ((big, "on cpu"), (big.cuda()[::2], "contiguous")):
+        with pytest.raises(ValueError, match=what):
+            sph.kv_attend(c, 0, q, 1, 0.1, workspace=bad)
+        with pytest.raises(ValueError, match=what):
+            sph.pages_grow(c, add, workspace=bad)
+        with pytest.raises(ValueError, match=what):
+            sph.pages_compact(c, workspace=bad)
+    say("workspaces of other types, in bytes")
+    ws = torch.empty((need + 3) // 4, dtype=torch.float32, device="cuda")
+    assert torch.equal(sph.kv_attend(c, 0, q, 1, 0.1, workspace=ws)[0], want)
+    with pytest.raises(sph.SphError, match="workspace"):
+        sph.kv_attend(c, 0, q, 1, 0.1, workspace=ws[:-1])
