@@ -453,7 +453,7 @@ int sph_kv_read(const sph_kv_cache* cache, int64_t layer, void* k, int64_t k_row
  *             max_pages * page_tokens).  It shares out the work; results are
  *             right for any, up to the order of sums.
  * lse_out     fp32 [n_sessions * R][q_heads] or NULL
- * workspace   >= sph_kv_attend_workspace bytes for the same arguments, 256-byte
+ * workspace   >= sph_kv_attend_workspace bytes for the same arguments, 16-byte
  *             aligned (NULL if that is 0)
  * Sums, maxima and the softmax are held in fp32; the weights softmax(x) enter
  * the second product as bf16.  Scores are fp32 too: a row with an x[j] above
@@ -490,6 +490,7 @@ int sph_kv_attend(const sph_kv_cache* cache, int64_t layer, const void* q, int64
  * into the free ones below, both in ascending order.  table_out [n_slots]
  * [ld_out] (max_pages entries a row) and refs_out [n_pages] say where pages are
  * now; they may be the cache's own.  live_out (device int32 [1]) = L.
+ * workspace: device memory, 16-byte aligned, of the bytes that the call's query names.
  */
 size_t sph_pages_grow_workspace(const sph_kv_cache* cache);
 int sph_pages_grow(const sph_kv_cache* cache, const int32_t* add, int32_t* status_out,

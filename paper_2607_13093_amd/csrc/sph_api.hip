@@ -972,7 +972,7 @@ int64_t kv_most(const sph_kv_cache* c, int64_t max_len) {
 
 int pages_ws(const char* fn, const void* workspace, size_t have, size_t need) {
   if (have < need || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))
-    return fail(SPH_E_WORKSPACE, "%s: workspace %p of %zu bytes, need %zu (aligned)", fn, workspace, have, need);
+    return fail(SPH_E_WORKSPACE, "%s: workspace %p of %zu bytes, need %zu (16-byte aligned)", fn, workspace, have, need);
   return SPH_OK;
 }
 

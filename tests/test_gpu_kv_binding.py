@@ -69,3 +69,31 @@ def test_workspaces_off_the_cache_s_device_are_refused():
     assert torch.equal(sph.kv_attend(c, 0, q, 1, 0.1, workspace=ws)[0], want)
     with pytest.raises(sph.SphError, match="workspace"):
         sph.kv_attend(c, 0, q, 1, 0.1, workspace=ws[:-1])
+
+
+def test_workspaces_begin_at_any_16_bytes():
+    rng = np.random.default_rng(4)
+    c, _, _ = filled(rng, [3000, 40], 1, 128, 16)
+    q, _ = bf16(rng, 2, 8, 128)
+    want, wl = sph.kv_attend(c, 0, q, 1, 0.1, want_lse=True)
+    buf = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    assert buf.data_ptr() % 256 == 0 and sph.kv_attend_workspace(c, 8, 2, 1) > 0
+    table, refs, lens = c.table.clone(), c.refs.clone(), c.lens.clone()
+    add = torch.tensor([20, 1], dtype=torch.int32).cuda()
+    kept = torch.tensor([3000, 40], dtype=torch.int32).cuda()
+    for at in (16, 240):
+        say("workspace at", at)
+        got, lse = sph.kv_attend(c, 0, q, 1, 0.1, want_lse=True, workspace=buf[at:])
+        assert torch.equal(got, want) and torch.equal(lse, wl)
+        assert host(sph.pages_grow(c, add, workspace=buf[at:])).tolist() == [0, 0]
+        assert host(c.lens).tolist() == [3020, 41]
+        sph.pages_trim(c, kept)
+        assert torch.equal(c.table, table) and torch.equal(c.refs, refs) and torch.equal(c.lens, lens)
+        out = torch.empty_like(table), torch.empty_like(refs)
+        live = sph.pages_compact(c, out=out, workspace=buf[at:])[2]
+        assert int(live) == int((refs > 0).sum()) == int((out[1] > 0).sum())
+        c.table.copy_(out[0]), c.refs.copy_(out[1])
+        assert torch.equal(sph.kv_attend(c, 0, q, 1, 0.1)[0], want)
+        table, refs = c.table.clone(), c.refs.clone()
+    with pytest.raises(sph.SphError, match="16"):
+        sph.kv_attend(c, 0, q, 1, 0.1, workspace=buf[8:])
