@@ -475,8 +475,9 @@ int sph_kv_attend(const sph_kv_cache* cache, int64_t layer, const void* q, int64
  * sph_pages_grow: lens[s] += add[s] (device int32 [n_slots]; negative counts as
  * 0), with pages for the new tokens.  Where the first of them falls into a page
  * that others hold too (refs > 1), the slot gets a copy of its own, in every
- * layer.  status_out (device int32 [2]): pages lacking in the pool, and slots
- * whose row of max_pages is too short; if either is not 0, nothing has changed.
+ * layer.  status_out (device int32 [2]): pages lacking in the pool (of 2^31 - 1
+ * at most), and slots whose row of max_pages is too short; if either is not 0,
+ * nothing has changed.
  * sph_pages_trim: lens[s] = min(lens[s], max(kept[s], 0)); pages past that are
  * given back (free once no slot holds them).  kept 0 frees a slot.
  * sph_pages_fork: slot children[i] gives back what it holds and shares all of

@@ -88,18 +88,26 @@ struct GrowScratch {
   int32_t* head;       // pairs, sessions with too short a row
 };
 
+// Sums of pages stop at 2^31 - 1, more than any pool has free.
+__device__ __forceinline__ uint32_t add_pages(uint32_t a, uint32_t b) {
+  return a + b < 0x7FFFFFFFu ? a + b : 0x7FFFFFFFu;
+}
+
 // What the sessions need, with the state as it was before the call, by 1024
 // threads: first[s], the pages of the sessions before s, and the shared pages that
 // are to be copied, in pairs pair[s].
 __device__ __forceinline__ void grow_needs(const PagesArgs& a, const int32_t* add, const GrowScratch& w, int32_t* first) {
-  __shared__ int s_need[16], s_pair[16], s_short;
+  __shared__ uint32_t s_need[16];
+  __shared__ int s_pair[16], s_short;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (threadIdx.x == 0) s_short = 0;
-  int need0 = 0, pair0 = 0;
+  uint32_t need0 = 0;
+  int pair0 = 0;
   __syncthreads();
   for (int at = 0; at < a.n_slots; at += 1024) {
     const int s = at + threadIdx.x;
-    int need = 0, source = -1;
+    uint32_t need = 0;
+    int source = -1;
     if (s < a.n_slots) {
       const int64_t len = a.lens[s] > 0 ? a.lens[s] : 0, more = add[s] > 0 ? add[s] : 0;
       const int64_t page = int64_t(1) << a.page_shift;
@@ -107,7 +115,7 @@ __device__ __forceinline__ void grow_needs(const PagesArgs& a, const int32_t* ad
       if (want > a.max_pages || len + more > kKvMost) {
         atomicAdd(&s_short, 1);
       } else {
-        need = (int)(want - have);
+        need = (uint32_t)(want - have);
         if (more > 0 && (len & (page - 1))) {  // a page partly filled: is it another's too?
           const int p = a.table[(int64_t)s * a.ld_table + (len >> a.page_shift)];
           if ((unsigned)p < (unsigned)a.n_pages && a.refs[p] > 1) source = p;
@@ -115,33 +123,36 @@ __device__ __forceinline__ void grow_needs(const PagesArgs& a, const int32_t* ad
         need += source >= 0;
       }
     }
-    int x = need, y = source >= 0;
+    uint32_t x = need;
+    int y = source >= 0;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-      const int u = __shfl_up(x, o, 64), v = __shfl_up(y, o, 64);
-      if (lane >= o) x += u, y += v;
+      const uint32_t u = (uint32_t)__shfl_up((int)x, o, 64);
+      const int v = __shfl_up(y, o, 64);
+      if (lane >= o) x = add_pages(x, u), y += v;
     }
     if (lane == 63) s_need[wave] = x, s_pair[wave] = y;
     __syncthreads();
-    int before = need0, pairs = pair0, all = 0, all_pairs = 0;
+    uint32_t before = need0, all = 0;
+    int pairs = pair0, all_pairs = 0;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      if (i < wave) before += s_need[i], pairs += s_pair[i];
-      all += s_need[i];
+      if (i < wave) before = add_pages(before, s_need[i]), pairs += s_pair[i];
+      all = add_pages(all, s_need[i]);
       all_pairs += s_pair[i];
     }
     if (s < a.n_slots) {
-      first[s] = before + x - need;
+      first[s] = (int)(before + x - need);  // (of no use where a sum stopped: no page is given out then)
       const int k = pairs + y - 1;
       w.pair[s] = source >= 0 ? k : -1;
       if (source >= 0) w.src[k] = source;
     }
-    need0 += all;
+    need0 = add_pages(need0, all);
     pair0 += all_pairs;
     __syncthreads();
   }
   if (threadIdx.x == 0) {
-    first[a.n_slots] = need0;
+    first[a.n_slots] = (int)need0;
     w.head[0] = pair0;
     w.head[1] = s_short;
   }
