@@ -101,3 +101,35 @@ def test_scores_beyond_fp32(hint):
     c, q, _ = _one_dimension(rng, [-(2.0 ** 100)], [2.0 ** 26] * 40, hint=hint)
     out, lse = (host(x) for x in sph.kv_attend(c, 0, q, 1, 2.0 ** 19, max_len=hint, want_lse=True))
     assert not out.any() and np.isneginf(lse).all()
+
+
+# ---- lengths of any size -----------------------------------------------------
+
+@pytest.mark.parametrize("d,page,R,window", [(64, 16, 3, 0), (128, 64, 1, 0), (128, 16, 70, 0), (256, 32, 5, 40)])
+@pytest.mark.parametrize("length", [(1 << 31) - 1, 1 << 30, 0])
+def test_lengths_beyond_a_slot_s_row_are_cut_to_it(d, page, R, window, length):
+    # every page of the row is written, so that a wrong cut shows
+    say("length", length, d, page, R, window)
+    rng = np.random.default_rng(d + R)
+    pages = 9
+    n = pages * page
+    c, keys, values = filled(rng, [n, n], 2, d, page, extra=0)
+    assert c.table.shape[1] == pages
+    q, q64 = bf16(rng, 2 * R, 4, d, scale=2.0)
+    c.lens[0] = length or n + 1                    # one more than the row holds, too
+    _check(c, q, q64, keys, values, R, d ** -0.5, [n, n], window=window)
+    got = sph.kv_read(c, 0, R)
+    for x, want in zip(got, (keys, values)):
+        rows = np.zeros((2, R, 2, d))
+        for s in range(2):
+            rows[s] = want[s][n - R:]
+        np.testing.assert_array_equal(host(x).reshape(2, R, 2, d), rows)
+    # rows appended stand at the end of the row
+    k, k64 = bf16(rng, 2 * R, 2, d)
+    sph.kv_append(c, 0, k, k, R)
+    c.lens[0] = n
+    for x in sph.kv_read(c, 0, R):
+        np.testing.assert_array_equal(host(x), O.quantize(k64))
+    whole = sph.kv_read(c, 0, n)
+    for x, want in zip(whole, (keys, values)):
+        np.testing.assert_array_equal(host(x).reshape(2, n, 2, d)[:, :n - R], np.stack([w[:n - R] for w in want]))
