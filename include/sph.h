@@ -429,8 +429,8 @@ int sph_kv_append(const sph_kv_cache* cache, int64_t layer, const void* k, int64
                   int64_t n_sessions, int64_t R, const int32_t* rows, const int32_t* slots,
                   void* stream);
 
-/* The same rows back as bf16, the values that the codes stand for (exact);
- * zeros for the rows past rows[s]. */
+/* The same rows back as bf16, the values that the codes stand for: exact from
+ * 2^-126 on, smaller ones off by 2^-126 at most; zeros for the rows past rows[s]. */
 int sph_kv_read(const sph_kv_cache* cache, int64_t layer, void* k, int64_t k_row, int64_t k_head,
                 void* v, int64_t v_row, int64_t v_head, int64_t n_sessions, int64_t R,
                 const int32_t* rows, const int32_t* slots, void* stream);

@@ -24,7 +24,7 @@ def quantize(x):
     out = np.zeros_like(g)
     for at in np.argwhere(top > 0):
         at = tuple(at)
-        # candidates upwards: the first whose largest element rounds to at most 6
+        # the least e for which the largest element rounds to at most 6
         f, b = np.frexp(top[at])                   # top = f 2^b, f in [0.5, 1)
         e = b - 3                                  # 2^(b-1) <= top: e = floor(log2 top) - 2
         if f >= 0.875:                             # 7/8: two significant bits round up to 2^b

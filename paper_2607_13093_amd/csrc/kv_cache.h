@@ -167,8 +167,7 @@ __device__ __forceinline__ float e8m0_operand_at(uint32_t word, int byte) {
   return __uint_as_float(r);
 }
 
-// Two E2M1 codes of a byte as bf16, exact (but for scales near the ends of the
-// exponent range).
+// Two E2M1 codes of a byte as bf16: exact, values below 2^-126 to within 2^-126.
 template <int BYTE>
 __device__ __forceinline__ uint32_t fp4_pair(uint32_t codes, float scale) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, BYTE));

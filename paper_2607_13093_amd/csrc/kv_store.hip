@@ -131,8 +131,8 @@ __global__ __launch_bounds__(2 * D) void k_kv_append(KvArgs a, KvRows k, KvRows 
   }
 }
 
-// The same rows back as the values that they stand for; zeros where there is no
-// row, or no page.
+// The same rows back as the values that they stand for (those below 2^-126 to
+// within that); zeros where there is no row, or no page.
 template <int D>
 __global__ __launch_bounds__(2 * D) void k_kv_read(KvArgs a, KvRows k, KvRows v) {
   constexpr int LPT = D / 8;
