@@ -507,6 +507,37 @@ int sph_pages_compact(const sph_kv_cache* cache, int32_t* table_out, int64_t ld_
                       void* stream);
 
 /*
+ * Eviction: a long session is kept at a budget.  The attention that each held
+ * token receives is added up in weights (sph_kv_weigh), and now and then the
+ * tokens that received least are dropped.
+ *
+ * sph_pages_evict: slot s keeps min(lens[s], max(keep[s], must)) tokens, the
+ * must of them for certain: its first `first` ones, its last `recent` ones, and
+ * all up to the end of the last page of its row that another slot holds too
+ * (refs > 1), since dropping those would free nothing.  The others are kept by
+ * their weight, the largest first, equal ones by position, a NaN as the
+ * smallest.  The kept tokens keep their order and move together in every layer
+ * and head; lens[s] becomes their number and pages past that are given back.
+ * A slot of keep >= lens is left as it is.  What pages hold past the kept tokens
+ * is left too; a token whose page is not in the pool moves as zeros.
+ *
+ * weights      fp32 [n_slots][ld_weights], position by position
+ * keep         device int32 [n_slots]
+ * weights_out  fp32 [n_slots][ld_out]: the kept tokens' weights, then zeros up to
+ *              the former length; the rest is left.  It may be weights (and
+ *              ld_out ld_weights), else it does not overlap it.
+ * kept_out     int32 [n_slots][ld_kept] or NULL: former positions of the kept
+ *              tokens; the rest is left
+ * ld_*         at least the tokens that a slot's row names, max_pages *
+ *              page_tokens (2^30 at most)
+ */
+size_t sph_pages_evict_workspace(const sph_kv_cache* cache);
+int sph_pages_evict(const sph_kv_cache* cache, const float* weights, int64_t ld_weights,
+                    const int32_t* keep, int64_t first, int64_t recent, float* weights_out,
+                    int64_t ld_out, int32_t* kept_out, int64_t ld_kept, void* workspace,
+                    size_t ws_bytes, void* stream);
+
+/*
  * Kernel tracing.  While a trace is active, each call records one duration
  * per kernel it launches: start and stop HIP events are attached to the
  * kernel dispatches themselves (hipExtLaunchKernelGGL), so a duration is

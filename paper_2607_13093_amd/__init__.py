@@ -34,6 +34,7 @@ from .api import (  # noqa: F401
     kv_read,
     pages_compact,
     pages_copy,
+    pages_evict,
     pages_fork,
     pages_grow,
     pages_trim,

@@ -126,6 +126,11 @@ SIGNATURES = {
     "sph_pages_compact": (ctypes.c_int, [
         c_vp, c_vp, c_i64, c_vp, c_vp,      # cache, table_out, ld_out, refs_out, live_out
         c_vp, ctypes.c_size_t, c_vp]),      # workspace, ws_bytes, stream
+    "sph_pages_evict_workspace": (ctypes.c_size_t, [c_vp]),
+    "sph_pages_evict": (ctypes.c_int, [
+        c_vp, c_vp, c_i64, c_vp,            # cache, weights, ld_weights, keep
+        c_i64, c_i64, c_vp, c_i64,          # first, recent, weights_out, ld_out
+        c_vp, c_i64, c_vp, ctypes.c_size_t, c_vp]),  # kept_out, ld_kept, workspace, ws_bytes, stream
     "sph_trace_start": (ctypes.c_int, [ctypes.c_int]),
     "sph_trace_stop": (ctypes.c_int, [c_vp, ctypes.c_int, ctypes.POINTER(ctypes.c_int)]),
     # include/sph_probe.h

@@ -726,6 +726,44 @@ def pages_compact(cache: KvCache, out=None, workspace: Optional[torch.Tensor] = 
     return table, refs, live
 
 
+def _kv_per_token(name: str, t: torch.Tensor, cache: KvCache, dtype) -> int:
+    """Row stride of a [slots, >= max_pages * page_tokens] tensor."""
+    most = min(cache.table.shape[1] * cache.page_tokens, 1 << 30)
+    if t.dtype != dtype or t.dim() != 2 or t.shape[0] != cache.n_slots or t.shape[1] < most or t.stride(1) != 1 \
+            or t.device != cache.device:
+        raise ValueError(f"{name}: expected {dtype} [{cache.n_slots}, >= {most}] with contiguous rows on {cache.device}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def pages_evict(cache: KvCache, weights: torch.Tensor, keep: torch.Tensor, first: int = 0, recent: int = 0,
+                want_kept: bool = False, workspace: Optional[torch.Tensor] = None, out=None):
+    """Keep `keep` (int32 [slots]) tokens of each slot: its first and recent ones,
+    those up to its last page that other slots hold too, and of the others those with
+    the largest weights (fp32 [slots, >= max_pages * page_tokens], as kv_weigh adds
+    them up; equal ones by position).  They move together, in order, in every layer, and
+    pages past them are given back.  Returns (the kept tokens' weights, their former
+    positions int32 or None): `weights` itself, changed in place, and with want_kept a
+    new tensor with -1 past the length, or `out` = (weights, positions or None)."""
+    lib = _lib.load()
+    dev = cache.device
+    ld = _kv_per_token("weights", weights, cache, torch.float32)
+    w_out, kept = (weights, None) if out is None else out
+    ld_out = _kv_per_token("out", w_out, cache, torch.float32)
+    if kept is None and want_kept:
+        kept = torch.full(weights.shape, -1, dtype=torch.int32, device=dev)
+    ld_kept = 0 if kept is None else _kv_per_token("kept", kept, cache, torch.int32)
+    if workspace is None:
+        need = int(lib.sph_pages_evict_workspace(cache.ptr))
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        ws = workspace.data_ptr(), need
+    else:
+        ws = _kv_workspace(workspace, dev)
+    check(lib.sph_pages_evict(cache.ptr, weights.data_ptr(), ld, _kv_ints("keep", keep, cache.n_slots, dev), int(first),
+                              int(recent), w_out.data_ptr(), ld_out, _ptr(kept), ld_kept, *ws, _stream_handle(dev)))
+    return w_out, kept
+
+
 def debug_sync(enable: Optional[bool] = None) -> bool:
     """Switch the library's debug synchronisation (a stream synchronisation
     and error check after every kernel launch region) on or off; None only

@@ -81,6 +81,17 @@ struct AttendCall {
   float* lse;
 };
 
+struct EvictCall {
+  const float* weights;    // [n_slots][ld_weights]
+  int64_t ld_weights;
+  const int32_t* keep;     // [n_slots]
+  int first, recent;
+  float* weights_out;      // may be weights
+  int64_t ld_out;
+  int32_t* kept;           // [n_slots][ld_kept] or null
+  int64_t ld_kept;
+};
+
 // Launchers (return the HIP launch status); d: the head size, 64, 128 or 256.
 hipError_t launch_kv_rows(bool append, int d, const KvArgs& a, const void* k, int64_t k_row,
                           int64_t k_head, const void* v, int64_t v_row, int64_t v_head,
@@ -107,6 +118,10 @@ hipError_t launch_pages_fork(const PagesArgs& a, const int32_t* parents, const i
 hipError_t launch_pages_copy(const PagesArgs& a, const int32_t* src, const int32_t* dst, int64_t n, hipStream_t s);
 hipError_t launch_pages_compact(const PagesArgs& a, int32_t* table_out, int64_t ld_out, int32_t* refs_out,
                                 int32_t* live_out, void* workspace, hipStream_t s);
+// most: tokens that a row of the table names
+size_t pages_evict_scratch(int64_t n_slots, int64_t most);
+hipError_t launch_pages_evict(int d, int heads, int64_t most, const PagesArgs& p, const EvictCall& c, void* workspace,
+                              hipStream_t s);
 
 struct KvSession {
   const int32_t* table;  // its page row

@@ -1134,6 +1134,42 @@ int sph_pages_compact(const sph_kv_cache* cache, int32_t* table_out, int64_t ld_
   return ok();
 }
 
+size_t sph_pages_evict_workspace(const sph_kv_cache* cache) {
+  if (!cache || cache->n_slots < 1 || cache->n_slots > kMaxIds || cache->max_pages < 1 || cache->max_pages > kMaxIds ||
+      !kv_sizes_ok(cache->kv_heads, cache->head_dim, cache->page_tokens))
+    return 0;
+  return sph::pages_evict_scratch(cache->n_slots, kv_most(cache, 0));
+}
+
+int sph_pages_evict(const sph_kv_cache* cache, const float* weights, int64_t ld_weights,
+                    const int32_t* keep, int64_t first, int64_t recent, float* weights_out,
+                    int64_t ld_out, int32_t* kept_out, int64_t ld_kept, void* workspace,
+                    size_t ws_bytes, void* stream) {
+  const char* fn = "sph_pages_evict";
+  int e = kv_check(fn, cache, true);
+  if (e != SPH_OK) return e;
+  if (!weights || !keep || !weights_out) return fail(SPH_E_INVALID_ARG, "%s: weights, keep or weights_out is NULL", fn);
+  if (first < 0 || recent < 0)
+    return fail(SPH_E_INVALID_ARG, "%s: first=%lld recent=%lld", fn, (long long)first, (long long)recent);
+  const int64_t most = kv_most(cache, 0);
+  if (ld_weights < most || ld_out < most || (kept_out && ld_kept < most))
+    return fail(SPH_E_INVALID_ARG, "%s: ld_weights=%lld ld_out=%lld ld_kept=%lld below the %lld tokens of a slot's row", fn,
+                (long long)ld_weights, (long long)ld_out, (long long)ld_kept, (long long)most);
+  if (weights_out == weights && ld_out != ld_weights)
+    return fail(SPH_E_INVALID_ARG, "%s: in place with ld_weights=%lld and ld_out=%lld", fn, (long long)ld_weights,
+                (long long)ld_out);
+  e = pages_ws(fn, workspace, ws_bytes, sph_pages_evict_workspace(cache));
+  if (e != SPH_OK) return e;
+  const sph::EvictCall c{weights, ld_weights, keep, (int)std::min<int64_t>(first, sph::kKvMost),
+                         (int)std::min<int64_t>(recent, sph::kKvMost), weights_out, ld_out, kept_out, ld_kept};
+  hipStream_t s = (hipStream_t)stream;
+  const hipError_t he = traced("pages_evict", s, [&] {
+    return sph::launch_pages_evict(cache->head_dim, cache->kv_heads, most, pages_args(cache), c, workspace, s);
+  });
+  if (he != hipSuccess) return hip_fail(he, "eviction launch");
+  return ok();
+}
+
 int sph_trace_start(int capacity) {
   if (capacity < 1 || capacity > (1 << 22))
     return fail(SPH_E_INVALID_ARG, "sph_trace_start: capacity %d out of range", capacity);
