@@ -508,9 +508,38 @@ int sph_pages_compact(const sph_kv_cache* cache, int32_t* table_out, int64_t ld_
 
 /*
  * Eviction: a long session is kept at a budget.  The attention that each held
- * token receives is added up in weights (sph_kv_weigh), and now and then the
- * tokens that received least are dropped.
+ * token receives is added up in weights (sph_kv_weigh after a layer's attention),
+ * and now and then the tokens that received least are dropped (sph_pages_evict).
  *
+ * sph_kv_weigh: of one layer,
+ *   weights[slot][j] += sum_{row, h} exp(scale * sum_i q[row, h, i] K[j, h / G, i] - lse[row, h])
+ * over the session's rows that see position j (sph_kv_attend; the same sessions,
+ * rows, slots, scale and window), which is the sum of their softmax weights if lse
+ * is what the attention call answered.  A row whose lse is -infinity adds nothing.
+ * Tokens that no row sees keep their weight.
+ *
+ * lse          fp32 [n_sessions * R][q_heads]
+ * max_len      as in sph_kv_attend
+ * fresh        not 0: the weights of the rows' own tokens (the session's last rows[s])
+ *              start at zero: given with a step's first layer, it clears what rejected
+ *              drafts or a slot's former session left there.  A forked slot takes its
+ *              parent's row of weights, which the caller copies.
+ * weights      fp32 [n_slots][ld_weights], ld_weights at least the tokens that a slot's
+ *              row names, max_pages * page_tokens (2^30 at most).  A slot is at most
+ *              once in a call.
+ * workspace    >= sph_kv_weigh_workspace bytes for the same arguments, 16-byte aligned
+ *              (NULL if that is 0)
+ * Products and sums are fp32, in an order that does not depend on timing.
+ */
+size_t sph_kv_weigh_workspace(const sph_kv_cache* cache, int64_t q_heads, int64_t n_sessions,
+                              int64_t R, int64_t max_len);
+int sph_kv_weigh(const sph_kv_cache* cache, int64_t layer, const void* q, int64_t q_row,
+                 int64_t q_head, int64_t q_heads, const float* lse, int64_t n_sessions, int64_t R,
+                 const int32_t* rows, const int32_t* slots, float scale, int64_t window,
+                 int64_t max_len, int fresh, float* weights, int64_t ld_weights, void* workspace,
+                 size_t ws_bytes, void* stream);
+
+/*
  * sph_pages_evict: slot s keeps min(lens[s], max(keep[s], must)) tokens, the
  * must of them for certain: its first `first` ones, its last `recent` ones, and
  * all up to the end of the last page of its row that another slot holds too

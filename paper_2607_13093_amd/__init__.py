@@ -32,6 +32,8 @@ from .api import (  # noqa: F401
     kv_attend_workspace,
     kv_page_bytes,
     kv_read,
+    kv_weigh,
+    kv_weigh_workspace,
     pages_compact,
     pages_copy,
     pages_evict,

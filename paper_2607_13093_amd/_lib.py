@@ -126,6 +126,14 @@ SIGNATURES = {
     "sph_pages_compact": (ctypes.c_int, [
         c_vp, c_vp, c_i64, c_vp, c_vp,      # cache, table_out, ld_out, refs_out, live_out
         c_vp, ctypes.c_size_t, c_vp]),      # workspace, ws_bytes, stream
+    "sph_kv_weigh_workspace": (ctypes.c_size_t, [c_vp, c_i64, c_i64, c_i64, c_i64]),
+    "sph_kv_weigh": (ctypes.c_int, [
+        c_vp, c_i64,                        # cache, layer
+        c_vp, c_i64, c_i64, c_i64, c_vp,    # q, q_row, q_head, q_heads, lse
+        c_i64, c_i64, c_vp, c_vp,           # n_sessions, R, rows, slots
+        ctypes.c_float, c_i64, c_i64,       # scale, window, max_len
+        ctypes.c_int, c_vp, c_i64,          # fresh, weights, ld_weights
+        c_vp, ctypes.c_size_t, c_vp]),      # workspace, ws_bytes, stream
     "sph_pages_evict_workspace": (ctypes.c_size_t, [c_vp]),
     "sph_pages_evict": (ctypes.c_int, [
         c_vp, c_vp, c_i64, c_vp,            # cache, weights, ld_weights, keep

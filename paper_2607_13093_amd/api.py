@@ -736,6 +736,40 @@ def _kv_per_token(name: str, t: torch.Tensor, cache: KvCache, dtype) -> int:
     return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
 
 
+def kv_weigh_workspace(cache: KvCache, q_heads: int, n_sessions: int, rows_per_session: int, max_len: int = 0) -> int:
+    return int(_lib.load().sph_kv_weigh_workspace(cache.ptr, int(q_heads), int(n_sessions), int(rows_per_session),
+                                                  int(max_len)))
+
+
+def kv_weigh(cache: KvCache, layer: int, q: torch.Tensor, lse: torch.Tensor, rows_per_session: int, scale: float,
+             weights: torch.Tensor, rows: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None,
+             window: int = 0, max_len: int = 0, fresh: bool = False,
+             workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Add to weights fp32 [slots, >= max_pages * page_tokens] what each held token
+    receives of the attention of the sessions' rows: the softmax weights of q bf16
+    [sessions * R, q_heads, head_dim] over the cache, summed over rows and heads, with lse
+    fp32 [sessions * R, q_heads] as kv_attend answers it for the same arguments.  fresh: the
+    rows' own tokens start at zero (a step's first layer).  Returns weights."""
+    lib = _lib.load()
+    R, dev = int(rows_per_session), cache.device
+    qs = _kv_rows("q", q, None, cache.head_dim, dev)
+    M, heads = q.shape[0], q.shape[1]
+    n = _kv_sessions(M, R)
+    if lse.dtype != torch.float32 or lse.shape != (M, heads) or not lse.is_contiguous() or lse.device != dev:
+        raise ValueError(f"lse: expected contiguous float32 ({M}, {heads}) on {dev}")
+    ld = _kv_per_token("weights", weights, cache, torch.float32)
+    if workspace is None:
+        need = kv_weigh_workspace(cache, heads, n, R, max_len)
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need > 0 else None
+        ws = _ptr(workspace), need
+    else:
+        ws = _kv_workspace(workspace, dev)
+    check(lib.sph_kv_weigh(cache.ptr, int(layer), q.data_ptr(), *qs, heads, lse.data_ptr(), n, R,
+                           _kv_ints("rows", rows, n, dev), _kv_ints("slots", slots, n, dev), float(scale), int(window),
+                           int(max_len), int(bool(fresh)), weights.data_ptr(), ld, *ws, _stream_handle(dev)))
+    return weights
+
+
 def pages_evict(cache: KvCache, weights: torch.Tensor, keep: torch.Tensor, first: int = 0, recent: int = 0,
                 want_kept: bool = False, workspace: Optional[torch.Tensor] = None, out=None):
     """Keep `keep` (int32 [slots]) tokens of each slot: its first and recent ones,

@@ -81,6 +81,19 @@ struct AttendCall {
   float* lse;
 };
 
+struct WeighCall {
+  const void* q;
+  int64_t q_row, q_head;
+  int q_heads;
+  const float* lse;
+  float scale;
+  int window;
+  int64_t max_len;
+  int fresh;
+  float* weights;          // [n_slots][ld_weights]
+  int64_t ld_weights;
+};
+
 struct EvictCall {
   const float* weights;    // [n_slots][ld_weights]
   int64_t ld_weights;
@@ -109,6 +122,9 @@ int64_t kv_window(int64_t window, int64_t most);
 // all_lo, all_hi, from, to.
 void kv_attend_span(int base, int r_lo, int r_hi, int window, int split, int splits, int chunk, int span[6]);
 hipError_t launch_kv_attend(int d, const KvArgs& kv, const AttendCall& c, void* workspace, hipStream_t s);
+
+size_t kv_weigh_scratch(int d, int64_t n_sessions, int64_t R, int64_t heads, int64_t q_heads, int64_t max_len);
+hipError_t launch_kv_weigh(int d, const KvArgs& kv, const WeighCall& c, void* workspace, hipStream_t s);
 
 size_t pages_grow_scratch(int64_t n_pages, int64_t n_slots);
 size_t pages_compact_scratch(int64_t n_pages);

@@ -1134,6 +1134,55 @@ int sph_pages_compact(const sph_kv_cache* cache, int32_t* table_out, int64_t ld_
   return ok();
 }
 
+size_t sph_kv_weigh_workspace(const sph_kv_cache* cache, int64_t q_heads, int64_t n_sessions,
+                              int64_t R, int64_t max_len) {
+  if (!cache || !kv_sizes_ok(cache->kv_heads, cache->head_dim, cache->page_tokens) || q_heads < 1 ||
+      q_heads % cache->kv_heads != 0 || n_sessions < 1 || R < 1 || max_len < 0 || cache->max_pages < 1)
+    return 0;
+  return sph::kv_weigh_scratch(cache->head_dim, n_sessions, R, cache->kv_heads, q_heads, kv_most(cache, max_len));
+}
+
+int sph_kv_weigh(const sph_kv_cache* cache, int64_t layer, const void* q, int64_t q_row,
+                 int64_t q_head, int64_t q_heads, const float* lse, int64_t n_sessions, int64_t R,
+                 const int32_t* rows, const int32_t* slots, float scale, int64_t window,
+                 int64_t max_len, int fresh, float* weights, int64_t ld_weights, void* workspace,
+                 size_t ws_bytes, void* stream) {
+  const char* fn = "sph_kv_weigh";
+  sph::KvArgs a;
+  const int e = kv_call(fn, cache, layer, n_sessions, R, rows, slots, &a);
+  if (e != SPH_OK) return e;
+  const int64_t d = cache->head_dim, most = kv_most(cache, 0);
+  if (q_heads < 1 || q_heads > 65535 || q_heads % cache->kv_heads != 0)
+    return fail(SPH_E_INVALID_ARG, "%s: q_heads=%lld is no multiple of kv_heads=%d", fn, (long long)q_heads,
+                cache->kv_heads);
+  if (!(scale > 0.0f && scale <= 1e6f)) return fail(SPH_E_INVALID_ARG, "%s: scale=%g not in (0, 1e6]", fn, scale);
+  if (window < 0 || max_len < 0)
+    return fail(SPH_E_INVALID_ARG, "%s: window=%lld max_len=%lld", fn, (long long)window, (long long)max_len);
+  if (!kv_strides_ok(q_row, q_head, q_heads, d))
+    return fail(SPH_E_INVALID_ARG, "%s: row and head strides %lld, %lld for %lld heads of %lld", fn, (long long)q_row,
+                (long long)q_head, (long long)q_heads, (long long)d);
+  if (ld_weights < most)
+    return fail(SPH_E_INVALID_ARG, "%s: ld_weights=%lld below the %lld tokens of a slot's row", fn, (long long)ld_weights,
+                (long long)most);
+  if (n_sessions == 0 || R == 0) return ok();
+  if (R * (q_heads / cache->kv_heads) > sph::kKvMost)
+    return fail(SPH_E_UNSUPPORTED, "%s: %lld rows of %lld heads each", fn, (long long)R,
+                (long long)(q_heads / cache->kv_heads));
+  if (!q || !lse || !weights) return fail(SPH_E_INVALID_ARG, "%s: q, lse or weights is NULL", fn);
+  max_len = kv_most(cache, max_len);
+  const size_t need = sph::kv_weigh_scratch((int)d, n_sessions, R, cache->kv_heads, q_heads, max_len);
+  if (need > 0) {
+    const int we = pages_ws(fn, workspace, ws_bytes, need);
+    if (we != SPH_OK) return we;
+  }
+  const sph::WeighCall c{q, q_row, q_head, (int)q_heads, lse, scale, (int)sph::kv_window(window, most), max_len,
+                         fresh != 0, weights, ld_weights};
+  hipStream_t s = (hipStream_t)stream;
+  const hipError_t he = traced("kv_weigh", s, [&] { return sph::launch_kv_weigh((int)d, a, c, workspace, s); });
+  if (he != hipSuccess) return hip_fail(he, "token weights launch");
+  return ok();
+}
+
 size_t sph_pages_evict_workspace(const sph_kv_cache* cache) {
   if (!cache || cache->n_slots < 1 || cache->n_slots > kMaxIds || cache->max_pages < 1 || cache->max_pages > kMaxIds ||
       !kv_sizes_ok(cache->kv_heads, cache->head_dim, cache->page_tokens))

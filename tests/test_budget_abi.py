@@ -69,3 +69,44 @@ def test_evict_workspace(lib):
     # sizes past what there is are refused, not wrapped
     huge = _cache(n_slots=(1 << 31) - 1, max_pages=1 << 27, ld_table=1 << 27)
     assert _evict(lib, huge, ld=1 << 30, ld_out=1 << 30, kept=None, n=(1 << 63)) == W
+
+
+def _weigh(lib, c, layer=0, q=16, q_row=4096, q_head=128, q_heads=32, lse=16, n=3, R=5, rows=None, slots=None, scale=0.1,
+           window=0, max_len=0, fresh=0, w=16, ld=128, ws=4096, nb=BIG):
+    return lib.sph_kv_weigh(_ptr(c), layer, q, q_row, q_head, q_heads, lse, n, R, rows, slots, scale, window, max_len,
+                            fresh, w, ld, ws, nb, None)
+
+
+@pytest.mark.parametrize("kw,code,msg", BAD_CACHES)
+def test_weigh_cache_checks(lib, kw, code, msg):
+    c = _cache(**kw)
+    assert _weigh(lib, c) == code and msg in lib.sph_last_error(), lib.sph_last_error()
+    assert _weigh(lib, None) == E
+
+
+@pytest.mark.parametrize("kw,code,msg", [
+    (dict(layer=2), E, b"layer=2"), (dict(layer=-1), E, b"layer=-1"), (dict(n=-1), E, b"n_sessions=-1"),
+    (dict(n=5), E, b"beyond n_slots=4"), (dict(R=-1), E, b"R=-1"), (dict(q_heads=12), E, b"q_heads=12"),
+    (dict(q_heads=0), E, b"q_heads=0"), (dict(scale=0.0), E, b"scale"), (dict(scale=float("nan")), E, b"scale"),
+    (dict(scale=2e6), E, b"scale"), (dict(window=-1), E, b"window=-1"), (dict(max_len=-1), E, b"max_len=-1"),
+    (dict(q_row=127), E, b"strides"), (dict(q_head=64), E, b"strides"), (dict(ld=127), E, b"ld_weights=127"),
+    (dict(R=1 << 30, n=1), U, b"rows of 4 heads"), (dict(q=None), E, b"NULL"), (dict(lse=None), E, b"NULL"),
+    (dict(w=None), E, b"NULL"), (dict(ws=None), W, b"workspace"), (dict(ws=4104), W, b"workspace"),
+    (dict(nb=8), W, b"workspace"),
+])
+def test_weigh_checks(lib, kw, code, msg):
+    c = _cache()
+    assert _weigh(lib, c, **kw) == code and msg in lib.sph_last_error(), lib.sph_last_error()
+
+
+def test_weigh_workspace_and_empty_calls(lib):
+    c = _cache()
+    p = _ptr(c)
+    need = lib.sph_kv_weigh_workspace(p, 32, 3, 5, 0)
+    assert need > 0 and _weigh(lib, c, nb=need - 1) == W
+    for bad in ((None, 32, 3, 5, 0), (p, 12, 3, 5, 0), (p, 32, 0, 5, 0), (p, 32, 3, 0, 0), (p, 32, 3, 5, -1)):
+        assert lib.sph_kv_weigh_workspace(*bad) == 0
+    # many sessions fill the device by their tokens alone
+    assert lib.sph_kv_weigh_workspace(_ptr(_cache(n_slots=4096)), 32, 4096, 1, 0) == 0
+    for kw in (dict(n=0), dict(R=0)):
+        assert _weigh(lib, c, q=None, lse=None, w=None, ws=None, nb=0, **kw) == 0
