@@ -468,6 +468,38 @@ int sph_kv_attend(const sph_kv_cache* cache, int64_t layer, const void* q, int64
                   void* workspace, size_t ws_bytes, void* stream);
 
 /*
+ * The same for sessions that hold pages in common (branches of one prompt, readers of
+ * one document: sph_pages_fork): what their rows of the table name alike from the
+ * start on is read once for all of them, up to three levels of groups deep.  Outputs
+ * are those of sph_kv_attend, up to the order of sums.
+ *
+ * sph_kv_share makes the plan of a step, for the calls of all its layers: after
+ * sph_pages_grow, from the tables, lens, rows and slots as they are then.  It holds until
+ * those change (its memory is the caller's; a plan of other tables gives wrong
+ * outputs, but touches nothing outside the cache; one of other sizes gives NaN).
+ * sph_kv_attend_shared is given the same cache, q_heads, sessions, R, rows, slots,
+ * window and max_len; the rest is as in sph_kv_attend.
+ *
+ * n_sessions <= 4096, n_sessions * R * q_heads <= 2^26
+ * max_len      as in sph_kv_attend
+ * plan         device memory of sph_kv_share_bytes, 16-byte aligned
+ * workspace    >= sph_kv_attend_shared_workspace bytes, 16-byte aligned
+ */
+size_t sph_kv_share_bytes(const sph_kv_cache* cache, int64_t q_heads, int64_t n_sessions,
+                          int64_t R, int64_t max_len);
+int sph_kv_share(const sph_kv_cache* cache, int64_t q_heads, int64_t n_sessions, int64_t R,
+                 const int32_t* rows, const int32_t* slots, int64_t window, int64_t max_len,
+                 void* plan, size_t plan_bytes, void* stream);
+size_t sph_kv_attend_shared_workspace(const sph_kv_cache* cache, int64_t q_heads,
+                                      int64_t n_sessions, int64_t R, int64_t max_len);
+int sph_kv_attend_shared(const sph_kv_cache* cache, int64_t layer, const void* q, int64_t q_row,
+                         int64_t q_head, int64_t q_heads, int64_t n_sessions, int64_t R,
+                         const int32_t* rows, const int32_t* slots, float scale, int64_t window,
+                         int64_t max_len, const void* plan, size_t plan_bytes, void* out,
+                         int64_t o_row, int64_t o_head, float* lse_out, void* workspace,
+                         size_t ws_bytes, void* stream);
+
+/*
  * Pages.  These calls change table, lens and refs on the device, without the
  * host: a step can be captured in a graph.  Pages are given out lowest first,
  * to slots in their order, so results do not depend on timing.

@@ -126,6 +126,20 @@ SIGNATURES = {
     "sph_pages_compact": (ctypes.c_int, [
         c_vp, c_vp, c_i64, c_vp, c_vp,      # cache, table_out, ld_out, refs_out, live_out
         c_vp, ctypes.c_size_t, c_vp]),      # workspace, ws_bytes, stream
+    "sph_kv_share_bytes": (ctypes.c_size_t, [c_vp, c_i64, c_i64, c_i64, c_i64]),
+    "sph_kv_share": (ctypes.c_int, [
+        c_vp, c_i64, c_i64, c_i64,          # cache, q_heads, n_sessions, R
+        c_vp, c_vp, c_i64, c_i64,           # rows, slots, window, max_len
+        c_vp, ctypes.c_size_t, c_vp]),      # plan, plan_bytes, stream
+    "sph_kv_attend_shared_workspace": (ctypes.c_size_t, [c_vp, c_i64, c_i64, c_i64, c_i64]),
+    "sph_kv_attend_shared": (ctypes.c_int, [
+        c_vp, c_i64,                        # cache, layer
+        c_vp, c_i64, c_i64, c_i64,          # q, q_row, q_head, q_heads
+        c_i64, c_i64, c_vp, c_vp,           # n_sessions, R, rows, slots
+        ctypes.c_float, c_i64, c_i64,       # scale, window, max_len
+        c_vp, ctypes.c_size_t,              # plan, plan_bytes
+        c_vp, c_i64, c_i64, c_vp,           # out, o_row, o_head, lse_out
+        c_vp, ctypes.c_size_t, c_vp]),      # workspace, ws_bytes, stream
     "sph_kv_weigh_workspace": (ctypes.c_size_t, [c_vp, c_i64, c_i64, c_i64, c_i64]),
     "sph_kv_weigh": (ctypes.c_int, [
         c_vp, c_i64,                        # cache, layer

@@ -623,6 +623,25 @@ def kv_attend_workspace(cache: KvCache, q_heads: int, n_sessions: int, rows_per_
                                                    int(rows_per_session), int(window), int(max_len)))
 
 
+def _attend_out(q: torch.Tensor, out, want_lse: bool, d: int, device):
+    """(outputs, their strides, log-sum-exp or None) of an attention call."""
+    M, heads = q.shape[0], q.shape[1]
+    if out is None:
+        o, lse = torch.empty_like(q) if q.is_contiguous() else q.new_empty((M, heads, d)), None
+        os = heads * d, d
+    else:
+        o, lse = out
+        os = _kv_rows("out", o, heads, d, device)
+        if o.shape[0] != M:
+            raise ValueError(f"out: expected {M} rows, got {o.shape[0]}")
+        if lse is not None and (lse.dtype != torch.float32 or lse.shape != (M, heads) or not lse.is_contiguous()
+                                or lse.device != device):
+            raise ValueError(f"lse: expected contiguous float32 ({M}, {heads}) on {device}")
+    if lse is None and want_lse:
+        lse = torch.empty((M, heads), dtype=torch.float32, device=device)
+    return o, os, lse
+
+
 def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, rows_per_session: int, scale: float,
               rows: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None, window: int = 0,
               max_len: int = 0, want_lse: bool = False, workspace: Optional[torch.Tensor] = None, out=None):
@@ -640,19 +659,7 @@ def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, rows_per_session: int
     M, heads = q.shape[0], q.shape[1]
     n = _kv_sessions(M, R)
     d = cache.head_dim
-    if out is None:
-        o, lse = torch.empty_like(q) if q.is_contiguous() else q.new_empty((M, heads, d)), None
-        os = heads * d, d
-    else:
-        o, lse = out
-        os = _kv_rows("out", o, heads, d, dev)
-        if o.shape[0] != M:
-            raise ValueError(f"out: expected {M} rows, got {o.shape[0]}")
-        if lse is not None and (lse.dtype != torch.float32 or lse.shape != (M, heads) or not lse.is_contiguous()
-                                or lse.device != dev):
-            raise ValueError(f"lse: expected contiguous float32 ({M}, {heads}) on {dev}")
-    if lse is None and want_lse:
-        lse = torch.empty((M, heads), dtype=torch.float32, device=dev)
+    o, os, lse = _attend_out(q, out, want_lse, d, dev)
     if workspace is None:
         need = kv_attend_workspace(cache, heads, n, R, window, max_len)
         workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need > 0 else None
@@ -663,6 +670,70 @@ def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, rows_per_session: int
                             _kv_ints("rows", rows, n, dev), _kv_ints("slots", slots, n, dev),
                             float(scale), int(window), int(max_len), o.data_ptr(), *os, _ptr(lse),
                             *ws, _stream_handle(dev)))
+    return o, lse
+
+
+class KvSharePlan:
+    """What sessions hold in common, as kv_share found it: for kv_attend_shared on the
+    same cache, until its tables or lengths change."""
+
+    def __init__(self, cache: KvCache, q_heads: int, n_sessions: int, rows_per_session: int,
+                 rows: Optional[torch.Tensor], slots: Optional[torch.Tensor], window: int, max_len: int):
+        lib = _lib.load()
+        self.cache, self.rows, self.slots = cache, rows, slots
+        self.q_heads, self.n_sessions, self.rows_per_session = int(q_heads), int(n_sessions), int(rows_per_session)
+        self.window, self.max_len = int(window), int(max_len)
+        sizes = cache.ptr, self.q_heads, self.n_sessions, self.rows_per_session, self.max_len
+        self.bytes, self.workspace_bytes = int(lib.sph_kv_share_bytes(*sizes)), int(lib.sph_kv_attend_shared_workspace(*sizes))
+        self.buffer = torch.empty(max(self.bytes, 1), dtype=torch.uint8, device=cache.device)
+
+
+def kv_share(cache: KvCache, q_heads: int, rows_per_session: int, rows: Optional[torch.Tensor] = None,
+             slots: Optional[torch.Tensor] = None, n_sessions: Optional[int] = None, window: int = 0, max_len: int = 0,
+             out: Optional[KvSharePlan] = None) -> KvSharePlan:
+    """Find what the sessions' rows of the table name alike from the start on: the plan of
+    a step, made after pages_grow, for kv_attend_shared on each layer.  Sessions, rows,
+    slots, window and max_len as in kv_attend; n_sessions: all slots (or all of `rows` or
+    `slots`) if None.  out: a plan of the same arguments to be made anew in its memory."""
+    n = n_sessions
+    if n is None:
+        given = rows if rows is not None else slots
+        n = cache.n_slots if given is None else given.shape[0]
+    R, dev = int(rows_per_session), cache.device
+    r, s = _kv_ints("rows", rows, n, dev), _kv_ints("slots", slots, n, dev)
+    if out is None:
+        out = KvSharePlan(cache, q_heads, n, R, rows, slots, window, max_len)
+    elif (out.cache, out.q_heads, out.n_sessions, out.rows_per_session, out.window, out.max_len) != \
+            (cache, int(q_heads), int(n), R, int(window), int(max_len)):
+        raise ValueError("out: a plan of other arguments")
+    check(_lib.load().sph_kv_share(cache.ptr, out.q_heads, out.n_sessions, R, r, s, out.window, out.max_len,
+                                   out.buffer.data_ptr(), out.bytes, _stream_handle(dev)))
+    out.rows, out.slots = rows, slots
+    return out
+
+
+def kv_attend_shared(cache: KvCache, layer: int, q: torch.Tensor, plan: KvSharePlan, scale: float,
+                     want_lse: bool = False, workspace: Optional[torch.Tensor] = None, out=None):
+    """kv_attend of the plan's sessions, rows and window, pages that sessions hold in
+    common read once for all of them.  Returns what kv_attend does, equal up to the order
+    of sums.  workspace: plan.workspace_bytes, 16-byte aligned."""
+    lib = _lib.load()
+    dev = cache.device
+    if plan.cache is not cache:
+        raise ValueError("plan: made for another cache")
+    qs = _kv_rows("q", q, plan.q_heads, cache.head_dim, dev)
+    n, R = plan.n_sessions, plan.rows_per_session
+    if q.shape[0] != n * R:
+        raise ValueError(f"q: expected {n * R} rows, got {q.shape[0]}")
+    o, os, lse = _attend_out(q, out, want_lse, cache.head_dim, dev)
+    if workspace is None:
+        workspace = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device=dev)
+        ws = workspace.data_ptr(), plan.workspace_bytes
+    else:
+        ws = _kv_workspace(workspace, dev)
+    check(lib.sph_kv_attend_shared(cache.ptr, int(layer), q.data_ptr(), *qs, plan.q_heads, n, R, _ptr(plan.rows),
+                                   _ptr(plan.slots), float(scale), plan.window, plan.max_len, plan.buffer.data_ptr(),
+                                   plan.bytes, o.data_ptr(), *os, _ptr(lse), *ws, _stream_handle(dev)))
     return o, lse
 
 

@@ -1,0 +1,833 @@
+// Attention of sessions that hold pages in common: what sessions' rows of the table
+// name alike from the start on is read once for all of them.
+//
+// A plan, made on the device from the tables, cuts the sessions' tokens into
+// segments: ranges that a set of sessions holds on the same pages, and what each session
+// holds alone.  Sessions are sorted by their rows of the table, a level at a time: those
+// of a group whose next page is the same form a group of the next level, and share
+// what they all name alike from there on.  So every row is the rows' end of a path of
+// segments, some levels long, and its softmax the join of its segments' parts:
+//   l_k = sum_j exp2(x_j - t_k),  o_k = sum_j exp2(x_j - t_k) V_j   over segment k
+//   out = sum_k exp2(t_k - t) o_k / sum_k exp2(t_k - t) l_k,  t = max_k t_k
+// Long segments are cut into shares of their tokens, which are parts too.
+//
+// The parts are computed as in kv_attend.hip, by workgroups that go over a list of
+// items, a share of a segment for a tile of the rows of all its sessions each: many
+// rows on a shared segment, so that its codes are converted once for 64 rows, few on
+// a session's own.
+#include "kv_tile.h"
+
+namespace sph {
+
+constexpr int kShareLevels = 3;
+constexpr int kShareStep = 128;   // tokens that shares are multiples of
+constexpr int kShareLeast = 256;  // and at least
+// Tokens whose reading a segment has to save: a part of every row costs about as much.
+constexpr int kShareWorth = 256;
+
+// An item: the rows of `members` sessions from place `first` of the order, tile
+// `tile` of them, over tokens from ... to - 1 of their pages.
+struct ShareItem {
+  int32_t first, members, tile, from, to, part, alone, pad;
+};
+
+struct ShareHead {
+  uint32_t key;      // of the sizes that the plan is for
+  int32_t items[2];  // on shared segments, on sessions' own
+  int32_t pad[5];
+};
+
+// Sizes of a plan, from a call's.
+struct ShareSizes {
+  int levels, parts;  // segments of a path that are shared at most, parts of a row
+  int extra;          // parts beyond one for each segment of a path
+  int rows[2];        // of a tile
+  int slots[2];       // workgroups that run at a time
+  int64_t cap[2];     // items at most
+  int mt[2], wt[2];
+};
+
+struct SharePlanArgs {
+  KvArgs kv;
+  ShareSizes z;
+  int group, window;
+  uint32_t key;
+  ShareHead* head;
+  int32_t* order;    // [S]: sessions, those of a segment side by side
+  int32_t* parts;    // [S]: parts of a session's rows
+  ShareItem* segs;   // [(levels + 1) S]: scratch; tile holds the segment's tiles, part its first
+  ShareItem* items[2];
+};
+
+constexpr int kPlanThreads = 1024;
+
+// Sum of x over the threads before this one; all: over all.  For 1024 threads.
+__device__ __forceinline__ int sum_before(int x, int* all) {
+  __shared__ int s_wave[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int y = x;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int z = __shfl_up(y, o, 64);
+    if (lane >= o) y += z;
+  }
+  __syncthreads();  // (a call before this one is read)
+  if (lane == 63) s_wave[wave] = y;
+  __syncthreads();
+  int before = 0, total = 0;
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const int n = s_wave[k];
+    if (k < wave) before += n;
+    total += n;
+  }
+  *all = total;
+  return before + y - x;
+}
+
+// Keys in ascending order, n a power of two.
+__device__ __forceinline__ void sort_keys(uint64_t* key, int n) {
+  for (int size = 2; size <= n; size <<= 1)
+    for (int gap = size >> 1; gap > 0; gap >>= 1) {
+      __syncthreads();
+      for (int i = threadIdx.x; i < n / 2; i += kPlanThreads) {
+        const int lo = i / gap * (2 * gap) + i % gap, hi = lo + gap;
+        const uint64_t a = key[lo], b = key[hi];
+        if ((a > b) == ((lo & size) == 0)) {
+          key[lo] = b;
+          key[hi] = a;
+        }
+      }
+    }
+  __syncthreads();
+}
+
+__global__ __launch_bounds__(kPlanThreads) void k_share_plan(SharePlanArgs a, int n2) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  uint64_t* key = reinterpret_cast<uint64_t*>(smem);           // [n2] by place: group, page, session
+  int32_t* limit = reinterpret_cast<int32_t*>(key + n2);       // [n2] by session: pages that may be shared
+  int32_t* depth = limit + n2;                                 // by place: pages shared so far
+  int32_t* group = depth + n2;                                 // by place
+  int32_t* first = group + n2;                                 // [n2 + 1] by group: its first place
+  int32_t* alike = first + n2 + 1;                             // by group: pages named alike
+  int32_t* low = alike + n2;                                   // by group: least position of a first row
+  int32_t* count = low + n2;                                   // by place: parts so far
+  __shared__ int s_segs, s_chunk[16];
+  const int S = a.kv.n_sessions, shift = a.kv.page_shift, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  auto table_of = [&](int s) { return kv_session(a.kv, s).table; };
+
+  for (int s = threadIdx.x; s < n2; s += kPlanThreads) {
+    int n = 0;
+    if (s < S) {
+      const KvSession ses = kv_session(a.kv, s);
+      n = ses.len > ses.rows ? ses.len - ses.rows : 0;  // all its rows see those
+    }
+    limit[s] = n >> shift;
+    depth[s] = group[s] = count[s] = 0;
+    key[s] = s < S ? (uint64_t)s : ~uint64_t(0);
+  }
+  if (threadIdx.x == 0) s_segs = 0;
+  __syncthreads();
+
+  int groups = 1, ends[kShareLevels + 1];  // segments up to each level
+  ends[0] = 0;
+  for (int level = 0; level < a.z.levels; ++level) {
+    for (int at = threadIdx.x; at < S; at += kPlanThreads) {
+      const int s = (int)(key[at] & 4095), d = depth[at];
+      const int page = d < limit[s] ? table_of(s)[d] : -1;
+      const bool valid = (unsigned)page < (unsigned)a.kv.n_pages;
+      key[at] = (uint64_t)group[at] << 44 | (valid ? (uint64_t)page << 12 : uint64_t(1) << 43 | (uint64_t)s << 12) | (uint64_t)s;
+    }
+    sort_keys(key, n2);
+    // groups of the level: places whose keys are alike but for the session
+    const int each = (n2 + kPlanThreads - 1) / kPlanThreads, mine = threadIdx.x * each;
+    int starts = 0;
+    for (int i = mine; i < mine + each && i < S; ++i) starts += i == 0 || key[i] >> 12 != key[i - 1] >> 12;
+    int id = sum_before(starts, &groups);
+    for (int i = mine; i < mine + each && i < S; ++i) {
+      if (i == 0 || key[i] >> 12 != key[i - 1] >> 12) first[id++] = i;
+      group[i] = id - 1;
+    }
+    if (threadIdx.x == 0) first[groups] = S;
+    for (int g = threadIdx.x; g < groups; g += kPlanThreads) {
+      alike[g] = kKvMost;
+      low[g] = kKvMost;
+    }
+    __syncthreads();
+    for (int at = threadIdx.x; at < S; at += kPlanThreads) {
+      const int s = (int)(key[at] & 4095);
+      atomicMin(&alike[group[at]], limit[s]);
+      if (a.window > 0) {
+        const KvSession ses = kv_session(a.kv, s);
+        atomicMin(&low[group[at]], ses.len - ses.rows);
+      }
+    }
+    __syncthreads();
+    // pages named alike by a group's first session and each of the others
+    for (int at = wave; at < S; at += 16) {
+      const int g = group[at], lead = first[g];
+      if (at == lead) continue;
+      const int32_t *x = table_of((int)(key[lead] & 4095)), *y = table_of((int)(key[at] & 4095));
+      for (int c = depth[at] + 1; c < *(volatile int32_t*)&alike[g]; c += 256) {
+        int32_t p[4], q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int at_c = c + i * 64 + lane < a.kv.max_pages ? c + i * 64 + lane : a.kv.max_pages - 1;
+          p[i] = x[at_c];
+          q[i] = y[at_c];
+        }
+        int differs = kKvMost;
+#pragma unroll
+        for (int i = 3; i >= 0; --i)
+          if (p[i] != q[i]) differs = c + i * 64 + lane;
+        const bool any = __any(differs != kKvMost);
+        if (differs != kKvMost) atomicMin(&alike[g], differs);
+        if (any) break;
+      }
+    }
+    __syncthreads();
+    // segments of the level, in the order of their groups
+    const int before = s_segs;
+    int made = 0;
+    for (int g0 = 0; g0 < groups; g0 += kPlanThreads) {
+      const int g = g0 + threadIdx.x;
+      bool take = false;
+      int from = 0, to = 0, members = 0;
+      if (g < groups) {
+        members = first[g + 1] - first[g];
+        from = depth[first[g]] << shift;
+        to = alike[g] << shift;
+        take = members > 1 && (int64_t)(to - from) * (members - 1) >= kShareWorth;
+      }
+      int all = 0;
+      const int at = sum_before(take ? 1 : 0, &all);
+      if (take) {
+        int seen = from;
+        if (a.window > 0) {
+          const int64_t lowest = (int64_t)low[g] - a.window + 1;
+          if (lowest > seen) seen = lowest < to ? (int)lowest & ~(kKvBlock - 1) : to;
+        }
+        ShareItem& t = a.segs[before + made + at];
+        t.first = first[g];
+        t.members = members;
+        t.from = seen;
+        t.to = to;
+      }
+      if (g < groups) low[g] = take;
+      made += all;
+    }
+    __syncthreads();
+    for (int at = threadIdx.x; at < S; at += kPlanThreads) {
+      const int g = group[at];
+      if (low[g]) depth[at] = alike[g];
+      else limit[(int)(key[at] & 4095)] = 0;  // nothing further
+    }
+    if (threadIdx.x == 0) s_segs = before + made;
+    ends[level + 1] = before + made;
+    __syncthreads();
+    if (made == 0) {
+      for (int k = level + 1; k < kShareLevels; ++k) ends[k + 1] = before;
+      break;
+    }
+  }
+  const int shared = s_segs;
+  __syncthreads();
+  for (int k = a.z.levels; k < kShareLevels; ++k) ends[k + 1] = shared;
+  // what sessions hold alone
+  int longest = 0;
+  for (int at = threadIdx.x; at < S; at += kPlanThreads) {
+    const int s = (int)(key[at] & 4095);
+    const KvSession ses = kv_session(a.kv, s);
+    int from = depth[at] << shift;
+    if (a.window > 0) {
+      const int64_t lowest = (int64_t)ses.len - ses.rows - a.window + 1;
+      if (lowest > from) from = (int)lowest & ~(kKvBlock - 1);
+    }
+    ShareItem& t = a.segs[shared + at];
+    t.first = at;
+    t.members = 1;
+    t.from = from;
+    t.to = ses.len > from ? ses.len : from;
+    a.order[at] = s;
+    if (ses.len > longest) longest = ses.len;
+  }
+  if (threadIdx.x == 0) s_segs = 0;
+  __syncthreads();
+  atomicMax(&s_segs, longest);
+  __syncthreads();
+  longest = s_segs;
+
+  // Shares: of each kind, the shortest that fill the device about once.
+  const int RG = a.kv.R * a.group;
+  int chunk[2];
+#pragma unroll
+  for (int kind = 0; kind < 2; ++kind) {
+    const ShareItem* segs = a.segs + (kind ? shared : 0);
+    const int n = kind ? S : shared, rows = a.z.rows[kind];
+    // (every wave sums them up for a candidate of its own)
+    int64_t load = 0, tiles = 0;
+    for (int i = lane; i < n; i += 64) {
+      const int64_t t = ((int64_t)segs[i].members * RG + rows - 1) / rows;
+      tiles += t;
+      load += t * (segs[i].to - segs[i].from);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      load += __shfl_xor(load, o, 64);
+      tiles += __shfl_xor(tiles, o, 64);
+    }
+    load *= a.kv.heads;
+    tiles *= a.kv.heads;
+    const int64_t slots = a.z.slots[kind];
+    const bool few = tiles < 2 * slots;
+    const int64_t target = 2 * tiles <= slots ? slots : 2 * slots;
+    int64_t c = few ? load * (8 + wave) / (8 * target) : load / slots;
+    const int64_t room = a.z.extra > 0 ? (longest + a.z.extra - 1) / a.z.extra : longest;
+    if (wave == 15 && few) c = longest;
+    if (c < room) c = room;
+    if (c < kShareLeast) c = kShareLeast;
+    c = (c + kShareStep - 1) / kShareStep * kShareStep;
+    int64_t items = 0;
+    for (int i = lane; i < n; i += 64)
+      items += ((int64_t)segs[i].members * RG + rows - 1) / rows * ((segs[i].to - segs[i].from + c - 1) / c);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) items += __shfl_xor(items, o, 64);
+    if (lane == 0) s_chunk[wave] = !few || wave == 15 || items * a.kv.heads <= target ? (int)c : INT32_MAX;
+    __syncthreads();
+    chunk[kind] = INT32_MAX;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) chunk[kind] = s_chunk[k] < chunk[kind] ? s_chunk[k] : chunk[kind];
+    __syncthreads();
+  }
+
+  // Parts of each segment, level by level along the paths, and the items.
+  int made[2] = {0, 0};
+#pragma unroll
+  for (int level = 0; level <= kShareLevels; ++level) {
+    const int kind = level == kShareLevels;
+    const int lo = kind ? shared : ends[level], hi = kind ? shared + S : ends[level + 1];
+    const int c = chunk[kind], rows = a.z.rows[kind];
+    for (int i0 = lo; i0 < hi; i0 += kPlanThreads) {
+      const int i = i0 + threadIdx.x;
+      int tiles = 0, shares = 0;
+      ShareItem t{};
+      if (i < hi) {
+        t = a.segs[i];
+        tiles = (int)(((int64_t)t.members * RG + rows - 1) / rows);
+        shares = (t.to - t.from + c - 1) / c;
+      }
+      int all = 0;
+      const int at = made[kind] + sum_before(tiles * shares, &all);
+      if (i < hi) {
+        const int part = count[t.first];
+        for (int k = 0; k < shares; ++k)
+          for (int x = 0; x < tiles; ++x) {
+            const int64_t to = (int64_t)t.from + (int64_t)(k + 1) * c;
+            const ShareItem it{t.first, t.members, x, t.from + k * c, to < t.to ? (int)to : t.to, part + k, tiles == 1, 0};
+            if (at + k * tiles + x < a.z.cap[kind]) a.items[kind][at + k * tiles + x] = it;
+          }
+        for (int m = 0; m < t.members; ++m) count[t.first + m] = part + shares;
+      }
+      made[kind] += all;
+      __syncthreads();
+    }
+  }
+  for (int at = threadIdx.x; at < S; at += kPlanThreads) a.parts[(int)(key[at] & 4095)] = count[at];
+  if (threadIdx.x < 2) a.head->items[threadIdx.x] = made[threadIdx.x];
+  if (threadIdx.x == 0) a.head->key = a.key;
+}
+
+struct ShareArgs {
+  KvArgs kv;
+  const uint16_t* q;
+  int64_t q_row, q_head;
+  uint16_t* out;
+  int64_t o_row, o_head;
+  float* lse;
+  int group, window;
+  float scale_log2, binade;
+  bool q_aligned, o_aligned;
+  uint32_t key;
+  const ShareHead* head;
+  const int32_t* order;
+  const int32_t* n_parts;
+  const ShareItem* items;
+  int kind;
+  int cap;
+  int parts;        // places of a row
+  float2* part_ml;  // [rows x heads][parts]: reference of the weights, their sum
+  float* part_o;    // [rows x heads][parts][D]
+};
+
+// A row of an item: number fq of its sessions' rows.
+struct ShareRow {
+  int session, r, in_group;  // in_group: query head of the key/value head's
+  bool is;
+};
+__device__ __forceinline__ ShareRow share_row(const ShareArgs& a, const ShareItem& it, int fq, int RG, int G) {
+  const int member = fq / RG, x = fq - member * RG;
+  ShareRow w;
+  w.r = x / G;
+  w.in_group = x - w.r * G;
+  const int at = it.first + member;
+  w.is = member < it.members && (unsigned)at < (unsigned)a.kv.n_sessions;
+  w.session = w.is ? a.order[at] : 0;
+  w.is = w.is && (unsigned)w.session < (unsigned)a.kv.n_sessions;
+  if (!w.is) w.session = 0;
+  return w;
+}
+
+template <int D, int MT, int WT>
+__global__ __launch_bounds__(64 * waves_in(WT), waves_of(D, MT, WT)) void k_share_part(ShareArgs a) {
+  constexpr int NS = stages_of(D, WT);
+  constexpr int NW = waves_in(WT);
+  constexpr int WR = NW / WT;
+  constexpr int KJ = D / 32;   // steps of the first product
+  constexpr int VC = D / 16;   // products of the second
+  constexpr bool QL = queries_in_lds(D, MT);
+  const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int wt = wave % WT, wr = wave / WT;
+  extern __shared__ __align__(16) uint8_t smem[];  // rings, then queries of each group of rows
+  const int G = a.group, RG = a.kv.R * G;
+  if (a.head->key != a.key) return;
+  const int n_items = a.head->items[a.kind] < a.cap ? a.head->items[a.kind] : a.cap;
+  const int64_t n_blocks = (int64_t)n_items * a.kv.heads;
+
+  for (int64_t block = blockIdx.x; block < n_blocks; block += gridDim.x) {
+    if (block != blockIdx.x) __syncthreads();  // the outputs in LDS are read
+    const int head = (int)(block % a.kv.heads);
+    const auto* x8 = (const __attribute__((address_space(4))) int32_t*)(a.items + block / a.kv.heads);
+    const ShareItem it{x8[0], x8[1], x8[2], x8[3], x8[4], x8[5], x8[6], 0};
+    const int lead = (unsigned)it.first < (unsigned)a.kv.n_sessions ? a.order[it.first] : 0;
+    const KvSession ses = kv_session(a.kv, (unsigned)lead < (unsigned)a.kv.n_sessions ? lead : 0);
+    const int row0 = (it.tile * WR + wr) * 16 * MT;  // the wave's first
+
+    u32x4_t* s_q = reinterpret_cast<u32x4_t*>(smem + NW * NS * Stage<D>::kBytes);
+    Queries<D, MT, QL> q;
+    q.l = s_q;
+    q.own = wr * (MT * KJ * 64) + lane;
+    int pos[MT];
+    int low = kKvMost, high = -1;  // of the rows that are
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const ShareRow w = share_row(a, it, row0 + m * 16 + n, RG, G);
+      const KvSession its = kv_session(a.kv, w.session);
+      const bool live = w.is && w.r < its.rows;
+      const int at = its.len - its.rows + w.r;
+      pos[m] = live ? at : -1;
+      if (live) {
+        low = at < low ? at : low;
+        high = at > high ? at : high;
+      }
+      const uint16_t* p = a.q + ((int64_t)w.session * a.kv.R + w.r) * a.q_row + (int64_t)(head * G + w.in_group) * a.q_head + g * (D / 4);
+#pragma unroll
+      for (int j = 0; j < KJ; ++j) {
+        u32x4_t x{0u, 0u, 0u, 0u};
+        // (waves that share rows share the work of it)
+        if (live && (!QL || j % WT == wt)) {
+          if (a.q_aligned) {
+            x = *reinterpret_cast<const u32x4_t*>(p + 8 * j);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = (uint32_t)p[8 * j + 2 * i] | ((uint32_t)p[8 * j + 2 * i + 1] << 16);
+          }
+        }
+        if constexpr (!QL) q.r[m][j] = __builtin_bit_cast(bf16x8_t, x);
+        else if (j % WT == wt) s_q[((wr * MT + m) * KJ + j) * 64 + lane] = x;
+      }
+    }
+    // tokens that the wave's rows see, and those that all of them see
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) {
+      const int x = __shfl_xor(low, o, 64), y = __shfl_xor(high, o, 64);
+      low = x < low ? x : low;
+      high = y > high ? y : high;
+    }
+    low = __builtin_amdgcn_readfirstlane(low);
+    high = __builtin_amdgcn_readfirstlane(high);
+    int from = it.from > 0 ? it.from & ~(kKvBlock - 1) : 0;
+    int to = it.to < high + 1 ? it.to : high + 1;
+    to = to < ses.len ? to : ses.len;
+    int all_lo = 0;
+    const int all_hi = low < 0 ? 0 : low + 1;
+    if (a.window > 0) {
+      const int64_t first = (int64_t)low - a.window + 1;
+      if (first > from) from = (int)first & ~(kKvBlock - 1);
+      all_lo = high - a.window + 1;
+    }
+
+    Rows<D, MT> w;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      w.top[m] = kNoScore;
+      w.sum[m] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < VC; ++c) w.o[m][c] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    // The wave's tiles as in kv_attend.hip: those that all its rows see whole first.
+    constexpr int STEP = 32 * WT;
+    const int start = from + 32 * wt;
+    int whole = start + (all_lo > start ? (all_lo - start + STEP - 1) / STEP * STEP : 0);
+    int part = whole + ((all_hi < to ? all_hi : to) - whole + STEP - 32) / STEP * STEP;
+    if (part <= whole) whole = part = start;
+    const int n_whole = (part - whole) / STEP, n_head = (whole - start) / STEP;
+    const int n_tiles = n_whole + n_head + (to > part ? (to - part + STEP - 1) / STEP : 0);
+    auto place = [&](int k) {
+      if (k >= n_tiles) return to;
+      return k < n_whole ? whole + k * STEP : (k < n_whole + n_head ? start : part - n_head * STEP) + (k - n_whole) * STEP;
+    };
+
+    uint8_t* ring = smem + wave * (NS * Stage<D>::kBytes);
+    uint32_t lane16 = lane * 16;
+    const bool alone = WT >= 4 && it.alone;
+    const uint32_t ring_at = (uint32_t)(uintptr_t)(lds_void_t*)ring;
+    // the lane's places in a stage: keys token n of a block, values as they lie
+    const uint32_t key_at = n * (D / 2) + g * (D / 8), value_at = KvLayout<D>::kValues + lane * (D / 8);
+    const uint32_t ks_at = Stage<D>::kCodes + (D == 64 ? g >> 1 : D == 128 ? g : 2 * g) * kKvBlock + n;
+    const uint32_t vs_at = Stage<D>::kCodes + D / 2 + n * D / 512 * kKvBlock + 4 * g;
+    uint32_t none = 0;  // of the tiles in flight, the next in the low bits: blocks without a page
+    auto none_of = [](const KvPages& p) { return (uint32_t)(p.page[0] < 0) | ((uint32_t)(p.page[1] < 0) << 1); };
+#pragma unroll
+    for (int i = 0; i < NS - 1; ++i)
+      if (i < n_tiles) {
+        const KvPages pages = tile_pages(a.kv, ses, place(i), to);
+        none |= none_of(pages) << (2 * i);
+        copy_tile<D>(ring + i * Stage<D>::kBytes, a.kv, head, place(i), pages, lane16, lane, alone);
+      }
+    if constexpr (QL) __syncthreads();
+    else  // here, not in the loop: the compiler's wait would be for all copies in flight
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < KJ; ++j) asm volatile("" : "+v"(q.r[m][j]));
+    KvPages ahead = tile_pages(a.kv, ses, place(NS - 1), to);
+    int k = 0, stage = 0, fill = NS - 1;  // stages read and written next
+    KvKeys<D> keys;
+    KvValues<D> values;
+    f32x4_t sc[MT][2];
+    bf16x8_t p[MT];
+    // asks for the tile NS - 1 ahead, waits for this one, and scores it
+    auto begin = [&] {
+      const KvPages after = tile_pages(a.kv, ses, place(k + NS), to);
+      if (k + NS - 1 < n_tiles) {
+        none |= none_of(ahead) << (2 * (NS - 1));
+        copy_tile<D>(ring + fill * Stage<D>::kBytes, a.kv, head, place(k + NS - 1), ahead, lane16, lane, alone);
+        wait_copies<(NS - 1) * Stage<D>::kCopies>();
+      } else if (NS > 2 && k + 2 == n_tiles) {
+        wait_copies<Stage<D>::kCopies>();
+      } else if (NS > 3 && k + 3 == n_tiles) {
+        wait_copies<2 * Stage<D>::kCopies>();
+      } else {
+        wait_copies<0>();
+      }
+      ahead = after;
+      const uint32_t at = ring_at + stage * Stage<D>::kBytes;
+      read_codes<D>(keys.c, keys.s[0], keys.s[1], at + key_at, at + ks_at, true);
+      take_keys(sc, keys, q);
+      read_codes<D>(values.c, values.s[0], values.s[1], at + value_at, at + vs_at, false);
+      if (none & 3) {  // no such tokens: no weight, and values that zero times is zero
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+          if ((none >> b) & 1) {
+            values.s[b] = 0u;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) sc[m][b] = f32x4_t{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          }
+      }
+      none >>= 2;
+      stage = stage + 1 == NS ? 0 : stage + 1;
+      fill = fill + 1 == NS ? 0 : fill + 1;
+    };
+    for (; k < n_whole; ++k) {
+      begin();
+      take_weights(p, w, sc, a.scale_log2);
+      take_values(w, values, p);
+    }
+    for (; k < n_tiles; ++k) {
+      const int t0 = place(k);
+      begin();
+      mask_scores(sc, pos, a.window, t0, g);
+      take_weights(p, w, sc, a.scale_log2);
+      if (t0 + 32 > ses.len) {
+        const int held[2] = {ses.len - t0, ses.len - t0 - kKvBlock};
+        clear_values(values, held, g);
+      }
+      take_values(w, values, p);
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) w.sum[m] = sum_over_groups(w.sum[m]);
+
+    // the waves' outputs, in what were rings
+    float* s_o = reinterpret_cast<float*>(smem);       // NW x 16 D
+    float* s_ml = reinterpret_cast<float*>(smem) + NW * 16 * D;
+    __syncthreads();
+    if (g == 0)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        s_ml[((wave * MT + m) * 16 + n) * 2] = w.top[m];
+        s_ml[((wave * MT + m) * 16 + n) * 2 + 1] = w.sum[m];
+      }
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      constexpr int PER = D / 4 / WT;  // values a lane ends with
+      float t = kNoScore, l = 0.0f;
+#pragma unroll
+      for (int k = 0; k < WT; ++k) t = fmaxf(t, s_ml[(((wr * WT + k) * MT + m) * 16 + n) * 2]);
+#pragma unroll
+      for (int k = 0; k < WT; ++k) {
+        const float* ml = &s_ml[(((wr * WT + k) * MT + m) * 16 + n) * 2];
+        l += ml[1] * __builtin_amdgcn_exp2f(ml[0] - t);
+      }
+      const float f = __builtin_amdgcn_exp2f(w.top[m] - t);
+      if (m > 0) __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int c = 0; c < VC; ++c) s_o[((wave * 4 + e) * VC + c) * 64 + lane] = w.o[m][c][e] * f;
+      __syncthreads();
+      float y[PER];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        float x = 0.0f;
+#pragma unroll
+        for (int k = 0; k < WT; ++k) x += s_o[((wr * WT + k) * 4 * VC + wt * PER + i) * 64 + lane];
+        y[i] = x;
+      }
+      const int d0 = g * (D / 4) + wt * PER;  // the first of them
+      const ShareRow row = share_row(a, it, row0 + m * 16 + n, RG, G);
+      if (row.is && (unsigned)it.part < (unsigned)a.parts) {
+        if (row.r >= kv_session(a.kv, row.session).rows) l = 0.0f;  // a row that is none
+        const int64_t at = (((int64_t)row.session * a.kv.R + row.r) * (a.kv.heads * G) + head * G + row.in_group) * a.parts + it.part;
+        if (g == 0 && wt == 0) a.part_ml[at] = make_float2(t, l);
+        if (!(l == 0.0f)) {
+#pragma unroll
+          for (int i = 0; i < PER; i += 4)
+            *reinterpret_cast<f32x4_t*>(a.part_o + at * D + d0 + i) = f32x4_t{y[i], y[i + 1], y[i + 2], y[i + 3]};
+        }
+      }
+    }
+  }
+}
+
+// A row's parts joined, in their order; D/4 lanes a row and head.
+template <int D>
+__global__ __launch_bounds__(256) void k_share_join(ShareArgs a, int64_t rows) {
+  constexpr int LPS = D / 4;
+  const int d4 = threadIdx.x % LPS;
+  const int64_t i = (int64_t)blockIdx.x * (256 / LPS) + threadIdx.x / LPS;
+  if (i >= rows) return;
+  const int heads = a.kv.heads * a.group;
+  const int64_t row = i / heads;
+  const int hq = (int)(i - row * heads);
+  const int session = (int)(row / a.kv.R);
+  const bool planned = a.head->key == a.key;
+  int n = planned ? a.n_parts[session] : 0;
+  n = n < a.parts ? n : a.parts;
+  if (row - (int64_t)session * a.kv.R >= kv_session(a.kv, session).rows) n = 0;
+  const float2* ml = a.part_ml + i * a.parts;
+  const float* part = a.part_o + i * a.parts * D + d4 * 4;
+  float top = kNoScore, l = planned ? 0.0f : NAN;
+  f32x4_t y{l, l, l, l};
+  for (int k0 = 0; k0 < n; k0 += 4) {
+    float2 x[4];
+    f32x4_t o[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int k = k0 + u;
+      x[u] = k < n ? ml[k] : make_float2(kNoScore, 0.0f);
+      // parts without a token left their place unwritten: read, not used
+      if (k < n) o[u] = *reinterpret_cast<const f32x4_t*>(part + (int64_t)k * D);
+    }
+    float t = top;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) t = fmaxf(t, x[u].x);
+    const float f = __builtin_amdgcn_exp2f(top - t);
+    l *= f;
+    y *= f;
+    top = t;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (x[u].y == 0.0f) continue;
+      const float e = __builtin_amdgcn_exp2f(x[u].x - top);
+      l += x[u].y * e;
+      y += o[u] * e;
+    }
+  }
+  const float f = l == 0.0f ? 0.0f : 1.0f / l;
+  uint16_t* dst = a.out + row * a.o_row + hq * a.o_head + d4 * 4;
+  const uint32_t lo = l == 0.0f ? 0u : pack_bf16(y[0] * f, y[1] * f), hi = l == 0.0f ? 0u : pack_bf16(y[2] * f, y[3] * f);
+  if (a.o_aligned) {
+    *reinterpret_cast<uint32_t*>(dst) = lo;
+    *reinterpret_cast<uint32_t*>(dst + 2) = hi;
+  } else {
+    dst[0] = (uint16_t)lo, dst[1] = (uint16_t)(lo >> 16);
+    dst[2] = (uint16_t)hi, dst[3] = (uint16_t)(hi >> 16);
+  }
+  if (a.lse && d4 == 0)
+    a.lse[i] = l == 0.0f ? -INFINITY : fmaf(top, a.binade, __builtin_amdgcn_logf(l) * kLn2);
+}
+
+namespace {
+
+ShareSizes share_sizes(int d, int64_t S, int64_t R, int64_t heads, int64_t group, int64_t max_len) {
+  ShareSizes z{};
+  const int64_t RG = R * group;
+  // Shared segments: as many rows a tile as the registers hold; own ones: as many as there are.
+  z.mt[0] = d == 256 ? 2 : 4;
+  z.wt[0] = d == 256 ? 8 : 4;
+  z.mt[1] = RG <= 16 ? 1 : d == 256 || RG <= 32 ? 2 : 4;
+  z.wt[1] = d == 256 && z.mt[1] == 2 ? 8 : 4;
+  if (S * RG > 65536) {  // prompts: nothing to cut
+    z.levels = 1;
+    z.extra = 0;
+  } else {
+    z.levels = kShareLevels;
+    const int64_t shares = (max_len + kShareLeast - 1) / kShareLeast;  // that there can be
+    z.extra = S >= 64 ? 2 : S >= 16 ? 8 : S >= 4 ? 24 : 56;
+    if (z.extra > shares) z.extra = (int)shares;
+  }
+  z.parts = z.levels + 1 + z.extra;
+  for (int k = 0; k < 2; ++k) {
+    z.rows[k] = 16 * z.mt[k] * (waves_in(z.wt[k]) / z.wt[k]);
+    z.slots[k] = kCUs * resident(d, z.mt[k], z.wt[k]);
+  }
+  // A level's segments have a tile more each than their rows fill, and shares.
+  const int64_t wide = (S * RG + z.rows[0] - 1) / z.rows[0] + S / 2 + 1, own = S * ((RG + z.rows[1] - 1) / z.rows[1]);
+  z.cap[0] = z.levels * wide * (1 + z.extra);
+  z.cap[1] = own * (1 + z.extra);
+  return z;
+}
+
+// Which calls a plan is for.
+uint32_t share_key(int d, const KvArgs& a, int group, int window, int extra) {
+  uint32_t h = 2166136261u;
+  for (const uint32_t x : {(uint32_t)d, (uint32_t)a.heads, (uint32_t)a.n_sessions, (uint32_t)a.R, (uint32_t)group,
+                           (uint32_t)window, (uint32_t)a.page_shift, (uint32_t)a.max_pages, (uint32_t)extra, 0x5348u})
+    h = (h ^ x) * 16777619u;
+  return h;
+}
+
+struct SharePlaces {
+  size_t order, parts, segs, items[2], all;
+};
+SharePlaces share_places(const ShareSizes& z, int64_t S) {
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  SharePlaces p{};
+  p.order = up(sizeof(ShareHead));
+  p.parts = p.order + up(S * 4);
+  p.segs = p.parts + up(S * 4);
+  p.items[0] = p.segs + up((z.levels + 1) * S * sizeof(ShareItem));
+  p.items[1] = p.items[0] + up(z.cap[0] * sizeof(ShareItem));
+  p.all = p.items[1] + up(z.cap[1] * sizeof(ShareItem));
+  return p;
+}
+
+template <int D, int MT, int WT>
+hipError_t launch_part(const ShareArgs& a, int64_t slots, hipStream_t s) {
+  constexpr size_t lds = attend_lds(D, MT, WT);
+  static std::atomic<uint64_t> done{0};
+  const hipError_t e = set_lds_limit_once(done, reinterpret_cast<const void*>(k_share_part<D, MT, WT>), lds);
+  if (e != hipSuccess) return e;
+  const int64_t most = (int64_t)a.cap * a.kv.heads;
+  launch_kernel(k_share_part<D, MT, WT>, dim3((unsigned)(most < slots ? most : slots)), dim3(64 * waves_in(WT)), (uint32_t)lds, s, a);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_parts(int mt, const ShareArgs& a, int64_t slots, hipStream_t s) {
+  if (mt == 1) return launch_part<D, 1, 4>(a, slots, s);
+  if constexpr (D == 256) {
+    return launch_part<D, 2, 8>(a, slots, s);
+  } else {
+    return mt == 2 ? launch_part<D, 2, 4>(a, slots, s) : launch_part<D, 4, 4>(a, slots, s);
+  }
+}
+
+}  // namespace
+
+bool kv_share_fits(int64_t n_sessions, int64_t R, int64_t q_heads) {
+  return n_sessions <= kShareSessions && n_sessions * R * q_heads <= (int64_t(1) << 26);
+}
+
+size_t kv_share_bytes(int d, int64_t n_sessions, int64_t R, int64_t heads, int64_t q_heads, int64_t max_len) {
+  return share_places(share_sizes(d, n_sessions, R, heads, q_heads / heads, max_len), n_sessions).all;
+}
+
+size_t kv_share_scratch(int d, int64_t n_sessions, int64_t R, int64_t heads, int64_t q_heads, int64_t max_len) {
+  const ShareSizes z = share_sizes(d, n_sessions, R, heads, q_heads / heads, max_len);
+  const size_t n = (size_t)n_sessions * R * q_heads * z.parts;
+  return (n * 8 + 255) / 256 * 256 + n * d * 4;
+}
+
+hipError_t launch_share_plan(int d, const KvArgs& kv, int q_heads, int window, int64_t max_len, void* plan, hipStream_t s) {
+  SharePlanArgs a{};
+  a.kv = kv;
+  a.group = q_heads / kv.heads;
+  a.window = window;
+  a.z = share_sizes(d, kv.n_sessions, kv.R, kv.heads, a.group, max_len);
+  a.key = share_key(d, kv, a.group, window, a.z.extra);
+  const SharePlaces p = share_places(a.z, kv.n_sessions);
+  uint8_t* base = static_cast<uint8_t*>(plan);
+  a.head = reinterpret_cast<ShareHead*>(base);
+  a.order = reinterpret_cast<int32_t*>(base + p.order);
+  a.parts = reinterpret_cast<int32_t*>(base + p.parts);
+  a.segs = reinterpret_cast<ShareItem*>(base + p.segs);
+  for (int k = 0; k < 2; ++k) a.items[k] = reinterpret_cast<ShareItem*>(base + p.items[k]);
+  int n2 = 2;
+  while (n2 < kv.n_sessions) n2 *= 2;
+  static std::atomic<uint64_t> done{0};
+  const hipError_t e = set_lds_limit_once(done, reinterpret_cast<const void*>(k_share_plan), kShareSessions * 36 + 16);
+  if (e != hipSuccess) return e;
+  launch_kernel(k_share_plan, dim3(1), dim3(kPlanThreads), (uint32_t)(n2 * 36 + 16), s, a, n2);
+  return hipGetLastError();
+}
+
+hipError_t launch_attend_shared(int d, const KvArgs& kv, const AttendCall& c, const void* plan, void* workspace, hipStream_t s) {
+  ShareArgs a{};
+  a.kv = kv;
+  a.q = static_cast<const uint16_t*>(c.q);
+  a.q_row = c.q_row;
+  a.q_head = c.q_head;
+  a.out = static_cast<uint16_t*>(c.out);
+  a.o_row = c.o_row;
+  a.o_head = c.o_head;
+  a.lse = c.lse;
+  a.group = c.q_heads / kv.heads;
+  a.window = c.window;
+  a.scale_log2 = c.scale * 1.44269504088896f;
+  a.binade = (float)((double)c.scale / a.scale_log2);
+  a.q_aligned = c.q_row % 8 == 0 && c.q_head % 8 == 0 && (reinterpret_cast<uintptr_t>(c.q) & 15) == 0;
+  a.o_aligned = c.o_row % 2 == 0 && c.o_head % 2 == 0 && (reinterpret_cast<uintptr_t>(c.out) & 3) == 0;
+  const ShareSizes z = share_sizes(d, kv.n_sessions, kv.R, kv.heads, a.group, c.max_len);
+  const SharePlaces p = share_places(z, kv.n_sessions);
+  const uint8_t* base = static_cast<const uint8_t*>(plan);
+  a.key = share_key(d, kv, a.group, c.window, z.extra);
+  a.head = reinterpret_cast<const ShareHead*>(base);
+  a.order = reinterpret_cast<const int32_t*>(base + p.order);
+  a.n_parts = reinterpret_cast<const int32_t*>(base + p.parts);
+  a.parts = z.parts;
+  const int64_t rows = (int64_t)kv.n_sessions * kv.R * c.q_heads;
+  a.part_ml = static_cast<float2*>(workspace);
+  a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + ((size_t)rows * z.parts * 8 + 255) / 256 * 256);
+  for (int k = 0; k < 2; ++k) {
+    if (k == 0 && kv.n_sessions == 1) continue;
+    a.kind = k;
+    a.cap = (int)z.cap[k];
+    a.items = reinterpret_cast<const ShareItem*>(base + p.items[k]);
+    const hipError_t e = d == 64    ? launch_parts<64>(z.mt[k], a, z.slots[k], s)
+                         : d == 128 ? launch_parts<128>(z.mt[k], a, z.slots[k], s)
+                                    : launch_parts<256>(z.mt[k], a, z.slots[k], s);
+    if (e != hipSuccess) return e;
+  }
+  const int64_t per = 256 / (d / 4);
+  const dim3 grid((unsigned)((rows + per - 1) / per));
+  if (d == 64) launch_kernel(k_share_join<64>, grid, dim3(256), 0, s, a, rows);
+  else if (d == 128) launch_kernel(k_share_join<128>, grid, dim3(256), 0, s, a, rows);
+  else launch_kernel(k_share_join<256>, grid, dim3(256), 0, s, a, rows);
+  return hipGetLastError();
+}
+
+}  // namespace sph

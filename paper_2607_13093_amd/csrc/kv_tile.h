@@ -332,6 +332,27 @@ __device__ __forceinline__ void take_values(Rows<D, MT>& w, const KvValues<D>& v
   }
 }
 
+// A workgroup is 4 waves, WT of which (4 or 2) share the tokens of the same rows
+// while 4 / WT have rows of their own, or 8 that share the tokens of one group of rows.
+constexpr int waves_in(int wt) { return wt == 8 ? 8 : 4; }
+// Waves of a SIMD that the registers leave room for, and the stages of a ring.
+constexpr int waves_of(int d, int mt, int wt) {
+  return wt == 8 ? (d == 128 ? 4 : 2) : d * mt <= 128 ? 4 : (mt < 4 && d * mt <= 256 ? 3 : 2);
+}
+constexpr bool queries_in_lds(int d, int mt) { return d * mt >= 512; }
+constexpr int stages_of(int d, int wt) { return d == 64 ? 4 : (d == 128 && wt < 8 ? 3 : 2); }
+// LDS of a workgroup: rings and queries, in their place the waves' outputs.
+constexpr int attend_lds(int d, int mt, int wt) {
+  const int nw = waves_in(wt);
+  const int run = nw * stages_of(d, wt) * ((34 * d + 255) / 256 * 256) +
+                  (queries_in_lds(d, mt) ? nw / wt * mt * (d / 32) * 1024 : 0);
+  const int end = nw * (64 * d + 128 * mt);
+  return run > end ? run : end;
+}
+constexpr int resident(int d, int mt, int wt) {  // workgroups of a CU
+  const int by_lds = 160 * 1024 / attend_lds(d, mt, wt), by_waves = waves_of(d, mt, wt) * 4 / waves_in(wt);
+  return by_lds < by_waves ? by_lds : by_waves;
+}
 // Tokens that rows r_lo ... r_hi of a session see (lo ... hi - 1, lo down to a whole
 // tile) and those that all of them see.  base: position of row 0, from -kKvMost on;
 // window below kKvMost (kv_window), so that nothing passes 32 bits.

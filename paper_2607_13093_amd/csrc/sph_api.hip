@@ -1134,6 +1134,94 @@ int sph_pages_compact(const sph_kv_cache* cache, int32_t* table_out, int64_t ld_
   return ok();
 }
 
+namespace {
+
+// Sizes that the queries of shared attention have in common with its calls.
+bool share_sizes_ok(const sph_kv_cache* c, int64_t q_heads, int64_t n_sessions, int64_t R, int64_t max_len) {
+  return c && kv_sizes_ok(c->kv_heads, c->head_dim, c->page_tokens) && q_heads >= 1 && q_heads <= 65535 &&
+         q_heads % c->kv_heads == 0 && n_sessions >= 1 && R >= 1 && R <= sph::kKvMost && max_len >= 0 &&
+         c->max_pages >= 1 && sph::kv_share_fits(n_sessions, R, q_heads);
+}
+
+int share_call(const char* fn, const sph_kv_cache* cache, int64_t layer, int64_t q_heads, int64_t n_sessions, int64_t R,
+               const int32_t* rows, const int32_t* slots, int64_t window, int64_t max_len, sph::KvArgs* a) {
+  const int e = kv_call(fn, cache, layer, n_sessions, R, rows, slots, a);
+  if (e != SPH_OK) return e;
+  if (q_heads < 1 || q_heads > 65535 || q_heads % cache->kv_heads != 0)
+    return fail(SPH_E_INVALID_ARG, "%s: q_heads=%lld is no multiple of kv_heads=%d", fn, (long long)q_heads,
+                cache->kv_heads);
+  if (window < 0 || max_len < 0)
+    return fail(SPH_E_INVALID_ARG, "%s: window=%lld max_len=%lld", fn, (long long)window, (long long)max_len);
+  if (!sph::kv_share_fits(n_sessions, R, q_heads))
+    return fail(SPH_E_UNSUPPORTED, "%s: n_sessions=%lld R=%lld q_heads=%lld (4096 sessions, 2^26 rows of heads at most)", fn,
+                (long long)n_sessions, (long long)R, (long long)q_heads);
+  return SPH_OK;
+}
+
+}  // namespace
+
+size_t sph_kv_share_bytes(const sph_kv_cache* cache, int64_t q_heads, int64_t n_sessions, int64_t R, int64_t max_len) {
+  if (!share_sizes_ok(cache, q_heads, n_sessions, R, max_len)) return 0;
+  return sph::kv_share_bytes(cache->head_dim, n_sessions, R, cache->kv_heads, q_heads, kv_most(cache, max_len));
+}
+
+int sph_kv_share(const sph_kv_cache* cache, int64_t q_heads, int64_t n_sessions, int64_t R,
+                 const int32_t* rows, const int32_t* slots, int64_t window, int64_t max_len,
+                 void* plan, size_t plan_bytes, void* stream) {
+  const char* fn = "sph_kv_share";
+  sph::KvArgs a;
+  const int e = share_call(fn, cache, 0, q_heads, n_sessions, R, rows, slots, window, max_len, &a);
+  if (e != SPH_OK) return e;
+  if (n_sessions == 0 || R == 0) return ok();
+  const int pe = pages_ws(fn, plan, plan_bytes, sph_kv_share_bytes(cache, q_heads, n_sessions, R, max_len));
+  if (pe != SPH_OK) return pe;
+  hipStream_t s = (hipStream_t)stream;
+  const int w = (int)sph::kv_window(window, kv_most(cache, 0));
+  const hipError_t he = traced("kv_share", s, [&] {
+    return sph::launch_share_plan(cache->head_dim, a, (int)q_heads, w, kv_most(cache, max_len), plan, s);
+  });
+  if (he != hipSuccess) return hip_fail(he, "sharing plan launch");
+  return ok();
+}
+
+size_t sph_kv_attend_shared_workspace(const sph_kv_cache* cache, int64_t q_heads, int64_t n_sessions, int64_t R,
+                                      int64_t max_len) {
+  if (!share_sizes_ok(cache, q_heads, n_sessions, R, max_len)) return 0;
+  return sph::kv_share_scratch(cache->head_dim, n_sessions, R, cache->kv_heads, q_heads, kv_most(cache, max_len));
+}
+
+int sph_kv_attend_shared(const sph_kv_cache* cache, int64_t layer, const void* q, int64_t q_row,
+                         int64_t q_head, int64_t q_heads, int64_t n_sessions, int64_t R,
+                         const int32_t* rows, const int32_t* slots, float scale, int64_t window,
+                         int64_t max_len, const void* plan, size_t plan_bytes, void* out,
+                         int64_t o_row, int64_t o_head, float* lse_out, void* workspace,
+                         size_t ws_bytes, void* stream) {
+  const char* fn = "sph_kv_attend_shared";
+  sph::KvArgs a;
+  const int e = share_call(fn, cache, layer, q_heads, n_sessions, R, rows, slots, window, max_len, &a);
+  if (e != SPH_OK) return e;
+  const int64_t d = cache->head_dim;
+  if (!(scale > 0.0f && scale <= 1e6f)) return fail(SPH_E_INVALID_ARG, "%s: scale=%g not in (0, 1e6]", fn, scale);
+  if (!kv_strides_ok(q_row, q_head, q_heads, d) || !kv_strides_ok(o_row, o_head, q_heads, d))
+    return fail(SPH_E_INVALID_ARG, "%s: row and head strides %lld, %lld and %lld, %lld for %lld heads of %lld", fn,
+                (long long)q_row, (long long)q_head, (long long)o_row, (long long)o_head, (long long)q_heads,
+                (long long)d);
+  if (n_sessions == 0 || R == 0) return ok();
+  if (!q || !out) return fail(SPH_E_INVALID_ARG, "%s: q or out is NULL", fn);
+  if (!plan || plan_bytes < sph_kv_share_bytes(cache, q_heads, n_sessions, R, max_len) || (reinterpret_cast<uintptr_t>(plan) & 15))
+    return fail(SPH_E_INVALID_ARG, "%s: plan %p of %zu bytes, need %zu (16-byte aligned)", fn, plan, plan_bytes,
+                sph_kv_share_bytes(cache, q_heads, n_sessions, R, max_len));
+  const int we = pages_ws(fn, workspace, ws_bytes, sph_kv_attend_shared_workspace(cache, q_heads, n_sessions, R, max_len));
+  if (we != SPH_OK) return we;
+  const sph::AttendCall c{q, q_row, q_head, (int)q_heads, scale, (int)sph::kv_window(window, kv_most(cache, 0)),
+                          kv_most(cache, max_len), out, o_row, o_head, lse_out};
+  hipStream_t s = (hipStream_t)stream;
+  const hipError_t he =
+      traced("kv_attend_shared", s, [&] { return sph::launch_attend_shared((int)d, a, c, plan, workspace, s); });
+  if (he != hipSuccess) return hip_fail(he, "shared attention launch");
+  return ok();
+}
+
 size_t sph_kv_weigh_workspace(const sph_kv_cache* cache, int64_t q_heads, int64_t n_sessions,
                               int64_t R, int64_t max_len) {
   if (!cache || !kv_sizes_ok(cache->kv_heads, cache->head_dim, cache->page_tokens) || q_heads < 1 ||

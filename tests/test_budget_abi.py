@@ -110,3 +110,60 @@ def test_weigh_workspace_and_empty_calls(lib):
     assert lib.sph_kv_weigh_workspace(_ptr(_cache(n_slots=4096)), 32, 4096, 1, 0) == 0
     for kw in (dict(n=0), dict(R=0)):
         assert _weigh(lib, c, q=None, lse=None, w=None, ws=None, nb=0, **kw) == 0
+
+
+def _share(lib, c, q_heads=32, n=3, R=5, rows=None, slots=None, window=0, max_len=0, plan=4096, nb=BIG):
+    return lib.sph_kv_share(_ptr(c), q_heads, n, R, rows, slots, window, max_len, plan, nb, None)
+
+
+def _shared(lib, c, layer=0, q=16, q_row=4096, q_head=128, q_heads=32, n=3, R=5, rows=None, slots=None, scale=0.1, window=0,
+            max_len=0, plan=4096, plan_bytes=BIG, out=16, o_row=4096, o_head=128, lse=None, ws=4096, nb=BIG):
+    return lib.sph_kv_attend_shared(_ptr(c), layer, q, q_row, q_head, q_heads, n, R, rows, slots, scale, window, max_len, plan,
+                                    plan_bytes, out, o_row, o_head, lse, ws, nb, None)
+
+
+@pytest.mark.parametrize("kw,code,msg", BAD_CACHES)
+def test_share_cache_checks(lib, kw, code, msg):
+    c = _cache(**kw)
+    for call in (_share, _shared):
+        assert call(lib, c) == code and msg in lib.sph_last_error(), lib.sph_last_error()
+        assert call(lib, None) == E
+
+
+BOTH = [
+    (dict(n=-1), E, b"n_sessions=-1"), (dict(n=5), E, b"beyond n_slots=4"), (dict(R=-1), E, b"R=-1"),
+    (dict(q_heads=12), E, b"q_heads=12"), (dict(q_heads=0), E, b"q_heads=0"), (dict(window=-1), E, b"window=-1"),
+    (dict(max_len=-1), E, b"max_len=-1"), (dict(n=4097, slots=16), U, b"4096 sessions"), (dict(R=1 << 24), U, b"2^26 rows"),
+]
+
+
+@pytest.mark.parametrize("kw,code,msg", BOTH + [
+    (dict(plan=None), W, b"workspace"), (dict(plan=4104), W, b"workspace"), (dict(nb=100), W, b"workspace")])
+def test_share_checks(lib, kw, code, msg):
+    c = _cache()
+    assert _share(lib, c, **kw) == code and msg in lib.sph_last_error(), lib.sph_last_error()
+
+
+@pytest.mark.parametrize("kw,code,msg", BOTH + [
+    (dict(layer=2), E, b"layer=2"), (dict(scale=0.0), E, b"scale"), (dict(scale=float("inf")), E, b"scale"),
+    (dict(q_row=127), E, b"strides"), (dict(q_head=64), E, b"strides"), (dict(o_row=127), E, b"strides"),
+    (dict(q=None), E, b"NULL"), (dict(out=None), E, b"NULL"), (dict(plan=None), E, b"plan"), (dict(plan=4104), E, b"plan"),
+    (dict(plan_bytes=100), E, b"plan"), (dict(ws=None), W, b"workspace"), (dict(ws=4104), W, b"workspace"),
+    (dict(nb=100), W, b"workspace")])
+def test_shared_attention_checks(lib, kw, code, msg):
+    c = _cache()
+    assert _shared(lib, c, **kw) == code and msg in lib.sph_last_error(), lib.sph_last_error()
+
+
+def test_share_sizes_and_empty_calls(lib):
+    c = _cache()
+    p = _ptr(c)
+    plan, ws = lib.sph_kv_share_bytes(p, 32, 3, 5, 0), lib.sph_kv_attend_shared_workspace(p, 32, 3, 5, 0)
+    assert plan > 0 and ws >= 3 * 5 * 32 * 2 * (128 * 4 + 8)
+    assert _share(lib, c, nb=plan - 1) == W and _shared(lib, c, plan_bytes=plan - 1) == E and _shared(lib, c, nb=ws - 1) == W
+    for bad in ((None, 32, 3, 5, 0), (p, 12, 3, 5, 0), (p, 32, 0, 5, 0), (p, 32, 3, 0, 0), (p, 32, 3, 5, -1),
+                (p, 32, 4097, 5, 0), (p, 32, 3, 1 << 24, 0)):
+        assert lib.sph_kv_share_bytes(*bad) == 0 and lib.sph_kv_attend_shared_workspace(*bad) == 0
+    for kw in (dict(n=0), dict(R=0)):
+        assert _share(lib, c, plan=None, nb=0, **kw) == 0
+        assert _shared(lib, c, q=None, out=None, plan=None, plan_bytes=0, ws=None, nb=0, **kw) == 0
