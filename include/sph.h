@@ -482,7 +482,8 @@ int sph_kv_attend(const sph_kv_cache* cache, int64_t layer, const void* q, int64
  *
  * n_sessions <= 4096, n_sessions * R * q_heads <= 2^26
  * max_len      as in sph_kv_attend
- * plan         device memory of sph_kv_share_bytes, 16-byte aligned
+ * plan         device memory of sph_kv_share_bytes, 16-byte aligned.  Calls that share
+ *              one must not overlap (it holds the calls' work queue).
  * workspace    >= sph_kv_attend_shared_workspace bytes, 16-byte aligned
  */
 size_t sph_kv_share_bytes(const sph_kv_cache* cache, int64_t q_heads, int64_t n_sessions,
@@ -495,7 +496,7 @@ size_t sph_kv_attend_shared_workspace(const sph_kv_cache* cache, int64_t q_heads
 int sph_kv_attend_shared(const sph_kv_cache* cache, int64_t layer, const void* q, int64_t q_row,
                          int64_t q_head, int64_t q_heads, int64_t n_sessions, int64_t R,
                          const int32_t* rows, const int32_t* slots, float scale, int64_t window,
-                         int64_t max_len, const void* plan, size_t plan_bytes, void* out,
+                         int64_t max_len, void* plan, size_t plan_bytes, void* out,
                          int64_t o_row, int64_t o_head, float* lse_out, void* workspace,
                          size_t ws_bytes, void* stream);
 

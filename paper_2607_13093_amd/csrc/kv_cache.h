@@ -128,7 +128,7 @@ bool kv_share_fits(int64_t n_sessions, int64_t R, int64_t q_heads);
 size_t kv_share_bytes(int d, int64_t n_sessions, int64_t R, int64_t heads, int64_t q_heads, int64_t max_len);
 size_t kv_share_scratch(int d, int64_t n_sessions, int64_t R, int64_t heads, int64_t q_heads, int64_t max_len);
 hipError_t launch_share_plan(int d, const KvArgs& kv, int q_heads, int window, int64_t max_len, void* plan, hipStream_t s);
-hipError_t launch_attend_shared(int d, const KvArgs& kv, const AttendCall& c, const void* plan, void* workspace, hipStream_t s);
+hipError_t launch_attend_shared(int d, const KvArgs& kv, const AttendCall& c, void* plan, void* workspace, hipStream_t s);
 
 size_t kv_weigh_scratch(int d, int64_t n_sessions, int64_t R, int64_t heads, int64_t q_heads, int64_t max_len);
 hipError_t launch_kv_weigh(int d, const KvArgs& kv, const WeighCall& c, void* workspace, hipStream_t s);

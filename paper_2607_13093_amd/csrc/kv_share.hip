@@ -25,26 +25,32 @@ constexpr int kShareLeast = 256;  // and at least
 // Tokens whose reading a segment has to save: a part of every row costs about as much.
 constexpr int kShareWorth = 256;
 
-// An item: the rows of `members` sessions from place `first` of the order, tile
-// `tile` of them, over tokens from ... to - 1 of their pages.
+// Tokens from ... to - 1 of `members` sessions from place `first` of the order.
+struct ShareSeg {
+  int32_t first, members, from, to;
+};
+
+// An item: tile `tile` of the rows of such sessions over such tokens, place `part` of
+// each row's parts; alone: no other tile reads them; own: of one session.
 struct ShareItem {
-  int32_t first, members, tile, from, to, part, alone, pad;
+  int32_t first, members, tile, from, to, part, alone, own;
 };
 
 struct ShareHead {
-  uint32_t key;      // of the sizes that the plan is for
-  int32_t items[2];  // on shared segments, on sessions' own
-  int32_t pad[5];
+  uint32_t key;   // of the sizes that the plan is for
+  int32_t items;
+  int32_t next;   // the next item that a workgroup takes, zero between calls
+  int32_t shared; // segments that several sessions hold
 };
 
 // Sizes of a plan, from a call's.
 struct ShareSizes {
   int levels, parts;  // segments of a path that are shared at most, parts of a row
   int extra;          // parts beyond one for each segment of a path
-  int rows[2];        // of a tile
-  int slots[2];       // workgroups that run at a time
-  int64_t cap[2];     // items at most
-  int mt[2], wt[2];
+  int mt[2], wt;      // row tiles of a wave on shared segments and on own ones, waves that share them
+  int rows[2];        // of a tile of an item
+  int slots;          // workgroups that run at a time
+  int cap;            // items at most
 };
 
 struct SharePlanArgs {
@@ -55,8 +61,8 @@ struct SharePlanArgs {
   ShareHead* head;
   int32_t* order;    // [S]: sessions, those of a segment side by side
   int32_t* parts;    // [S]: parts of a session's rows
-  ShareItem* segs;   // [(levels + 1) S]: scratch; tile holds the segment's tiles, part its first
-  ShareItem* items[2];
+  ShareSeg* segs;    // [(levels + 1) S], scratch
+  ShareItem* items;  // [cap]
 };
 
 constexpr int kPlanThreads = 1024;
@@ -85,8 +91,25 @@ __device__ __forceinline__ int sum_before(int x, int* all) {
   return before + y - x;
 }
 
-// Keys in ascending order, n a power of two.
+// Keys in ascending order, no two alike, n a power of two.  Up to 256 each is counted
+// into its place by four threads, one step; more are merged in log2(n)^2 / 2.
 __device__ __forceinline__ void sort_keys(uint64_t* key, int n) {
+  __syncthreads();
+  if (n <= kPlanThreads / 4) {
+    const int i = threadIdx.x >> 2, quarter = threadIdx.x & 3;
+    const uint64_t mine = i < n ? key[i] : 0;
+    int below = 0;
+    if (i < n) {
+#pragma unroll 8
+      for (int k = quarter; k < n; k += 4) below += key[k] < mine;
+    }
+    below += __shfl_xor(below, 1, 64);
+    below += __shfl_xor(below, 2, 64);
+    __syncthreads();
+    if (i < n && quarter == 0) key[below] = mine;
+    __syncthreads();
+    return;
+  }
   for (int size = 2; size <= n; size <<= 1)
     for (int gap = size >> 1; gap > 0; gap >>= 1) {
       __syncthreads();
@@ -102,39 +125,60 @@ __device__ __forceinline__ void sort_keys(uint64_t* key, int n) {
   __syncthreads();
 }
 
+constexpr int plan_lds(int n2) { return 38 * n2 + 16; }
+
+// (40 us of a step for 256 sessions of which each wrote its own items; 1024 threads for the
+// comparing of tables, which is bound by the latency of its loads)
 __global__ __launch_bounds__(kPlanThreads) void k_share_plan(SharePlanArgs a, int n2) {
   extern __shared__ __align__(16) uint8_t smem[];
   uint64_t* key = reinterpret_cast<uint64_t*>(smem);           // [n2] by place: group, page, session
   int32_t* limit = reinterpret_cast<int32_t*>(key + n2);       // [n2] by session: pages that may be shared
-  int32_t* depth = limit + n2;                                 // by place: pages shared so far
-  int32_t* group = depth + n2;                                 // by place
-  int32_t* first = group + n2;                                 // [n2 + 1] by group: its first place
-  int32_t* alike = first + n2 + 1;                             // by group: pages named alike
+  int32_t* slot = limit + n2;                                  // by session: its row of the table
+  int32_t* base = slot + n2;                                   // by session: position of its first row
+  int32_t* depth = base + n2;                                  // by place: pages shared so far
+  int32_t* alike = depth + n2;                                 // by group: pages named alike
   int32_t* low = alike + n2;                                   // by group: least position of a first row
-  int32_t* count = low + n2;                                   // by place: parts so far
-  __shared__ int s_segs, s_chunk[16];
+  uint16_t* count = reinterpret_cast<uint16_t*>(low + n2);     // by place: parts so far
+  uint16_t* group = count + n2;                                // by place
+  uint16_t* first = group + n2;                                // [n2 + 1] by group: its first place
+  __shared__ int s_segs, s_longest, s_chunk[16];
   const int S = a.kv.n_sessions, shift = a.kv.page_shift, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  auto table_of = [&](int s) { return kv_session(a.kv, s).table; };
+  auto row_of = [&](int at) { return a.kv.table + (int64_t)slot[(int)(key[at] & 4095)] * a.kv.ld_table; };
 
+  if (threadIdx.x == 0) s_segs = s_longest = 0;
+  __syncthreads();
+  int longest = 0;
   for (int s = threadIdx.x; s < n2; s += kPlanThreads) {
-    int n = 0;
+    int n = 0, at = 0, b = 0;
     if (s < S) {
       const KvSession ses = kv_session(a.kv, s);
-      n = ses.len > ses.rows ? ses.len - ses.rows : 0;  // all its rows see those
+      at = (int)((ses.table - a.kv.table) / a.kv.ld_table);
+      b = ses.len - ses.rows;
+      n = b > 0 ? b : 0;  // all its rows see those
+      longest = ses.len > longest ? ses.len : longest;
     }
     limit[s] = n >> shift;
-    depth[s] = group[s] = count[s] = 0;
+    slot[s] = at;
+    base[s] = b;
+    depth[s] = count[s] = 0;
+    group[s] = 0;
     key[s] = s < S ? (uint64_t)s : ~uint64_t(0);
   }
-  if (threadIdx.x == 0) s_segs = 0;
+  if (longest > 0) atomicMax(&s_longest, longest);
   __syncthreads();
+  longest = s_longest;
 
   int groups = 1, ends[kShareLevels + 1];  // segments up to each level
-  ends[0] = 0;
-  for (int level = 0; level < a.z.levels; ++level) {
+#pragma unroll
+  for (int k = 0; k <= kShareLevels; ++k) ends[k] = 0;
+  bool more = S > 1;
+#pragma unroll
+  for (int level = 0; level < kShareLevels; ++level) {
+    ends[level + 1] = ends[level];
+    if (!more || level >= a.z.levels) continue;
     for (int at = threadIdx.x; at < S; at += kPlanThreads) {
       const int s = (int)(key[at] & 4095), d = depth[at];
-      const int page = d < limit[s] ? table_of(s)[d] : -1;
+      const int page = d < limit[s] ? row_of(at)[d] : -1;
       const bool valid = (unsigned)page < (unsigned)a.kv.n_pages;
       key[at] = (uint64_t)group[at] << 44 | (valid ? (uint64_t)page << 12 : uint64_t(1) << 43 | (uint64_t)s << 12) | (uint64_t)s;
     }
@@ -144,45 +188,64 @@ __global__ __launch_bounds__(kPlanThreads) void k_share_plan(SharePlanArgs a, in
     int starts = 0;
     for (int i = mine; i < mine + each && i < S; ++i) starts += i == 0 || key[i] >> 12 != key[i - 1] >> 12;
     int id = sum_before(starts, &groups);
+    if (groups == S) {  // no two alike
+      more = false;
+      continue;
+    }
     for (int i = mine; i < mine + each && i < S; ++i) {
-      if (i == 0 || key[i] >> 12 != key[i - 1] >> 12) first[id++] = i;
-      group[i] = id - 1;
+      if (i == 0 || key[i] >> 12 != key[i - 1] >> 12) first[id++] = (uint16_t)i;
+      group[i] = (uint16_t)(id - 1);
     }
-    if (threadIdx.x == 0) first[groups] = S;
-    for (int g = threadIdx.x; g < groups; g += kPlanThreads) {
-      alike[g] = kKvMost;
-      low[g] = kKvMost;
-    }
+    if (threadIdx.x == 0) first[groups] = (uint16_t)S;
+    for (int g = threadIdx.x; g < groups; g += kPlanThreads) alike[g] = low[g] = kKvMost;
     __syncthreads();
     for (int at = threadIdx.x; at < S; at += kPlanThreads) {
       const int s = (int)(key[at] & 4095);
       atomicMin(&alike[group[at]], limit[s]);
-      if (a.window > 0) {
-        const KvSession ses = kv_session(a.kv, s);
-        atomicMin(&low[group[at]], ses.len - ses.rows);
-      }
+      if (a.window > 0) atomicMin(&low[group[at]], base[s]);
     }
     __syncthreads();
-    // pages named alike by a group's first session and each of the others
-    for (int at = wave; at < S; at += 16) {
-      const int g = group[at], lead = first[g];
-      if (at == lead) continue;
-      const int32_t *x = table_of((int)(key[lead] & 4095)), *y = table_of((int)(key[at] & 4095));
-      for (int c = depth[at] + 1; c < *(volatile int32_t*)&alike[g]; c += 256) {
-        int32_t p[4], q[4];
+    // Pages named alike by a group's first session and each of the others: a wave takes
+    // four others at a time, so that their loads are on their way together.
+    for (int at0 = wave; at0 < S; at0 += 64) {
+      const int32_t *x[4], *y[4];
+      int g[4], c = kKvMost;
+      uint32_t open = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int at_c = c + i * 64 + lane < a.kv.max_pages ? c + i * 64 + lane : a.kv.max_pages - 1;
-          p[i] = x[at_c];
-          q[i] = y[at_c];
+      for (int m = 0; m < 4; ++m) {
+        const int at = at0 + 16 * m < S ? at0 + 16 * m : at0;
+        g[m] = group[at];
+        x[m] = row_of(first[g[m]]);
+        y[m] = row_of(at);
+        if (at0 + 16 * m < S && at != first[g[m]]) {
+          open |= 1u << m;
+          c = depth[at] + 1 < c ? depth[at] + 1 : c;
         }
-        int differs = kKvMost;
+      }
+      while (open) {
+        int32_t p[4][4], q[4][4];
 #pragma unroll
-        for (int i = 3; i >= 0; --i)
-          if (p[i] != q[i]) differs = c + i * 64 + lane;
-        const bool any = __any(differs != kKvMost);
-        if (differs != kKvMost) atomicMin(&alike[g], differs);
-        if (any) break;
+        for (int m = 0; m < 4; ++m) {
+          if (!(open >> m & 1)) continue;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int col = c + i * 64 + lane < a.kv.max_pages ? c + i * 64 + lane : a.kv.max_pages - 1;
+            p[m][i] = x[m][col];
+            q[m][i] = y[m][col];
+          }
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          if (!(open >> m & 1)) continue;
+          int differs = kKvMost;
+#pragma unroll
+          for (int i = 3; i >= 0; --i)
+            if (p[m][i] != q[m][i]) differs = c + i * 64 + lane;
+          const bool any = __any(differs != kKvMost);
+          if (differs != kKvMost) atomicMin(&alike[g[m]], differs);
+          if (any || c + 256 >= *(volatile int32_t*)&alike[g[m]]) open &= ~(1u << m);
+        }
+        c += 256;
       }
     }
     __syncthreads();
@@ -207,11 +270,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_share_plan(SharePlanArgs a, in
           const int64_t lowest = (int64_t)low[g] - a.window + 1;
           if (lowest > seen) seen = lowest < to ? (int)lowest & ~(kKvBlock - 1) : to;
         }
-        ShareItem& t = a.segs[before + made + at];
-        t.first = first[g];
-        t.members = members;
-        t.from = seen;
-        t.to = to;
+        a.segs[before + made + at] = ShareSeg{first[g], members, seen, to};
       }
       if (g < groups) low[g] = take;
       made += all;
@@ -224,52 +283,48 @@ __global__ __launch_bounds__(kPlanThreads) void k_share_plan(SharePlanArgs a, in
     }
     if (threadIdx.x == 0) s_segs = before + made;
     ends[level + 1] = before + made;
+    more = made > 0;
     __syncthreads();
-    if (made == 0) {
-      for (int k = level + 1; k < kShareLevels; ++k) ends[k + 1] = before;
-      break;
-    }
   }
-  const int shared = s_segs;
-  __syncthreads();
-  for (int k = a.z.levels; k < kShareLevels; ++k) ends[k + 1] = shared;
-  // what sessions hold alone
-  int longest = 0;
+  const int shared = ends[kShareLevels];
+  // What sessions hold alone, the longest first.
+  const int own_n2 = n2;
   for (int at = threadIdx.x; at < S; at += kPlanThreads) {
     const int s = (int)(key[at] & 4095);
-    const KvSession ses = kv_session(a.kv, s);
+    const int rows = a.kv.rows ? a.kv.rows[s] : a.kv.R;
+    const int len = base[s] + (rows < 0 ? 0 : rows > a.kv.R ? a.kv.R : rows);
     int from = depth[at] << shift;
     if (a.window > 0) {
-      const int64_t lowest = (int64_t)ses.len - ses.rows - a.window + 1;
+      const int64_t lowest = (int64_t)base[s] - a.window + 1;
       if (lowest > from) from = (int)lowest & ~(kKvBlock - 1);
     }
-    ShareItem& t = a.segs[shared + at];
-    t.first = at;
-    t.members = 1;
-    t.from = from;
-    t.to = ses.len > from ? ses.len : from;
-    a.order[at] = s;
-    if (ses.len > longest) longest = ses.len;
+    alike[at] = from;
+    low[at] = len > from ? len : from;
+    a.order[at] = limit[at] = s;
   }
-  if (threadIdx.x == 0) s_segs = 0;
   __syncthreads();
-  atomicMax(&s_segs, longest);
+  for (int at = threadIdx.x; at < own_n2; at += kPlanThreads)
+    key[at] = at < S ? (uint64_t)(uint32_t)(kKvMost - (low[at] - alike[at])) << 12 | (uint64_t)at : ~uint64_t(0);
+  sort_keys(key, own_n2);
+  for (int i = threadIdx.x; i < S; i += kPlanThreads) {
+    const int at = (int)(key[i] & 4095);
+    a.segs[shared + i] = ShareSeg{at, 1, alike[at], low[at]};
+  }
   __syncthreads();
-  longest = s_segs;
 
-  // Shares: of each kind, the shortest that fill the device about once.
+  // Shares, of each kind the shortest that fill the device about once: eight waves
+  // sum up a kind's items for a candidate each.
   const int RG = a.kv.R * a.group;
-  int chunk[2];
-#pragma unroll
-  for (int kind = 0; kind < 2; ++kind) {
-    const ShareItem* segs = a.segs + (kind ? shared : 0);
+  {
+    const int kind = wave >> 3, candidate = wave & 7;
+    const ShareSeg* segs = a.segs + (kind ? shared : 0);
     const int n = kind ? S : shared, rows = a.z.rows[kind];
-    // (every wave sums them up for a candidate of its own)
     int64_t load = 0, tiles = 0;
     for (int i = lane; i < n; i += 64) {
-      const int64_t t = ((int64_t)segs[i].members * RG + rows - 1) / rows;
-      tiles += t;
-      load += t * (segs[i].to - segs[i].from);
+      const ShareSeg t = segs[i];
+      const int64_t k = ((int64_t)t.members * RG + rows - 1) / rows;
+      tiles += k;
+      load += k * (t.to - t.from);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
@@ -278,30 +333,33 @@ __global__ __launch_bounds__(kPlanThreads) void k_share_plan(SharePlanArgs a, in
     }
     load *= a.kv.heads;
     tiles *= a.kv.heads;
-    const int64_t slots = a.z.slots[kind];
+    const int64_t slots = a.z.slots;
     const bool few = tiles < 2 * slots;
     const int64_t target = 2 * tiles <= slots ? slots : 2 * slots;
-    int64_t c = few ? load * (8 + wave) / (8 * target) : load / slots;
+    int64_t c = few ? load * (8 + 2 * candidate) / (8 * target) : load / slots;
     const int64_t room = a.z.extra > 0 ? (longest + a.z.extra - 1) / a.z.extra : longest;
-    if (wave == 15 && few) c = longest;
+    const bool last = !few || candidate == 7;
+    if (few && last) c = longest;
     if (c < room) c = room;
     if (c < kShareLeast) c = kShareLeast;
     c = (c + kShareStep - 1) / kShareStep * kShareStep;
     int64_t items = 0;
-    for (int i = lane; i < n; i += 64)
-      items += ((int64_t)segs[i].members * RG + rows - 1) / rows * ((segs[i].to - segs[i].from + c - 1) / c);
+    for (int i = lane; i < n; i += 64) {
+      const ShareSeg t = segs[i];
+      items += ((int64_t)t.members * RG + rows - 1) / rows * ((t.to - t.from + c - 1) / c);
+    }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) items += __shfl_xor(items, o, 64);
-    if (lane == 0) s_chunk[wave] = !few || wave == 15 || items * a.kv.heads <= target ? (int)c : INT32_MAX;
-    __syncthreads();
-    chunk[kind] = INT32_MAX;
-#pragma unroll
-    for (int k = 0; k < 16; ++k) chunk[kind] = s_chunk[k] < chunk[kind] ? s_chunk[k] : chunk[kind];
-    __syncthreads();
+    if (lane == 0) s_chunk[wave] = last || items * a.kv.heads <= target ? (int)c : INT32_MAX;
   }
+  __syncthreads();
+  int chunk[2] = {INT32_MAX, INT32_MAX};
+#pragma unroll
+  for (int k = 0; k < 16; ++k) chunk[k >> 3] = s_chunk[k] < chunk[k >> 3] ? s_chunk[k] : chunk[k >> 3];
 
-  // Parts of each segment, level by level along the paths, and the items.
-  int made[2] = {0, 0};
+  // Parts of each segment, level by level along the paths, and the items: those of a
+  // segment by a wave.
+  int made = 0;
 #pragma unroll
   for (int level = 0; level <= kShareLevels; ++level) {
     const int kind = level == kShareLevels;
@@ -309,32 +367,32 @@ __global__ __launch_bounds__(kPlanThreads) void k_share_plan(SharePlanArgs a, in
     const int c = chunk[kind], rows = a.z.rows[kind];
     for (int i0 = lo; i0 < hi; i0 += kPlanThreads) {
       const int i = i0 + threadIdx.x;
-      int tiles = 0, shares = 0;
-      ShareItem t{};
-      if (i < hi) {
-        t = a.segs[i];
-        tiles = (int)(((int64_t)t.members * RG + rows - 1) / rows);
-        shares = (t.to - t.from + c - 1) / c;
-      }
+      ShareSeg t{0, 0, 0, 0};
+      if (i < hi) t = a.segs[i];
+      const int tiles = (int)(((int64_t)t.members * RG + rows - 1) / rows), shares = (t.to - t.from + c - 1) / c;
       int all = 0;
-      const int at = made[kind] + sum_before(tiles * shares, &all);
-      if (i < hi) {
-        const int part = count[t.first];
-        for (int k = 0; k < shares; ++k)
-          for (int x = 0; x < tiles; ++x) {
-            const int64_t to = (int64_t)t.from + (int64_t)(k + 1) * c;
-            const ShareItem it{t.first, t.members, x, t.from + k * c, to < t.to ? (int)to : t.to, part + k, tiles == 1, 0};
-            if (at + k * tiles + x < a.z.cap[kind]) a.items[kind][at + k * tiles + x] = it;
-          }
-        for (int m = 0; m < t.members; ++m) count[t.first + m] = part + shares;
+      const int before = made + sum_before(i < hi ? tiles * shares : 0, &all);
+      const int n = hi - i0 - wave * 64 < 64 ? hi - i0 - wave * 64 : 64;
+      for (int k = 0; k < n; ++k) {
+        const ShareSeg u{__builtin_amdgcn_readlane(t.first, k), __builtin_amdgcn_readlane(t.members, k),
+                         __builtin_amdgcn_readlane(t.from, k), __builtin_amdgcn_readlane(t.to, k)};
+        const int at = __builtin_amdgcn_readlane(before, k), nt = __builtin_amdgcn_readlane(tiles, k);
+        const int ns = __builtin_amdgcn_readlane(shares, k), part = count[u.first];
+        for (int x = lane; x < nt * ns; x += 64) {
+          const int share = x / nt, tile = x - share * nt;
+          const int64_t to = (int64_t)u.from + (int64_t)(share + 1) * c;
+          if (at + x < a.z.cap)
+            a.items[at + x] = ShareItem{u.first, u.members, tile, u.from + share * c, to < u.to ? (int)to : u.to,
+                                        part + share, nt == 1, kind};
+        }
+        for (int m = lane; m < u.members; m += 64) count[u.first + m] = (uint16_t)(part + ns);
       }
-      made[kind] += all;
+      made += all;
       __syncthreads();
     }
   }
-  for (int at = threadIdx.x; at < S; at += kPlanThreads) a.parts[(int)(key[at] & 4095)] = count[at];
-  if (threadIdx.x < 2) a.head->items[threadIdx.x] = made[threadIdx.x];
-  if (threadIdx.x == 0) a.head->key = a.key;
+  for (int at = threadIdx.x; at < S; at += kPlanThreads) a.parts[limit[at]] = count[at];
+  if (threadIdx.x == 0) *a.head = ShareHead{a.key, made, 0, shared};
 }
 
 struct ShareArgs {
@@ -348,11 +406,10 @@ struct ShareArgs {
   float scale_log2, binade;
   bool q_aligned, o_aligned;
   uint32_t key;
-  const ShareHead* head;
+  ShareHead* head;
   const int32_t* order;
   const int32_t* n_parts;
   const ShareItem* items;
-  int kind;
   int cap;
   int parts;        // places of a row
   float2* part_ml;  // [rows x heads][parts]: reference of the weights, their sum
@@ -377,8 +434,9 @@ __device__ __forceinline__ ShareRow share_row(const ShareArgs& a, const ShareIte
   return w;
 }
 
+// The parts of an item's rows for one key/value head.
 template <int D, int MT, int WT>
-__global__ __launch_bounds__(64 * waves_in(WT), waves_of(D, MT, WT)) void k_share_part(ShareArgs a) {
+__device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& it, int head, uint8_t* smem) {
   constexpr int NS = stages_of(D, WT);
   constexpr int NW = waves_in(WT);
   constexpr int WR = NW / WT;
@@ -388,17 +446,8 @@ __global__ __launch_bounds__(64 * waves_in(WT), waves_of(D, MT, WT)) void k_shar
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int wt = wave % WT, wr = wave / WT;
-  extern __shared__ __align__(16) uint8_t smem[];  // rings, then queries of each group of rows
   const int G = a.group, RG = a.kv.R * G;
-  if (a.head->key != a.key) return;
-  const int n_items = a.head->items[a.kind] < a.cap ? a.head->items[a.kind] : a.cap;
-  const int64_t n_blocks = (int64_t)n_items * a.kv.heads;
-
-  for (int64_t block = blockIdx.x; block < n_blocks; block += gridDim.x) {
-    if (block != blockIdx.x) __syncthreads();  // the outputs in LDS are read
-    const int head = (int)(block % a.kv.heads);
-    const auto* x8 = (const __attribute__((address_space(4))) int32_t*)(a.items + block / a.kv.heads);
-    const ShareItem it{x8[0], x8[1], x8[2], x8[3], x8[4], x8[5], x8[6], 0};
+  {
     const int lead = (unsigned)it.first < (unsigned)a.kv.n_sessions ? a.order[it.first] : 0;
     const KvSession ses = kv_session(a.kv, (unsigned)lead < (unsigned)a.kv.n_sessions ? lead : 0);
     const int row0 = (it.tile * WR + wr) * 16 * MT;  // the wave's first
@@ -612,12 +661,47 @@ __global__ __launch_bounds__(64 * waves_in(WT), waves_of(D, MT, WT)) void k_shar
   }
 }
 
+constexpr int share_lds(int d, int mt, int own_mt, int wt) {
+  return attend_lds(d, mt, wt) > attend_lds(d, own_mt, wt) ? attend_lds(d, mt, wt) : attend_lds(d, own_mt, wt);
+}
+constexpr int share_waves(int d, int mt, int wt) { return waves_of(d, mt, wt) < 2 ? waves_of(d, mt, wt) : 2; }
+constexpr int share_resident(int d, int mt, int own_mt, int wt) {  // workgroups of a CU
+  const int by_lds = 160 * 1024 / share_lds(d, mt, own_mt, wt), by_waves = share_waves(d, mt, wt) * 4 / waves_in(wt);
+  return by_lds < by_waves ? by_lds : by_waves;
+}
+
+// Workgroups take an item and head at a time, in the order of the list: the shared
+// segments' first, bound by the matrix cores and the softmax, beside which the sessions'
+// own tokens come from memory, the longest first.  MT, OWN: row tiles of a wave on
+// either.
+template <int D, int MT, int OWN, int WT>
+__global__ __launch_bounds__(64 * waves_in(WT), share_waves(D, MT, WT)) void k_share_parts(ShareArgs a) {
+  extern __shared__ __align__(16) uint8_t smem[];  // rings, then queries of each group of rows
+  __shared__ int s_next;
+  if (a.head->key != a.key) return;
+  const int items = a.head->items < a.cap ? a.head->items : a.cap;
+  const int units = items * a.kv.heads;
+  int unit = blockIdx.x;
+  while (unit < units) {
+    if (threadIdx.x == 0) s_next = gridDim.x + atomicAdd(&a.head->next, 1);
+    const int head = unit % a.kv.heads;
+    const auto* x8 = (const __attribute__((address_space(4))) int32_t*)(a.items + unit / a.kv.heads);
+    const ShareItem it{x8[0], x8[1], x8[2], x8[3], x8[4], x8[5], x8[6], x8[7]};
+    if (OWN == MT || !it.own) share_item<D, MT, WT>(a, it, head, smem);
+    else share_item<D, OWN, WT>(a, it, head, smem);
+    __syncthreads();  // the outputs in LDS are read, the next unit is known
+    unit = __builtin_amdgcn_readfirstlane(s_next);
+    __syncthreads();
+  }
+}
+
 // A row's parts joined, in their order; D/4 lanes a row and head.
 template <int D>
 __global__ __launch_bounds__(256) void k_share_join(ShareArgs a, int64_t rows) {
   constexpr int LPS = D / 4;
   const int d4 = threadIdx.x % LPS;
   const int64_t i = (int64_t)blockIdx.x * (256 / LPS) + threadIdx.x / LPS;
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.head->next = 0;  // for the next call
   if (i >= rows) return;
   const int heads = a.kv.heads * a.group;
   const int64_t row = i / heads;
@@ -677,9 +761,8 @@ ShareSizes share_sizes(int d, int64_t S, int64_t R, int64_t heads, int64_t group
   const int64_t RG = R * group;
   // Shared segments: as many rows a tile as the registers hold; own ones: as many as there are.
   z.mt[0] = d == 256 ? 2 : 4;
-  z.wt[0] = d == 256 ? 8 : 4;
+  z.wt = d == 256 ? 8 : 4;
   z.mt[1] = RG <= 16 ? 1 : d == 256 || RG <= 32 ? 2 : 4;
-  z.wt[1] = d == 256 && z.mt[1] == 2 ? 8 : 4;
   if (S * RG > 65536) {  // prompts: nothing to cut
     z.levels = 1;
     z.extra = 0;
@@ -690,14 +773,11 @@ ShareSizes share_sizes(int d, int64_t S, int64_t R, int64_t heads, int64_t group
     if (z.extra > shares) z.extra = (int)shares;
   }
   z.parts = z.levels + 1 + z.extra;
-  for (int k = 0; k < 2; ++k) {
-    z.rows[k] = 16 * z.mt[k] * (waves_in(z.wt[k]) / z.wt[k]);
-    z.slots[k] = kCUs * resident(d, z.mt[k], z.wt[k]);
-  }
+  for (int k = 0; k < 2; ++k) z.rows[k] = 16 * z.mt[k];
+  z.slots = kCUs * (d == 64 ? share_resident(64, 4, 4, 4) : d == 128 ? share_resident(128, 4, 4, 4) : share_resident(256, 2, 2, 8));
   // A level's segments have a tile more each than their rows fill, and shares.
   const int64_t wide = (S * RG + z.rows[0] - 1) / z.rows[0] + S / 2 + 1, own = S * ((RG + z.rows[1] - 1) / z.rows[1]);
-  z.cap[0] = z.levels * wide * (1 + z.extra);
-  z.cap[1] = own * (1 + z.extra);
+  z.cap = (int)((z.levels * wide + own) * (1 + z.extra));
   return z;
 }
 
@@ -711,7 +791,7 @@ uint32_t share_key(int d, const KvArgs& a, int group, int window, int extra) {
 }
 
 struct SharePlaces {
-  size_t order, parts, segs, items[2], all;
+  size_t order, parts, segs, items, all;
 };
 SharePlaces share_places(const ShareSizes& z, int64_t S) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
@@ -719,31 +799,30 @@ SharePlaces share_places(const ShareSizes& z, int64_t S) {
   p.order = up(sizeof(ShareHead));
   p.parts = p.order + up(S * 4);
   p.segs = p.parts + up(S * 4);
-  p.items[0] = p.segs + up((z.levels + 1) * S * sizeof(ShareItem));
-  p.items[1] = p.items[0] + up(z.cap[0] * sizeof(ShareItem));
-  p.all = p.items[1] + up(z.cap[1] * sizeof(ShareItem));
+  p.items = p.segs + up((z.levels + 1) * S * sizeof(ShareSeg));
+  p.all = p.items + up(z.cap * sizeof(ShareItem));
   return p;
 }
 
-template <int D, int MT, int WT>
-hipError_t launch_part(const ShareArgs& a, int64_t slots, hipStream_t s) {
-  constexpr size_t lds = attend_lds(D, MT, WT);
+template <int D, int MT, int OWN, int WT>
+hipError_t launch_parts(const ShareArgs& a, int slots, hipStream_t s) {
+  constexpr size_t lds = share_lds(D, MT, OWN, WT);
   static std::atomic<uint64_t> done{0};
-  const hipError_t e = set_lds_limit_once(done, reinterpret_cast<const void*>(k_share_part<D, MT, WT>), lds);
+  const hipError_t e = set_lds_limit_once(done, reinterpret_cast<const void*>(k_share_parts<D, MT, OWN, WT>), lds);
   if (e != hipSuccess) return e;
   const int64_t most = (int64_t)a.cap * a.kv.heads;
-  launch_kernel(k_share_part<D, MT, WT>, dim3((unsigned)(most < slots ? most : slots)), dim3(64 * waves_in(WT)), (uint32_t)lds, s, a);
+  launch_kernel(k_share_parts<D, MT, OWN, WT>, dim3((unsigned)(most < slots ? most : slots)), dim3(64 * waves_in(WT)),
+                (uint32_t)lds, s, a);
   return hipGetLastError();
 }
 
 template <int D>
-hipError_t launch_parts(int mt, const ShareArgs& a, int64_t slots, hipStream_t s) {
-  if (mt == 1) return launch_part<D, 1, 4>(a, slots, s);
-  if constexpr (D == 256) {
-    return launch_part<D, 2, 8>(a, slots, s);
-  } else {
-    return mt == 2 ? launch_part<D, 2, 4>(a, slots, s) : launch_part<D, 4, 4>(a, slots, s);
-  }
+hipError_t launch_own(int own, const ShareArgs& a, int slots, hipStream_t s) {
+  if constexpr (D == 256) return own == 1 ? launch_parts<D, 2, 1, 8>(a, slots, s) : launch_parts<D, 2, 2, 8>(a, slots, s);
+  else
+    return own == 1 ? launch_parts<D, 4, 1, 4>(a, slots, s)
+           : own == 2 ? launch_parts<D, 4, 2, 4>(a, slots, s)
+                      : launch_parts<D, 4, 4, 4>(a, slots, s);
 }
 
 }  // namespace
@@ -774,18 +853,18 @@ hipError_t launch_share_plan(int d, const KvArgs& kv, int q_heads, int window, i
   a.head = reinterpret_cast<ShareHead*>(base);
   a.order = reinterpret_cast<int32_t*>(base + p.order);
   a.parts = reinterpret_cast<int32_t*>(base + p.parts);
-  a.segs = reinterpret_cast<ShareItem*>(base + p.segs);
-  for (int k = 0; k < 2; ++k) a.items[k] = reinterpret_cast<ShareItem*>(base + p.items[k]);
+  a.segs = reinterpret_cast<ShareSeg*>(base + p.segs);
+  a.items = reinterpret_cast<ShareItem*>(base + p.items);
   int n2 = 2;
   while (n2 < kv.n_sessions) n2 *= 2;
   static std::atomic<uint64_t> done{0};
-  const hipError_t e = set_lds_limit_once(done, reinterpret_cast<const void*>(k_share_plan), kShareSessions * 36 + 16);
+  const hipError_t e = set_lds_limit_once(done, reinterpret_cast<const void*>(k_share_plan), plan_lds(kShareSessions));
   if (e != hipSuccess) return e;
-  launch_kernel(k_share_plan, dim3(1), dim3(kPlanThreads), (uint32_t)(n2 * 36 + 16), s, a, n2);
+  launch_kernel(k_share_plan, dim3(1), dim3(kPlanThreads), (uint32_t)plan_lds(n2), s, a, n2);
   return hipGetLastError();
 }
 
-hipError_t launch_attend_shared(int d, const KvArgs& kv, const AttendCall& c, const void* plan, void* workspace, hipStream_t s) {
+hipError_t launch_attend_shared(int d, const KvArgs& kv, const AttendCall& c, void* plan, void* workspace, hipStream_t s) {
   ShareArgs a{};
   a.kv = kv;
   a.q = static_cast<const uint16_t*>(c.q);
@@ -803,25 +882,21 @@ hipError_t launch_attend_shared(int d, const KvArgs& kv, const AttendCall& c, co
   a.o_aligned = c.o_row % 2 == 0 && c.o_head % 2 == 0 && (reinterpret_cast<uintptr_t>(c.out) & 3) == 0;
   const ShareSizes z = share_sizes(d, kv.n_sessions, kv.R, kv.heads, a.group, c.max_len);
   const SharePlaces p = share_places(z, kv.n_sessions);
-  const uint8_t* base = static_cast<const uint8_t*>(plan);
+  uint8_t* base = static_cast<uint8_t*>(plan);
   a.key = share_key(d, kv, a.group, c.window, z.extra);
-  a.head = reinterpret_cast<const ShareHead*>(base);
+  a.head = reinterpret_cast<ShareHead*>(base);
   a.order = reinterpret_cast<const int32_t*>(base + p.order);
   a.n_parts = reinterpret_cast<const int32_t*>(base + p.parts);
   a.parts = z.parts;
   const int64_t rows = (int64_t)kv.n_sessions * kv.R * c.q_heads;
   a.part_ml = static_cast<float2*>(workspace);
   a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + ((size_t)rows * z.parts * 8 + 255) / 256 * 256);
-  for (int k = 0; k < 2; ++k) {
-    if (k == 0 && kv.n_sessions == 1) continue;
-    a.kind = k;
-    a.cap = (int)z.cap[k];
-    a.items = reinterpret_cast<const ShareItem*>(base + p.items[k]);
-    const hipError_t e = d == 64    ? launch_parts<64>(z.mt[k], a, z.slots[k], s)
-                         : d == 128 ? launch_parts<128>(z.mt[k], a, z.slots[k], s)
-                                    : launch_parts<256>(z.mt[k], a, z.slots[k], s);
-    if (e != hipSuccess) return e;
-  }
+  a.cap = z.cap;
+  a.items = reinterpret_cast<const ShareItem*>(base + p.items);
+  const hipError_t e = d == 64    ? launch_own<64>(z.mt[1], a, z.slots, s)
+                       : d == 128 ? launch_own<128>(z.mt[1], a, z.slots, s)
+                                  : launch_own<256>(z.mt[1], a, z.slots, s);
+  if (e != hipSuccess) return e;
   const int64_t per = 256 / (d / 4);
   const dim3 grid((unsigned)((rows + per - 1) / per));
   if (d == 64) launch_kernel(k_share_join<64>, grid, dim3(256), 0, s, a, rows);

@@ -1193,7 +1193,7 @@ size_t sph_kv_attend_shared_workspace(const sph_kv_cache* cache, int64_t q_heads
 int sph_kv_attend_shared(const sph_kv_cache* cache, int64_t layer, const void* q, int64_t q_row,
                          int64_t q_head, int64_t q_heads, int64_t n_sessions, int64_t R,
                          const int32_t* rows, const int32_t* slots, float scale, int64_t window,
-                         int64_t max_len, const void* plan, size_t plan_bytes, void* out,
+                         int64_t max_len, void* plan, size_t plan_bytes, void* out,
                          int64_t o_row, int64_t o_head, float* lse_out, void* workspace,
                          size_t ws_bytes, void* stream) {
   const char* fn = "sph_kv_attend_shared";
