@@ -480,7 +480,7 @@ int sph_kv_attend(const sph_kv_cache* cache, int64_t layer, const void* q, int64
  * sph_kv_attend_shared is given the same cache, q_heads, sessions, R, rows, slots,
  * window and max_len; the rest is as in sph_kv_attend.
  *
- * n_sessions <= 4096, n_sessions * R * q_heads <= 2^26
+ * n_sessions <= 2048, n_sessions * R * q_heads <= 2^26
  * max_len      as in sph_kv_attend
  * plan         device memory of sph_kv_share_bytes, 16-byte aligned.  Calls that share
  *              one must not overlap (it holds the calls' work queue).

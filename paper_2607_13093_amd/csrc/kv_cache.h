@@ -123,7 +123,7 @@ int64_t kv_window(int64_t window, int64_t most);
 void kv_attend_span(int base, int r_lo, int r_hi, int window, int split, int splits, int chunk, int span[6]);
 hipError_t launch_kv_attend(int d, const KvArgs& kv, const AttendCall& c, void* workspace, hipStream_t s);
 
-constexpr int kShareSessions = 4096;  // of a plan
+constexpr int kShareSessions = 2048;  // of a plan
 bool kv_share_fits(int64_t n_sessions, int64_t R, int64_t q_heads);
 size_t kv_share_bytes(int d, int64_t n_sessions, int64_t R, int64_t heads, int64_t q_heads, int64_t max_len);
 size_t kv_share_scratch(int d, int64_t n_sessions, int64_t R, int64_t heads, int64_t q_heads, int64_t max_len);

@@ -125,17 +125,80 @@ __device__ __forceinline__ void sort_keys(uint64_t* key, int n) {
   __syncthreads();
 }
 
-constexpr int plan_lds(int n2) { return 38 * n2 + 16; }
+// The rows of the table of a level's groups, in LDS but for the table.
+struct Alike {
+  const uint64_t* key;
+  const int32_t *slot, *depth;
+  int32_t* alike;
+  const uint16_t *group, *first;
+  const int32_t* table;
+  int64_t ld_table;
+};
 
-// (40 us of a step for 256 sessions of which each wrote its own items; 1024 threads for the
-// comparing of tables, which is bound by the latency of its loads)
-__global__ __launch_bounds__(kPlanThreads) void k_share_plan(SharePlanArgs a, int n2) {
+// Each session's row against its group's first from the place after `depth` on, up to
+// alike[group], which is lowered to the first place where they differ.  A wave takes M
+// sessions at a time, 64 COLS places of each, so that their loads are on their way together.
+template <int M, int COLS>
+__device__ __forceinline__ void compare_rows(const Alike& a, int S) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  for (int at0 = wave; at0 < S; at0 += 16 * M) {
+    const int32_t *x[M], *y[M];
+    int g[M], c = kKvMost;
+    uint32_t open = 0;
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      const int at = at0 + 16 * m < S ? at0 + 16 * m : at0;
+      g[m] = __builtin_amdgcn_readfirstlane((int)a.group[at]);
+      const int lead = __builtin_amdgcn_readfirstlane((int)a.first[g[m]]);
+      const int sx = a.slot[(int)(a.key[lead] & 4095)], sy = a.slot[(int)(a.key[at] & 4095)];
+      x[m] = a.table + __builtin_amdgcn_readfirstlane(sx) * a.ld_table;
+      y[m] = a.table + __builtin_amdgcn_readfirstlane(sy) * a.ld_table;
+      if (at0 + 16 * m < S && at != lead) {
+        const int d = __builtin_amdgcn_readfirstlane(a.depth[at]) + 1;
+        open |= 1u << m;
+        c = d < c ? d : c;
+      }
+    }
+    while (open) {
+      int32_t p[M][COLS], q[M][COLS];
+      int end[M];  // at most a row's places
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+        end[m] = open >> m & 1 ? __builtin_amdgcn_readfirstlane(*(volatile const int32_t*)&a.alike[g[m]]) : 0;
+#pragma unroll
+        for (int i = 0; i < COLS; ++i)
+          if (c + i * 64 < end[m]) {
+            const int col = c + i * 64 + lane < end[m] ? c + i * 64 + lane : end[m] - 1;
+            p[m][i] = x[m][col];
+            q[m][i] = y[m][col];
+          }
+      }
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+        int differs = kKvMost;
+#pragma unroll
+        for (int i = COLS - 1; i >= 0; --i)
+          if (c + i * 64 < end[m] && p[m][i] != q[m][i]) differs = c + i * 64 + lane;
+        const bool any = __any(differs != kKvMost);
+        if (differs != kKvMost) atomicMin(&a.alike[g[m]], differs);
+        if (any || c + COLS * 64 >= end[m]) open &= ~(1u << m);
+      }
+      c += COLS * 64;
+    }
+  }
+}
+
+constexpr int plan_lds(int n2) { return 46 * n2 + 16; }
+
+__global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a, int n2) {
   extern __shared__ __align__(16) uint8_t smem[];
   uint64_t* key = reinterpret_cast<uint64_t*>(smem);           // [n2] by place: group, page, session
   int32_t* limit = reinterpret_cast<int32_t*>(key + n2);       // [n2] by session: pages that may be shared
   int32_t* slot = limit + n2;                                  // by session: its row of the table
   int32_t* base = slot + n2;                                   // by session: position of its first row
-  int32_t* depth = base + n2;                                  // by place: pages shared so far
+  int32_t* length = base + n2;                                 // by session
+  int32_t* page0 = length + n2;                                // by session: its first page; later parts and items before a segment's
+  int32_t* depth = page0 + n2;                                 // by place: pages shared so far
   int32_t* alike = depth + n2;                                 // by group: pages named alike
   int32_t* low = alike + n2;                                   // by group: least position of a first row
   uint16_t* count = reinterpret_cast<uint16_t*>(low + n2);     // by place: parts so far
@@ -149,10 +212,13 @@ __global__ __launch_bounds__(kPlanThreads) void k_share_plan(SharePlanArgs a, in
   __syncthreads();
   int longest = 0;
   for (int s = threadIdx.x; s < n2; s += kPlanThreads) {
-    int n = 0, at = 0, b = 0;
+    int n = 0, at = 0, b = 0, p0 = -1, len = 0;
     if (s < S) {
+      const int mine = a.kv.slots ? a.kv.slots[s] : s;
+      at = (unsigned)mine < (unsigned)a.kv.n_slots ? mine : 0;
+      p0 = a.kv.table[at * a.kv.ld_table];  // (beside the lengths)
       const KvSession ses = kv_session(a.kv, s);
-      at = (int)((ses.table - a.kv.table) / a.kv.ld_table);
+      len = ses.len;
       b = ses.len - ses.rows;
       n = b > 0 ? b : 0;  // all its rows see those
       longest = ses.len > longest ? ses.len : longest;
@@ -160,6 +226,8 @@ __global__ __launch_bounds__(kPlanThreads) void k_share_plan(SharePlanArgs a, in
     limit[s] = n >> shift;
     slot[s] = at;
     base[s] = b;
+    length[s] = len;
+    page0[s] = p0;
     depth[s] = count[s] = 0;
     group[s] = 0;
     key[s] = s < S ? (uint64_t)s : ~uint64_t(0);
@@ -178,7 +246,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_share_plan(SharePlanArgs a, in
     if (!more || level >= a.z.levels) continue;
     for (int at = threadIdx.x; at < S; at += kPlanThreads) {
       const int s = (int)(key[at] & 4095), d = depth[at];
-      const int page = d < limit[s] ? row_of(at)[d] : -1;
+      const int page = d >= limit[s] ? -1 : level == 0 ? page0[s] : row_of(at)[d];
       const bool valid = (unsigned)page < (unsigned)a.kv.n_pages;
       key[at] = (uint64_t)group[at] << 44 | (valid ? (uint64_t)page << 12 : uint64_t(1) << 43 | (uint64_t)s << 12) | (uint64_t)s;
     }
@@ -205,49 +273,11 @@ __global__ __launch_bounds__(kPlanThreads) void k_share_plan(SharePlanArgs a, in
       if (a.window > 0) atomicMin(&low[group[at]], base[s]);
     }
     __syncthreads();
-    // Pages named alike by a group's first session and each of the others: a wave takes
-    // four others at a time, so that their loads are on their way together.
-    for (int at0 = wave; at0 < S; at0 += 64) {
-      const int32_t *x[4], *y[4];
-      int g[4], c = kKvMost;
-      uint32_t open = 0;
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const int at = at0 + 16 * m < S ? at0 + 16 * m : at0;
-        g[m] = group[at];
-        x[m] = row_of(first[g[m]]);
-        y[m] = row_of(at);
-        if (at0 + 16 * m < S && at != first[g[m]]) {
-          open |= 1u << m;
-          c = depth[at] + 1 < c ? depth[at] + 1 : c;
-        }
-      }
-      while (open) {
-        int32_t p[4][4], q[4][4];
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          if (!(open >> m & 1)) continue;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int col = c + i * 64 + lane < a.kv.max_pages ? c + i * 64 + lane : a.kv.max_pages - 1;
-            p[m][i] = x[m][col];
-            q[m][i] = y[m][col];
-          }
-        }
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          if (!(open >> m & 1)) continue;
-          int differs = kKvMost;
-#pragma unroll
-          for (int i = 3; i >= 0; --i)
-            if (p[m][i] != q[m][i]) differs = c + i * 64 + lane;
-          const bool any = __any(differs != kKvMost);
-          if (differs != kKvMost) atomicMin(&alike[g[m]], differs);
-          if (any || c + 256 >= *(volatile int32_t*)&alike[g[m]]) open &= ~(1u << m);
-        }
-        c += 256;
-      }
-    }
+    // pages named alike by a group's first session and each of the others
+    const Alike all{key, slot, depth, alike, group, first, a.kv.table, a.kv.ld_table};
+    if (S <= 16) compare_rows<1, 16>(all, S);
+    else if (S <= 64) compare_rows<4, 4>(all, S);
+    else compare_rows<16, 1>(all, S);
     __syncthreads();
     // segments of the level, in the order of their groups
     const int before = s_segs;
@@ -288,108 +318,127 @@ __global__ __launch_bounds__(kPlanThreads) void k_share_plan(SharePlanArgs a, in
   }
   const int shared = ends[kShareLevels];
   // What sessions hold alone, the longest first.
-  const int own_n2 = n2;
   for (int at = threadIdx.x; at < S; at += kPlanThreads) {
     const int s = (int)(key[at] & 4095);
-    const int rows = a.kv.rows ? a.kv.rows[s] : a.kv.R;
-    const int len = base[s] + (rows < 0 ? 0 : rows > a.kv.R ? a.kv.R : rows);
     int from = depth[at] << shift;
     if (a.window > 0) {
       const int64_t lowest = (int64_t)base[s] - a.window + 1;
       if (lowest > from) from = (int)lowest & ~(kKvBlock - 1);
     }
     alike[at] = from;
-    low[at] = len > from ? len : from;
+    low[at] = length[s] > from ? length[s] : from;
     a.order[at] = limit[at] = s;
   }
   __syncthreads();
-  for (int at = threadIdx.x; at < own_n2; at += kPlanThreads)
+  for (int at = threadIdx.x; at < n2; at += kPlanThreads)
     key[at] = at < S ? (uint64_t)(uint32_t)(kKvMost - (low[at] - alike[at])) << 12 | (uint64_t)at : ~uint64_t(0);
-  sort_keys(key, own_n2);
-  for (int i = threadIdx.x; i < S; i += kPlanThreads) {
-    const int at = (int)(key[i] & 4095);
-    a.segs[shared + i] = ShareSeg{at, 1, alike[at], low[at]};
-  }
-  __syncthreads();
+  sort_keys(key, n2);
 
   // Shares, of each kind the shortest that fill the device about once: eight waves
   // sum up a kind's items for a candidate each.
-  const int RG = a.kv.R * a.group;
+  const int RG = a.kv.R * a.group, row_shift[2] = {__ffs(a.z.rows[0]) - 1, __ffs(a.z.rows[1]) - 1};
+  auto tiles_of = [&](int members, int kind) { return (int)(((uint32_t)members * RG + a.z.rows[kind] - 1) >> row_shift[kind]); };
   {
     const int kind = wave >> 3, candidate = wave & 7;
-    const ShareSeg* segs = a.segs + (kind ? shared : 0);
-    const int n = kind ? S : shared, rows = a.z.rows[kind];
-    int64_t load = 0, tiles = 0;
+    const int n = kind ? S : shared;
+    auto segment = [&](int i) { return kind ? ShareSeg{i, 1, alike[i], low[i]} : a.segs[i]; };
+    // (in floating point: the number of shares is free)
+    float load = 0.0f, tiles = 0.0f;
     for (int i = lane; i < n; i += 64) {
-      const ShareSeg t = segs[i];
-      const int64_t k = ((int64_t)t.members * RG + rows - 1) / rows;
+      const ShareSeg t = segment(i);
+      const float k = (float)tiles_of(t.members, kind);
       tiles += k;
-      load += k * (t.to - t.from);
+      load += k * (float)(t.to - t.from);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
       load += __shfl_xor(load, o, 64);
       tiles += __shfl_xor(tiles, o, 64);
     }
-    load *= a.kv.heads;
-    tiles *= a.kv.heads;
-    const int64_t slots = a.z.slots;
+    load *= (float)a.kv.heads;
+    tiles *= (float)a.kv.heads;
+    const float slots = (float)a.z.slots;
     const bool few = tiles < 2 * slots;
-    const int64_t target = 2 * tiles <= slots ? slots : 2 * slots;
-    int64_t c = few ? load * (8 + 2 * candidate) / (8 * target) : load / slots;
-    const int64_t room = a.z.extra > 0 ? (longest + a.z.extra - 1) / a.z.extra : longest;
+    const float target = 2 * tiles <= slots ? slots : 2 * slots;
+    float c = few ? load * (0.125f * (8 + 2 * candidate)) / target : load / slots;
+    const int room = a.z.extra > 0 ? (longest + a.z.extra - 1) / a.z.extra : longest;
     const bool last = !few || candidate == 7;
-    if (few && last) c = longest;
-    if (c < room) c = room;
-    if (c < kShareLeast) c = kShareLeast;
-    c = (c + kShareStep - 1) / kShareStep * kShareStep;
-    int64_t items = 0;
+    if (few && last) c = (float)longest;
+    int chunk = c < (float)longest ? (int)c : longest;
+    chunk = chunk > room ? chunk : room;
+    chunk = chunk > kShareLeast ? chunk : kShareLeast;
+    chunk = (chunk + kShareStep - 1) / kShareStep * kShareStep;
+    float items = 0.0f;
     for (int i = lane; i < n; i += 64) {
-      const ShareSeg t = segs[i];
-      items += ((int64_t)t.members * RG + rows - 1) / rows * ((t.to - t.from + c - 1) / c);
+      const ShareSeg t = segment(i);
+      items += (float)(tiles_of(t.members, kind) * ((uint32_t)(t.to - t.from + chunk - 1) / (uint32_t)chunk));
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) items += __shfl_xor(items, o, 64);
-    if (lane == 0) s_chunk[wave] = last || items * a.kv.heads <= target ? (int)c : INT32_MAX;
+    if (lane == 0) s_chunk[wave] = last || items * a.kv.heads <= target ? chunk : INT32_MAX;
   }
   __syncthreads();
   int chunk[2] = {INT32_MAX, INT32_MAX};
 #pragma unroll
   for (int k = 0; k < 16; ++k) chunk[k >> 3] = s_chunk[k] < chunk[k >> 3] ? s_chunk[k] : chunk[k >> 3];
 
-  // Parts of each segment, level by level along the paths, and the items: those of a
-  // segment by a wave.
+  // Parts of each segment, level by level along the paths, and the items, one a
+  // thread, which looks for its segment in the sums of them.
+  int32_t *before = page0, *part_of = base;  // of up to n2 segments
   int made = 0;
 #pragma unroll
   for (int level = 0; level <= kShareLevels; ++level) {
     const int kind = level == kShareLevels;
-    const int lo = kind ? shared : ends[level], hi = kind ? shared + S : ends[level + 1];
-    const int c = chunk[kind], rows = a.z.rows[kind];
+    const int lo = kind ? 0 : ends[level], hi = kind ? S : ends[level + 1];
+    const uint32_t c = chunk[kind];
+    auto segment = [&](int i) {
+      if (!kind) return a.segs[i];
+      const int at = (int)(key[i] & 4095);
+      return ShareSeg{at, 1, alike[at], low[at]};
+    };
+    int sum = 0;
     for (int i0 = lo; i0 < hi; i0 += kPlanThreads) {
       const int i = i0 + threadIdx.x;
+      int n = 0, shares = 0, all = 0;
       ShareSeg t{0, 0, 0, 0};
-      if (i < hi) t = a.segs[i];
-      const int tiles = (int)(((int64_t)t.members * RG + rows - 1) / rows), shares = (t.to - t.from + c - 1) / c;
-      int all = 0;
-      const int before = made + sum_before(i < hi ? tiles * shares : 0, &all);
-      const int n = hi - i0 - wave * 64 < 64 ? hi - i0 - wave * 64 : 64;
-      for (int k = 0; k < n; ++k) {
-        const ShareSeg u{__builtin_amdgcn_readlane(t.first, k), __builtin_amdgcn_readlane(t.members, k),
-                         __builtin_amdgcn_readlane(t.from, k), __builtin_amdgcn_readlane(t.to, k)};
-        const int at = __builtin_amdgcn_readlane(before, k), nt = __builtin_amdgcn_readlane(tiles, k);
-        const int ns = __builtin_amdgcn_readlane(shares, k), part = count[u.first];
-        for (int x = lane; x < nt * ns; x += 64) {
-          const int share = x / nt, tile = x - share * nt;
-          const int64_t to = (int64_t)u.from + (int64_t)(share + 1) * c;
-          if (at + x < a.z.cap)
-            a.items[at + x] = ShareItem{u.first, u.members, tile, u.from + share * c, to < u.to ? (int)to : u.to,
-                                        part + share, nt == 1, kind};
-        }
-        for (int m = lane; m < u.members; m += 64) count[u.first + m] = (uint16_t)(part + ns);
+      if (i < hi) {
+        t = segment(i);
+        shares = (uint32_t)(t.to - t.from + c - 1) / c;
+        n = tiles_of(t.members, kind) * shares;
+        part_of[i - lo] = count[t.first];
       }
-      made += all;
-      __syncthreads();
+      const int at = sum + sum_before(n, &all);
+      if (i < hi) before[i - lo] = at;
+      sum += all;
+      if (kind) {
+        if (i < hi) count[t.first] = (uint16_t)(count[t.first] + shares);
+      } else {  // (a segment's members by a wave)
+        const int mine = hi - i0 - wave * 64 < 64 ? hi - i0 - wave * 64 : 64;
+        for (int k = 0; k < mine; ++k) {
+          const int from = __builtin_amdgcn_readlane(t.first, k), m = __builtin_amdgcn_readlane(t.members, k);
+          const int more_parts = __builtin_amdgcn_readlane(shares, k);
+          for (int x = lane; x < m; x += 64) count[from + x] = (uint16_t)(count[from + x] + more_parts);
+        }
+      }
     }
+    __syncthreads();
+    for (int x = threadIdx.x; x < sum; x += kPlanThreads) {
+      int i = 0, past = hi - lo;  // the last segment with before <= x (one without items has the next one's)
+      while (past - i > 1) {
+        const int mid = (i + past) >> 1;
+        if (before[mid] <= x) i = mid;
+        else past = mid;
+      }
+      const ShareSeg t = segment(lo + i);
+      const uint32_t nt = tiles_of(t.members, kind), rest = x - before[i];
+      const uint32_t share = rest / nt, tile = rest - share * nt;
+      const int64_t to = (int64_t)t.from + (int64_t)(share + 1) * c;
+      if (made + x < a.z.cap)
+        a.items[made + x] = ShareItem{t.first, t.members, (int)tile, (int)(t.from + share * c), to < t.to ? (int)to : t.to,
+                                      (int)(part_of[i] + share), nt == 1, kind};
+    }
+    made += sum;
+    __syncthreads();
   }
   for (int at = threadIdx.x; at < S; at += kPlanThreads) a.parts[limit[at]] = count[at];
   if (threadIdx.x == 0) *a.head = ShareHead{a.key, made, 0, shared};

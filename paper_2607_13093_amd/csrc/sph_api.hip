@@ -1153,7 +1153,7 @@ int share_call(const char* fn, const sph_kv_cache* cache, int64_t layer, int64_t
   if (window < 0 || max_len < 0)
     return fail(SPH_E_INVALID_ARG, "%s: window=%lld max_len=%lld", fn, (long long)window, (long long)max_len);
   if (!sph::kv_share_fits(n_sessions, R, q_heads))
-    return fail(SPH_E_UNSUPPORTED, "%s: n_sessions=%lld R=%lld q_heads=%lld (4096 sessions, 2^26 rows of heads at most)", fn,
+    return fail(SPH_E_UNSUPPORTED, "%s: n_sessions=%lld R=%lld q_heads=%lld (2048 sessions, 2^26 rows of heads at most)", fn,
                 (long long)n_sessions, (long long)R, (long long)q_heads);
   return SPH_OK;
 }

@@ -133,7 +133,7 @@ def test_share_cache_checks(lib, kw, code, msg):
 BOTH = [
     (dict(n=-1), E, b"n_sessions=-1"), (dict(n=5), E, b"beyond n_slots=4"), (dict(R=-1), E, b"R=-1"),
     (dict(q_heads=12), E, b"q_heads=12"), (dict(q_heads=0), E, b"q_heads=0"), (dict(window=-1), E, b"window=-1"),
-    (dict(max_len=-1), E, b"max_len=-1"), (dict(n=4097, slots=16), U, b"4096 sessions"), (dict(R=1 << 24), U, b"2^26 rows"),
+    (dict(max_len=-1), E, b"max_len=-1"), (dict(n=2049, slots=16), U, b"2048 sessions"), (dict(R=1 << 24), U, b"2^26 rows"),
 ]
 
 
@@ -162,7 +162,7 @@ def test_share_sizes_and_empty_calls(lib):
     assert plan > 0 and ws >= 3 * 5 * 32 * 2 * (128 * 4 + 8)
     assert _share(lib, c, nb=plan - 1) == W and _shared(lib, c, plan_bytes=plan - 1) == E and _shared(lib, c, nb=ws - 1) == W
     for bad in ((None, 32, 3, 5, 0), (p, 12, 3, 5, 0), (p, 32, 0, 5, 0), (p, 32, 3, 0, 0), (p, 32, 3, 5, -1),
-                (p, 32, 4097, 5, 0), (p, 32, 3, 1 << 24, 0)):
+                (p, 32, 2049, 5, 0), (p, 32, 3, 1 << 24, 0)):
         assert lib.sph_kv_share_bytes(*bad) == 0 and lib.sph_kv_attend_shared_workspace(*bad) == 0
     for kw in (dict(n=0), dict(R=0)):
         assert _share(lib, c, plan=None, nb=0, **kw) == 0
