@@ -35,9 +35,8 @@ struct WeighArgs {
 };
 
 constexpr float kLog2e = 1.44269504088896f;
-constexpr int kWeighTiles = 4;                                         // tiles of 32 tokens of a wave
-constexpr int weigh_tiles(int d, bool many) { return many && d == 256 ? 2 : kWeighTiles; }
-constexpr int weigh_tokens(int d, bool many) { return 4 * 32 * weigh_tiles(d, many); }  // of a workgroup
+constexpr int weigh_tiles(int d) { return d == 256 ? 2 : 4; }          // of 32 tokens, of a wave
+constexpr int weigh_tokens(int d) { return 4 * 32 * weigh_tiles(d); }  // of a workgroup
 
 // What a workgroup does of a call: tokens `at` x TOKENS ... of a session for some heads
 // and tiles of rows.
@@ -206,13 +205,21 @@ __device__ __forceinline__ void read_keys(KvKeys<D>& k, uint32_t at_c, uint32_t 
   }
 }
 
-constexpr int kKeyStages = 4;
+// What of the queries of a head a workgroup holds in LDS: operands [MT][D / 32][64 lanes]
+// of 16 bytes, then the lanes' log-sum-exp [MT][64].
+template <int D, int MT>
+struct QueryStage {
+  static constexpr int kChunks = MT * (D / 32);
+  static constexpr int kBytes = kChunks * 1024 + MT * 256;
+  static constexpr int kCopies = (kChunks + 3) / 4 + 1;  // of each of four waves
+};
 constexpr int weigh_waves(int d, int mt) { return d * mt <= 128 ? 4 : d * mt <= 256 ? 3 : 2; }
 
 template <int D, int MT>
 __global__ __launch_bounds__(256, weigh_waves(D, MT)) void k_weigh_few(WeighArgs a) {
-  constexpr int TT = kWeighTiles, KJ = D / 32, TOKENS = weigh_tokens(D, false), NS = kKeyStages;
-  __shared__ __align__(16) uint8_t smem[4 * NS * KeyStage<D>::kBytes];
+  constexpr int TT = weigh_tiles(D), KJ = D / 32, TOKENS = weigh_tokens(D), NS = TT;  // (a head's tiles are the ring's stages)
+  using Q = QueryStage<D, MT>;
+  __shared__ __align__(16) uint8_t smem[4 * NS * KeyStage<D>::kBytes + 2 * Q::kBytes];
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int part_of = blockIdx.x % a.parts;
@@ -221,82 +228,116 @@ __global__ __launch_bounds__(256, weigh_waves(D, MT)) void k_weigh_few(WeighArgs
   const KvSession ses = kv_session(a.kv, s);
   const int G = a.group, live = ses.rows * G, base = ses.len - ses.rows;
   const int slot = a.kv.slots ? a.kv.slots[s] : s;
+  if (live <= 0) return;
   uint8_t* ring = smem + wave * (NS * KeyStage<D>::kBytes);
+  uint8_t* queries = smem + 4 * NS * KeyStage<D>::kBytes;
   const uint32_t ring_at = (uint32_t)(uintptr_t)(lds_void_t*)ring;
   const uint32_t key_at = n * (D / 2) + g * (D / 8);
   const uint32_t ks_at = KeyStage<D>::kCodes + (D == 64 ? g >> 1 : D == 128 ? g : 2 * g) * kKvBlock + n;
+
+  // rows: fq = r G + query head of the key/value head's; those past the session's are
+  // its last, of no weight
+  int row_at[MT], head_at[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int fq = m * 16 + n < live ? m * 16 + n : live - 1;
+    row_at[m] = fq / G;
+    head_at[m] = fq - row_at[m] * G;
+  }
+  // A wave's share of a head's queries, on their way into LDS: a lane's 16 bytes are the
+  // ones that it reads.
+  auto fetch_queries = [&](int head, int buffer) {
+    uint8_t* to = queries + buffer * Q::kBytes;
+#pragma unroll
+    for (int i = 0; i < (Q::kChunks + 3) / 4; ++i) {
+      const int chunk = Q::kChunks < 4 ? wave % Q::kChunks : i * 4 + wave, m = chunk / KJ, j = chunk % KJ;
+      int r = row_at[0], in = head_at[0];
+#pragma unroll
+      for (int k = 1; k < MT; ++k)
+        if (m == k) r = row_at[k], in = head_at[k];
+      const uint16_t* p = a.q + ((int64_t)s * a.kv.R + r) * a.q_row + (int64_t)(head * G + in) * a.q_head + g * (D / 4) + 8 * j;
+      if (a.q_aligned) {
+        __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint8_t*>(p), (lds_void_t*)(to + chunk * 1024), 16, 0, 0);
+      } else {
+        u32x4_t x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = (uint32_t)p[2 * e] | ((uint32_t)p[2 * e + 1] << 16);
+        *reinterpret_cast<u32x4_t*>(to + chunk * 1024 + lane * 16) = x;
+      }
+    }
+    const int m = wave % MT;
+    int r = row_at[0], in = head_at[0];
+#pragma unroll
+    for (int k = 1; k < MT; ++k)
+      if (m == k) r = row_at[k], in = head_at[k];
+    const float* p = a.lse + ((int64_t)s * a.kv.R + r) * (a.kv.heads * G) + head * G + in;
+    __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint8_t*>(p), (lds_void_t*)(to + Q::kChunks * 1024 + m * 256), 4, 0, 0);
+  };
 
   for (int at = rest / a.kv.n_sessions; at * TOKENS < ses.len; at += a.groups) {
     const WeighShare share = weigh_share(a, part_of, at);
     const int t0 = at * TOKENS + wave * (32 * TT), t1 = t0 + 32 * TT;
     if (share.h0 >= share.h1) continue;
     KvPages pages[TT];
-    bool paged = true;
+    bool whole = true;  // every row sees every token
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
       pages[t] = tile_pages(a.kv, ses, t0 + 32 * t, ses.len);
-      paged = paged && pages[t].page[0] >= 0 && pages[t].page[1] >= 0;
+      whole = whole && pages[t].page[0] >= 0 && pages[t].page[1] >= 0;
     }
-    int rt0, rt1;
-    rows_that_see(ses, G, a.window, t0, t1, &rt0, &rt1);
-    // groups of MT tiles, those of this part
-    const int g0 = rt0 / MT + share.phase, g1 = rt1 > rt0 ? (rt1 + MT - 1) / MT : 0;
-
+    whole = whole && base >= t1 - 1 && (a.window == 0 || t0 > ses.len - 1 - a.window);
+    int from[MT], span[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const int pos = base + row_at[m], most = pos < 0 || m * 16 + n >= live ? 0 : pos + 1;
+      span[m] = a.window > 0 && a.window < most ? a.window : most;
+      from[m] = t0 + 4 * g - (pos - span[m] + 1);
+    }
     f32x4_t acc[TT][2];
 #pragma unroll
     for (int t = 0; t < TT; ++t) acc[t][0] = acc[t][1] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
-    // units: heads x groups of tiles; each goes over the TT tiles of tokens
-    int head = share.h0, rg = g0;
-    int ahead_head = head, ahead_rg = rg;  // of the unit that the next copies are for
-    if (g0 < g1) {
+    __syncthreads();  // the queries of the tokens before are read
+    fetch_queries(share.h0, 0);
 #pragma unroll
-      for (int t = 0; t < NS - 1; ++t) copy_keys<D>(ring + t * KeyStage<D>::kBytes, a.kv, head, t0 + 32 * t, pages[t], lane);
-    }
-    while (g0 < g1 && head < share.h1) {
-      ahead_rg = rg + share.step;
-      ahead_head = head;
-      if (ahead_rg >= g1) {
-        ahead_rg = g0;
-        ++ahead_head;
-      }
-      const bool more = ahead_head < share.h1;
+    for (int t = 0; t < NS - 1; ++t) copy_keys<D>(ring + t * KeyStage<D>::kBytes, a.kv, share.h0, t0 + 32 * t, pages[t], lane);
+    for (int head = share.h0; head < share.h1; ++head) {
+      constexpr int C = KeyStage<D>::kCopies;
+      const bool more = head + 1 < share.h1;
+      const int buffer = (head - share.h0) & 1;
+      wait_copies<(NS - 1) * C>();  // the queries are older than those of the tiles
+      __syncthreads();
+      if (more) fetch_queries(head + 1, buffer ^ 1);
+      const uint8_t* held = queries + buffer * Q::kBytes;
       u32x4_t qf[MT][KJ];
       float l[MT];
-      int from[MT], span[MT];
-      bool whole = paged;
+      bool dead = false;
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        const int fq = (rg * MT + m) * 16 + n;
-        const int r = fq / G;
-        l[m] = fetch_query<D>(a, qf[m], s, head, r, fq - r * G, fq < live, g);
-      }
+        // (what a row sees is compared for every head: kept, the answers would be spilled)
+        asm volatile("" : "+v"(from[m]), "+v"(span[m]));
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const int low = (rg * MT + m) * 16, high = low + 15 < live ? low + 15 : live - 1;
-        const int r = (low + n) / G, pos = base + r;
-        const bool dead = l[m] == -INFINITY;  // the row sees nothing
-        whole = whole && low + 16 <= live && base + low / G >= t1 - 1 && (a.window == 0 || t0 > base + high / G - a.window) &&
-                !__any(dead);
-        const int most = pos < 0 || dead ? 0 : pos + 1;
-        span[m] = a.window > 0 && a.window < most ? a.window : most;
-        from[m] = t0 + 4 * g - (pos - span[m] + 1);
-        l[m] *= kLog2e;
+        for (int j = 0; j < KJ; ++j) qf[m][j] = *reinterpret_cast<const u32x4_t*>(held + (m * KJ + j) * 1024 + lane * 16);
+        const float x = *reinterpret_cast<const float*>(held + Q::kChunks * 1024 + m * 256 + lane * 4);
+        const bool is = m * 16 + n < live;
+        dead = dead || (is && x == -INFINITY);  // a row that sees nothing
+        l[m] = is && x != -INFINITY ? x * kLog2e : INFINITY;  // no weight of finite scores
       }
+      const bool alive = whole && !__any(dead);
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
-        constexpr int C = KeyStage<D>::kCopies;
         const int next = t + NS - 1;
-        static_assert(NS == TT, "a unit's tiles are the ring's stages");
-        if (next < TT) {
-          copy_keys<D>(ring + next * KeyStage<D>::kBytes, a.kv, head, t0 + 32 * next, pages[next], lane);
+        if (next < TT) copy_keys<D>(ring + next * KeyStage<D>::kBytes, a.kv, head, t0 + 32 * next, pages[next], lane);
+        else if (more)
+          copy_keys<D>(ring + (next - TT) * KeyStage<D>::kBytes, a.kv, head + 1, t0 + 32 * (next - TT), pages[next - TT], lane);
+        if (more) {
+          if (a.q_aligned && t < TT - 1) wait_copies<(NS - 1) * C + Q::kCopies>();
+          else wait_copies<(NS - 1) * C>();
+        } else if (t == 0) {
           wait_copies<(NS - 1) * C>();
-        } else if (more) {
-          copy_keys<D>(ring + (next - TT) * KeyStage<D>::kBytes, a.kv, ahead_head, t0 + 32 * (next - TT), pages[next - TT], lane);
-          wait_copies<(NS - 1) * C>();
-        } else if (t == 1) {
+        } else if (t + 2 < TT) {
           wait_copies<2 * C>();
-        } else if (t == 2) {
+        } else if (t + 1 < TT) {
           wait_copies<C>();
         } else {
           wait_copies<0>();
@@ -304,6 +345,11 @@ __global__ __launch_bounds__(256, weigh_waves(D, MT)) void k_weigh_few(WeighArgs
         KvKeys<D> keys;
         const uint32_t stage = ring_at + t * KeyStage<D>::kBytes;
         read_keys<D>(keys, stage + key_at, stage + ks_at);
+        // (a key that is no number would weigh on rows that are none)
+        bool numbers = keys.s[0] != 255u && keys.s[1] != 255u;
+        if constexpr (D == 256)
+          numbers = (keys.s[0] & 255u) != 255u && keys.s[0] >> 8 != 255u && (keys.s[1] & 255u) != 255u && keys.s[1] >> 8 != 255u;
+        const bool all = alive && __all(numbers);
         f32x4_t sc[MT][2];
 #pragma unroll
         for (int m = 0; m < MT; ++m) sc[m][0] = sc[m][1] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
@@ -324,14 +370,15 @@ __global__ __launch_bounds__(256, weigh_waves(D, MT)) void k_weigh_few(WeighArgs
             sc[m][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[1], q, sc[m][1], 0, 0, 0);
           }
         }
+        if (all) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          if (whole) add_weights(acc[t], sc[m], a.scale_log2, l[m]);
-          else add_seen(acc[t], sc[m], a.scale_log2, l[m], from[m] + 32 * t, span[m], pages[t].page);
+          for (int m = 0; m < MT; ++m) add_weights(acc[t], sc[m], a.scale_log2, l[m]);
+        } else {
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+            add_seen(acc[t], sc[m], a.scale_log2, l[m], from[m] + 32 * t, l[m] == INFINITY ? 0 : span[m], pages[t].page);
         }
       }
-      head = ahead_head;
-      rg = ahead_rg;
     }
     give_weights<TT>(a, ses, s, slot, part_of, share.whole, t0, TOKENS, acc, g, n);
   }
@@ -340,7 +387,7 @@ __global__ __launch_bounds__(256, weigh_waves(D, MT)) void k_weigh_few(WeighArgs
 // Many rows: a head's keys stay in registers as operands while its tiles of rows pass.
 template <int D>
 __global__ __launch_bounds__(256, 2) void k_weigh_many(WeighArgs a) {
-  constexpr int TT = weigh_tiles(D, true), KJ = D / 32, TOKENS = weigh_tokens(D, true);
+  constexpr int TT = weigh_tiles(D), KJ = D / 32, TOKENS = weigh_tokens(D);
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int part_of = blockIdx.x % a.parts;
@@ -407,20 +454,38 @@ __global__ __launch_bounds__(256, 2) void k_weigh_many(WeighArgs a) {
         const bool dead = l == -INFINITY;  // the row sees nothing
         const bool whole = paged && low + 16 <= live && base + low / G >= t1 - 1 &&
                            (a.window == 0 || t0 > base + high / G - a.window) && !__any(dead);
-        const int most = pos < 0 || dead ? 0 : pos + 1;
-        const int span = a.window > 0 && a.window < most ? a.window : most;
-        const int from = t0 + 4 * g - (pos - span + 1);
-#pragma unroll
-        for (int t = 0; t < TT; ++t) {
-          f32x4_t sc[2];
-          sc[0] = sc[1] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        f32x4_t sc[2][2];
+        auto score = [&](int t) {
+          f32x4_t(&x)[2] = sc[t & 1];
+          x[0] = x[1] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
           for (int j = 0; j < KJ; ++j) {
-            sc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t][0][j], q[j], sc[0], 0, 0, 0);
-            sc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t][1][j], q[j], sc[1], 0, 0, 0);
+            x[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t][0][j], q[j], x[0], 0, 0, 0);
+            x[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t][1][j], q[j], x[1], 0, 0, 0);
           }
-          if (whole) add_weights(acc[t], sc, a.scale_log2, l);
-          else add_seen(acc[t], sc, a.scale_log2, l, from + 32 * t, span, pages[t]);
+        };
+        score(0);
+        if (whole) {  // the products of the next tile beside the weights of this one
+#pragma unroll
+          for (int t = 0; t < TT; ++t) {
+            if (t + 1 < TT) score(t + 1);
+            add_weights(acc[t], sc[t & 1], a.scale_log2, l);
+#pragma unroll
+            for (int i = 0; i < 2 * KJ; ++i) {
+              __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);                // a product,
+              __builtin_amdgcn_sched_group_barrier(0x2, 16 / (2 * KJ) > 0 ? 16 / (2 * KJ) : 1, 0);  // vector instructions,
+              __builtin_amdgcn_sched_group_barrier(0x400, 8 / (2 * KJ) > 0 ? 8 / (2 * KJ) : 1, 0);  // exponentials
+            }
+          }
+        } else {
+          const int most = pos < 0 || dead ? 0 : pos + 1;
+          const int span = a.window > 0 && a.window < most ? a.window : most;
+          const int from = t0 + 4 * g - (pos - span + 1);
+#pragma unroll
+          for (int t = 0; t < TT; ++t) {
+            if (t > 0) score(t);
+            add_seen(acc[t], sc[t & 1], a.scale_log2, l, from + 32 * t, span, pages[t]);
+          }
         }
       }
     }
@@ -432,9 +497,10 @@ __global__ __launch_bounds__(256, 2) void k_weigh_many(WeighArgs a) {
 __global__ __launch_bounds__(256) void k_weigh_join(WeighArgs a, int tokens) {
   const int s = blockIdx.x % a.kv.n_sessions, j = blockIdx.x / a.kv.n_sessions * 256 + threadIdx.x;
   const KvSession ses = kv_session(a.kv, s);
-  if (j >= tokens || j >= ses.len) return;
+  if (j >= tokens || j >= ses.len || ses.rows <= 0) return;
   const float* part = a.part + (int64_t)s * a.parts * tokens + j;
   float x = 0.0f;
+#pragma unroll 8
   for (int k = 0; k < a.parts; ++k) x += part[(int64_t)k * tokens];
   float* w = a.w + (a.kv.slots ? a.kv.slots[s] : s) * a.ld_w + j;
   *w = (a.fresh && j >= ses.len - ses.rows ? 0.0f : *w) + x;
@@ -452,12 +518,12 @@ WeighPlan weigh_plan(int d, int64_t n_sessions, int64_t R, int64_t heads, int64_
   WeighPlan p{};
   const int64_t tiles = (R * group + 15) / 16;
   p.mt = tiles > (d == 256 ? 2 : 4) ? 0 : tiles > 2 ? 4 : (int)tiles;
-  p.tokens = weigh_tokens(d, p.mt == 0);
+  p.tokens = weigh_tokens(d);
   p.groups = (int)((max_len + p.tokens - 1) / p.tokens);
   // (a workgroup goes on to further groups of tokens)
   const int64_t most_groups = (1 << 22) / n_sessions > 1 ? (1 << 22) / n_sessions : 1;
   if (p.groups > most_groups) p.groups = (int)most_groups;
-  const int64_t units = n_sessions * p.groups, want = (p.mt == 0 ? 8 : 2) * kCUs;
+  const int64_t units = n_sessions * p.groups, want = (p.mt == 0 ? 16 : 2) * kCUs;
   p.by_rows = 1;
   p.heads_each = (int)heads;
   p.parts = 1;
