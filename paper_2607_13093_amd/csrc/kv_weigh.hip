@@ -206,11 +206,11 @@ __device__ __forceinline__ void read_keys(KvKeys<D>& k, uint32_t at_c, uint32_t 
 }
 
 // What of the queries of a head a workgroup holds in LDS: operands [MT][D / 32][64 lanes]
-// of 16 bytes, then the lanes' log-sum-exp [MT][64].
+// of 16 bytes, then the rows' log-sum-exp [MT][16].
 template <int D, int MT>
 struct QueryStage {
   static constexpr int kChunks = MT * (D / 32);
-  static constexpr int kBytes = kChunks * 1024 + MT * 256;
+  static constexpr int kBytes = kChunks * 1024 + 256;
   static constexpr int kCopies = (kChunks + 3) / 4 + 1;  // of each of four waves
 };
 constexpr int weigh_waves(int d, int mt) { return d * mt <= 128 ? 4 : d * mt <= 256 ? 3 : 2; }
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(256, weigh_waves(D, MT)) void k_weigh_few(WeighArgs
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int part_of = blockIdx.x % a.parts;
   const int rest = blockIdx.x / a.parts;
-  const int s = rest % a.kv.n_sessions;
+  const int s = (rest + rest / a.kv.n_sessions) % a.kv.n_sessions;  // (a session's groups of tokens on all XCDs)
   const KvSession ses = kv_session(a.kv, s);
   const int G = a.group, live = ses.rows * G, base = ses.len - ses.rows;
   const int slot = a.kv.slots ? a.kv.slots[s] : s;
@@ -265,13 +265,12 @@ __global__ __launch_bounds__(256, weigh_waves(D, MT)) void k_weigh_few(WeighArgs
         *reinterpret_cast<u32x4_t*>(to + chunk * 1024 + lane * 16) = x;
       }
     }
-    const int m = wave % MT;
-    int r = row_at[0], in = head_at[0];
+    int r = row_at[0], in = head_at[0];  // lane g 16 + n: row n of tile g
 #pragma unroll
     for (int k = 1; k < MT; ++k)
-      if (m == k) r = row_at[k], in = head_at[k];
+      if (g == k) r = row_at[k], in = head_at[k];
     const float* p = a.lse + ((int64_t)s * a.kv.R + r) * (a.kv.heads * G) + head * G + in;
-    __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint8_t*>(p), (lds_void_t*)(to + Q::kChunks * 1024 + m * 256), 4, 0, 0);
+    __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint8_t*>(p), (lds_void_t*)(to + Q::kChunks * 1024), 4, 0, 0);
   };
 
   for (int at = rest / a.kv.n_sessions; at * TOKENS < ses.len; at += a.groups) {
@@ -318,7 +317,7 @@ __global__ __launch_bounds__(256, weigh_waves(D, MT)) void k_weigh_few(WeighArgs
         asm volatile("" : "+v"(from[m]), "+v"(span[m]));
 #pragma unroll
         for (int j = 0; j < KJ; ++j) qf[m][j] = *reinterpret_cast<const u32x4_t*>(held + (m * KJ + j) * 1024 + lane * 16);
-        const float x = *reinterpret_cast<const float*>(held + Q::kChunks * 1024 + m * 256 + lane * 4);
+        const float x = *reinterpret_cast<const float*>(held + Q::kChunks * 1024 + (m * 16 + n) * 4);
         const bool is = m * 16 + n < live;
         dead = dead || (is && x == -INFINITY);  // a row that sees nothing
         l[m] = is && x != -INFINITY ? x * kLog2e : INFINITY;  // no weight of finite scores
@@ -392,7 +391,7 @@ __global__ __launch_bounds__(256, 2) void k_weigh_many(WeighArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int part_of = blockIdx.x % a.parts;
   const int rest = blockIdx.x / a.parts;
-  const int s = rest % a.kv.n_sessions;
+  const int s = (rest + rest / a.kv.n_sessions) % a.kv.n_sessions;  // (a session's groups of tokens on all XCDs)
   const KvSession ses = kv_session(a.kv, s);
   const int G = a.group, live = ses.rows * G, base = ses.len - ses.rows;
   const int slot = a.kv.slots ? a.kv.slots[s] : s;
