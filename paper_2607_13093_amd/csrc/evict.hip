@@ -36,11 +36,37 @@ __device__ __forceinline__ uint32_t order_of(float w) {
 }
 
 constexpr int kChoose = 1024;  // threads that choose a slot's tokens
-constexpr int kLook = 4;       // tokens a thread looks at in a turn
+constexpr int kLook = 4;       // tokens of a thread that are numbered at a time
+constexpr int kBins = 2048;    // of a digit of 11 bits; three digits are an order
 
-__global__ __launch_bounds__(kChoose) void k_evict_choose(EvictArgs a) {
-  __shared__ uint32_t s_bins[16][256];
-  __shared__ int s_sure[64], s_tie[64];
+// Sum over the threads before this one, and over all.  For kChoose threads.
+__device__ __forceinline__ int threads_before(int x, int* all, int* s_wave) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int y = x;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int z = __shfl_up(y, o, 64);
+    if (lane >= o) y += z;
+  }
+  if (lane == 63) s_wave[wave] = y;
+  __syncthreads();
+  int before = 0, total = 0;
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const int n = s_wave[k];
+    if (k < wave) before += n;
+    total += n;
+  }
+  *all = total;
+  return before + y - x;
+}
+
+// The tokens of a slot.  KEPT: weights that a thread holds in registers, all of a slot
+// of up to 1024 KEPT tokens; longer ones are read once more for each digit.
+template <int KEPT>
+__device__ __forceinline__ void choose_tokens(const EvictArgs& a, int len, int held) {
+  __shared__ uint32_t s_bins[kBins];
+  __shared__ int s_sure[64], s_tie[64], s_wave[16];
   __shared__ int s_shared, s_start, s_digit, s_need;
   const int s = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const PagesArgs& p = a.p;
@@ -50,9 +76,13 @@ __global__ __launch_bounds__(kChoose) void k_evict_choose(EvictArgs a) {
   int32_t* kept = a.c.kept ? a.c.kept + s * a.c.ld_kept : nullptr;
   int64_t* from = a.from + (int64_t)s * a.most;
 
-  const int held_len = p.lens[s];
-  const int len = held_len < 0 ? 0 : (held_len < a.most ? held_len : a.most);
-  const int held = (len + (1 << p.page_shift) - 1) >> p.page_shift;
+  float mine[KEPT > 0 ? KEPT : 1];
+#pragma unroll
+  for (int i = 0; i < KEPT; ++i) {
+    const int j = i * kChoose + threadIdx.x;
+    mine[i] = j < len ? w[j] : 0.0f;
+  }
+  const int want = a.c.keep[s];
   if (threadIdx.x == 0) {
     s_shared = 0;
     s_start = len;
@@ -64,67 +94,73 @@ __global__ __launch_bounds__(kChoose) void k_evict_choose(EvictArgs a) {
     if ((unsigned)page < (unsigned)p.n_pages && p.refs[page] > 1) last = c + 1;
   }
   if (last) atomicMax(&s_shared, last);
+  for (int i = threadIdx.x; i < kBins; i += kChoose) s_bins[i] = 0;
   __syncthreads();
   const int64_t fixed = (int64_t)s_shared << p.page_shift;
-  int front = fixed > a.c.first ? (fixed < len ? (int)fixed : len) : (a.c.first < len ? a.c.first : len);
+  const int front = fixed > a.c.first ? (fixed < len ? (int)fixed : len) : (a.c.first < len ? a.c.first : len);
   const int back = len - front > a.c.recent ? len - a.c.recent : front;
   const int must = front + len - back;
-  const int want = a.c.keep[s];
   const int n = want < must ? must : (want < len ? want : len);
   int need = n - must;  // of the tokens from front to back
 
   // the weight of the last that is kept, and how many of that weight are
   uint32_t least = 0;
   if (need > 0 && n < len) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = threadIdx.x; i < 16 * 256; i += kChoose) s_bins[0][i] = 0;
-      __syncthreads();
-      for (int j = front + threadIdx.x; j < back; j += kChoose) {
-        const uint32_t x = order_of(w[j]);
-        if (shift == 24 || (x ^ least) >> (shift + 8) == 0) atomicAdd(&s_bins[wave][(x >> shift) & 255], 1u);
+#pragma unroll
+    for (int digit = 0; digit < 3; ++digit) {
+      const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit == 2 ? 10 : 11;
+      auto count = [&](int j, float x) {
+        const uint32_t o = order_of(x);
+        if (j >= front && j < back && (digit == 0 || (o ^ least) >> (shift + bits) == 0))
+          atomicAdd(&s_bins[(o >> shift) & ((1 << bits) - 1)], 1u);
+      };
+      if constexpr (KEPT > 0) {
+#pragma unroll
+        for (int i = 0; i < KEPT; ++i) count(i * kChoose + threadIdx.x, mine[i]);
+      } else {
+        for (int j0 = front; j0 < back; j0 += 8 * kChoose) {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int j = j0 + i * kChoose + threadIdx.x;
+            x[i] = j < back ? w[j] : 0.0f;
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) count(j0 + i * kChoose + threadIdx.x, x[i]);
+        }
       }
       __syncthreads();
-      if (threadIdx.x < 256) {
-        uint32_t t = 0;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) t += s_bins[k][threadIdx.x];
-        s_bins[0][threadIdx.x] = t;
-      }
-      __syncthreads();
-      if (wave == 0) {  // lane l: digits 255 - 4 l ... down
-        int t[4], all = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) all += t[k] = s_bins[0][255 - 4 * lane - k];
-        int before = all;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-          const int y = __shfl_up(before, o, 64);
-          if (lane >= o) before += y;
-        }
-        before -= all;
-        if (before < need && need <= before + all) {
-          int k = 0;
-          while (k < 3 && need > before + t[k]) before += t[k++];
-          s_digit = 255 - 4 * lane - k;
-          s_need = need - before;
-        }
+      // a thread's two digits, from the largest down
+      const int top = kBins - 1 - 2 * threadIdx.x;
+      const int t0 = s_bins[top], t1 = s_bins[top - 1];
+      int all = 0;
+      const int before = threads_before(t0 + t1, &all, s_wave);
+      s_bins[top] = s_bins[top - 1] = 0;  // for the next
+      if (before < need && need <= before + t0 + t1) {
+        const bool first = need <= before + t0;
+        s_digit = first ? top : top - 1;
+        s_need = need - before - (first ? 0 : t0);
       }
       __syncthreads();
       least |= (uint32_t)s_digit << shift;
       need = s_need;
-      __syncthreads();
     }
   }
 
   // numbers of the kept ones, in order; equal weights are kept from the first on
   int sure_before = 0, tie_before = 0;
-  for (int at = 0; at < len; at += kLook * kChoose) {
-    float x[kLook];
+  constexpr int kTurns = KEPT > 0 ? KEPT / kLook : 1;
+  auto number = [&](int at, const float (&x)[kLook]) {
+    int page[kLook];
     uint64_t sure[kLook], tie[kLook];
 #pragma unroll
     for (int i = 0; i < kLook; ++i) {
       const int j = at + i * kChoose + threadIdx.x;
-      x[i] = j < len ? w[j] : 0.0f;
+      page[i] = j < len ? row[j >> p.page_shift] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < kLook; ++i) {
+      const int j = at + i * kChoose + threadIdx.x;
       bool is_sure = n == len && j < len, is_tie = false;
       if (j < front || (j >= back && j < len)) is_sure = true;
       else if (j < len && n < len && need > 0) {
@@ -147,10 +183,11 @@ __global__ __launch_bounds__(kChoose) void k_evict_choose(EvictArgs a) {
       const int y = __shfl_up(ns, o, 64), z = __shfl_up(nt, o, 64);
       if (lane >= o) ns += y, nt += z;
     }
-    const int all_sure = __shfl(ns, 63, 64), all_tie = __shfl(nt, 63, 64);
+    const int all_sure = __builtin_amdgcn_readlane(ns, 63), all_tie = __builtin_amdgcn_readlane(nt, 63);
     ns -= ms;
     nt -= mt;
     const uint64_t below = (uint64_t(1) << lane) - 1;
+    int start = len;
 #pragma unroll
     for (int i = 0; i < kLook; ++i) {
       const int j = at + i * kChoose + threadIdx.x;
@@ -158,20 +195,40 @@ __global__ __launch_bounds__(kChoose) void k_evict_choose(EvictArgs a) {
       const int to = sure_before + __shfl(ns, i * 16 + wave, 64) + __popcll(sure[i] & below) + (t < need ? t : need);
       const bool stays = (sure[i] >> lane & 1) || ((tie[i] >> lane & 1) && t < need);
       if (stays) {
-        const int page = row[j >> p.page_shift];
         const int in_page = j & ((1 << p.page_shift) - 1);
-        from[to] = (unsigned)page < (unsigned)p.n_pages
-                       ? (page * p.page_stride + (in_page / kKvBlock) * a.block_bytes) | (in_page % kKvBlock)
+        from[to] = (unsigned)page[i] < (unsigned)p.n_pages
+                       ? (page[i] * p.page_stride + (in_page / kKvBlock) * a.block_bytes) | (in_page % kKvBlock)
                        : -1;
         w_out[to] = x[i];
         if (kept) kept[to] = j;
-      } else if (j < len) {
-        atomicMin(&s_start, j);
+      } else if (j < start) {
+        start = j;
       }
     }
+    if (start < len) atomicMin(&s_start, start);
     sure_before += all_sure;
     tie_before += all_tie;
     __syncthreads();  // the counts are free, the row and these weights read
+  };
+  if constexpr (KEPT > 0) {
+#pragma unroll
+    for (int turn = 0; turn < kTurns; ++turn) {
+      if (turn * kLook * kChoose >= len) continue;
+      float x[kLook];
+#pragma unroll
+      for (int i = 0; i < kLook; ++i) x[i] = mine[turn * kLook + i];
+      number(turn * kLook * kChoose, x);
+    }
+  } else {
+    for (int at = 0; at < len; at += kLook * kChoose) {
+      float x[kLook];
+#pragma unroll
+      for (int i = 0; i < kLook; ++i) {
+        const int j = at + i * kChoose + threadIdx.x;
+        x[i] = j < len ? w[j] : 0.0f;
+      }
+      number(at, x);
+    }
   }
   for (int j = n + threadIdx.x; j < len; j += kChoose) w_out[j] = 0.0f;
   const int stay = (n + (1 << p.page_shift) - 1) >> p.page_shift;
@@ -186,48 +243,91 @@ __global__ __launch_bounds__(kChoose) void k_evict_choose(EvictArgs a) {
   }
 }
 
+// A slot of 16384 tokens takes 72 us where its weights are read again for each digit of
+// eight bits.
+__global__ __launch_bounds__(kChoose) void k_evict_choose(EvictArgs a) {
+  const PagesArgs& p = a.p;
+  const int held_len = p.lens[blockIdx.x];
+  const int len = held_len < 0 ? 0 : (held_len < a.most ? held_len : a.most);
+  const int held = (len + (1 << p.page_shift) - 1) >> p.page_shift;
+  if (len <= 4 * kChoose) choose_tokens<4>(a, len, held);
+  else if (len <= 16 * kChoose) choose_tokens<16>(a, len, held);
+  else choose_tokens<0>(a, len, held);
+}
+
 // One block of 16 tokens on its way: lane l = 16 g + n has 16-byte pieces of keys,
 // the codes of its part of four values, and scale bytes of token n.
 template <int D>
 struct MovedBlock {
   static constexpr int kKeys = D == 256 ? 2 : 1, kScales = D == 256 ? 4 : 2, kPart = D / 32;
   u32x4_t k[kKeys];
-  uint64_t v[4];      // kPart bytes each
-  uint8_t s[kScales]; // keys', then values'
+  typename std::conditional<D == 256, uint64_t, uint32_t>::type v[4];  // kPart bytes each
+  uint32_t s[kScales];  // bytes: keys', then values'
+  uint32_t none;        // pieces of tokens that are none: keys', four values', scales'
 
   static __device__ __forceinline__ int key_token(int lane, int i) { return (i * 64 + lane) / (D / 32); }
   static __device__ __forceinline__ bool key_lane(int lane) { return D >= 128 || lane < 32; }
   // byte among the scales of a block, its token being lane % 16
   static __device__ __forceinline__ int scale_at(int lane, int i) { return i * 64 + lane; }
 
-  // from: where the block's tokens lie, `held` of them
-  __device__ __forceinline__ void read(const uint8_t* base, const int64_t* from, int held, int lane) {
-    auto place = [&](int t) { return t < held ? from[t] : -1; };
+  // where the block's tokens lie, `held` of them: of the lane's pieces of keys, its four
+  // tokens' values and its scales' token; -1 for what is none
+  struct Places {
+    int64_t k[kKeys], v[4], s;
+  };
+  static __device__ __forceinline__ Places places(const int64_t* from, int held, int lane) {
+    Places f;
+    auto place = [&](int t) {
+      const int64_t x = from[t < held ? t : 0];
+      return t < held ? x : -1;
+    };
 #pragma unroll
-    for (int i = 0; i < kKeys; ++i) {
-      k[i] = u32x4_t{0u, 0u, 0u, 0u};
-      const int64_t f = key_lane(lane) ? place(key_token(lane, i)) : -1;
-      if (f >= 0)
-        k[i] = *reinterpret_cast<const u32x4_t*>(base + (f & ~15) + (f & 15) * (D / 2) + (i * 64 + lane) % (D / 32) * 16);
-    }
+    for (int i = 0; i < kKeys; ++i) f.k[i] = place(key_token(lane, i));
+#pragma unroll
+    for (int t = 0; t < 4; ++t) f.v[t] = place(lane / 16 * 4 + t);
+    f.s = place(lane & 15);
+    return f;
+  }
+  // (loads of every lane, from the first block where a token is none, so that nothing waits
+  // for a branch)
+  __device__ __forceinline__ void read(const uint8_t* base, const Places& f, int lane) {
+    auto block = [&](int64_t x) { return base + (x < 0 ? 0 : x & ~int64_t(15)); };
+    auto token = [&](int64_t x) { return (int)x & 15; };
+    none = (f.s < 0 ? 64u : 0u);
+#pragma unroll
+    for (int i = 0; i < kKeys; ++i) none |= f.k[i] < 0 ? 1u << i : 0u;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) none |= f.v[t] < 0 ? 4u << t : 0u;
+#pragma unroll
+    for (int i = 0; i < kKeys; ++i)
+      k[i] = *reinterpret_cast<const u32x4_t*>(block(f.k[i]) + token(f.k[i]) * (D / 2) + (i * 64 + lane) % (D / 32) * 16);
     const int part = lane & 15;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const int64_t f = place(lane / 16 * 4 + t);
-      v[t] = 0;
-      if (f >= 0) {
-        const uint8_t* at = base + (f & ~15) + 8 * D + (((f & 15) >> 2) * 16 + part) * (D / 8) + (f & 3) * kPart;
-        if constexpr (D == 64) v[t] = *reinterpret_cast<const uint16_t*>(at);
-        else if constexpr (D == 128) v[t] = *reinterpret_cast<const uint32_t*>(at);
-        else v[t] = *reinterpret_cast<const uint64_t*>(at);
-      }
+      const uint8_t* at = block(f.v[t]) + 8 * D + ((token(f.v[t]) >> 2) * 16 + part) * (D / 8) + (token(f.v[t]) & 3) * kPart;
+      if constexpr (D == 64) v[t] = *reinterpret_cast<const uint16_t*>(at);
+      else if constexpr (D == 128) v[t] = *reinterpret_cast<const uint32_t*>(at);
+      else v[t] = *reinterpret_cast<const uint64_t*>(at);
     }
-    const int64_t f = place(lane & 15);
+#pragma unroll
+    for (int i = 0; i < kScales; ++i) s[i] = block(f.s)[16 * D + scale_at(lane, i) % D / 16 * 16 + token(f.s)];
+  }
+  // Waits for the loads; a token that is none is zeros.
+  __device__ __forceinline__ void arrive() {
+#pragma unroll
+    for (int i = 0; i < kKeys; ++i) {
+      asm volatile("" : "+v"(k[i]));
+      if (none >> i & 1) k[i] = u32x4_t{0u, 0u, 0u, 0u};
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      asm volatile("" : "+v"(v[t]));
+      if (none >> (2 + t) & 1) v[t] = 0;
+    }
 #pragma unroll
     for (int i = 0; i < kScales; ++i) {
-      const int b = scale_at(lane, i);
-      s[i] = 0;
-      if (f >= 0 && b < D) s[i] = base[(f & ~15) + 16 * D + b / 16 * 16 + (f & 15)];
+      asm volatile("" : "+v"(s[i]));
+      if (none >> 6 & 1) s[i] = 0;
     }
   }
   // tokens past `held` stay as they are
@@ -247,7 +347,7 @@ struct MovedBlock {
 #pragma unroll
     for (int i = 0; i < kScales; ++i) {
       const int b = scale_at(lane, i);
-      if (b < D && (lane & 15) < held) block[16 * D + b] = s[i];
+      if (b < D && (lane & 15) < held) block[16 * D + b] = (uint8_t)s[i];
     }
   }
 };
@@ -263,25 +363,55 @@ __global__ __launch_bounds__(64 * kMoveWaves) void k_evict_move(EvictArgs a, int
     const int64_t rest = u / a.heads;
     const int layer = (int)(rest % p.layers), slot = (int)(rest / p.layers);
     const EvictSlot at = a.slots[slot];
-    const int32_t* row = p.table + (int64_t)slot * p.ld_table;
+    // (read as constants, by scalar loads, which the vector loads on their way do not hold up)
+    const auto* row = (const __attribute__((address_space(4))) int32_t*)(p.table + (int64_t)slot * p.ld_table);
     const int64_t* from = a.from + (int64_t)slot * a.most;
     const int per_head = (1 << p.page_shift) / kKvBlock;
     uint8_t* base = p.pool + layer * p.layer_stride + (int64_t)head * per_head * a.block_bytes;
-    for (int first = at.start & ~(kKvBlock - 1); first < at.len; first += kMoveWaves * kMoveBlocks * kKvBlock) {
-      MovedBlock<D> b[kMoveBlocks];
-      const int mine = first + wave * kMoveBlocks * kKvBlock;
-#pragma unroll
-      for (int i = 0; i < kMoveBlocks; ++i) b[i].read(base, from + mine + i * kKvBlock, at.len - mine - i * kKvBlock, lane);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // read, in every wave, before any of it is written
-      __syncthreads();
+    // A chunk's places are asked for two chunks ahead, its tokens one ahead.
+    constexpr int CHUNK = kMoveWaves * kMoveBlocks * kKvBlock;
+    using Block = MovedBlock<D>;
+    struct Chunk {
+      Block b[kMoveBlocks];
+      typename Block::Places f[kMoveBlocks];
+    };
+    if (at.start >= at.len) continue;
+    auto ask = [&](int t0, Chunk& x) {
 #pragma unroll
       for (int i = 0; i < kMoveBlocks; ++i) {
-        const int t = mine + i * kKvBlock;
+        const int t = t0 + i * kKvBlock;
+        x.f[i] = Block::places(from + (t < at.len ? t : 0), at.len - t, lane);
+      }
+    };
+    auto fetch = [&](Chunk& x) {
+#pragma unroll
+      for (int i = 0; i < kMoveBlocks; ++i) x.b[i].read(base, x.f[i], lane);
+    };
+    auto move = [&](int t0, Chunk& now, Chunk& next) {
+      // (asked for before: loads end in their order)
+      ask(t0 + 2 * CHUNK, now);
+      fetch(next);
+#pragma unroll
+      for (int i = 0; i < kMoveBlocks; ++i) now.b[i].arrive();
+      __syncthreads();  // read, in every wave, before any of it is written
+#pragma unroll
+      for (int i = 0; i < kMoveBlocks; ++i) {
+        const int t = t0 + i * kKvBlock;
         const int page = t < at.len ? row[t >> p.page_shift] : -1;
         if ((unsigned)page < (unsigned)p.n_pages)
-          b[i].write(base + page * p.page_stride + ((t & ((1 << p.page_shift) - 1)) / kKvBlock) * a.block_bytes, at.len - t, lane);
+          now.b[i].write(base + page * p.page_stride + ((t & ((1 << p.page_shift) - 1)) / kKvBlock) * a.block_bytes, at.len - t, lane);
       }
+    };
+    const int first = at.start & ~(kKvBlock - 1), mine = wave * kMoveBlocks * kKvBlock;
+    Chunk x, y;
+    ask(first + mine, x);
+    ask(first + mine + CHUNK, y);
+    fetch(x);
+    for (int t0 = first; t0 < at.len; t0 += 2 * CHUNK) {
+      move(t0 + mine, x, y);
+      if (t0 + CHUNK < at.len) move(t0 + mine + CHUNK, y, x);
     }
+    __syncthreads();  // (the next unit's tokens are other bytes, but its waves may not run ahead of these)
   }
 }
 
