@@ -352,10 +352,15 @@ struct MovedBlock {
   }
 };
 
-constexpr int kMoveWaves = 8, kMoveBlocks = 2;  // waves of a workgroup, blocks of a wave at a time
+// Waves of a workgroup, a block of tokens each at a time: two where there are many
+// workgroups, which leaves more of them room (8192 units of 64 dimensions: 2.2 GB in 442 us,
+// 5.0 TB/s, 482 with eight waves), eight where few have to take a slot's tokens faster
+// (1024 units of 128 dimensions 43 -> 38 us).  Two blocks a wave cost registers and
+// starts: 527 us.
+constexpr int64_t kManyUnits = 4096;
 
-template <int D>
-__global__ __launch_bounds__(64 * kMoveWaves) void k_evict_move(EvictArgs a, int64_t units) {
+template <int D, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_evict_move(EvictArgs a, int64_t units) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const PagesArgs& p = a.p;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
@@ -369,50 +374,42 @@ __global__ __launch_bounds__(64 * kMoveWaves) void k_evict_move(EvictArgs a, int
     const int per_head = (1 << p.page_shift) / kKvBlock;
     uint8_t* base = p.pool + layer * p.layer_stride + (int64_t)head * per_head * a.block_bytes;
     // A chunk's places are asked for two chunks ahead, its tokens one ahead.
-    constexpr int CHUNK = kMoveWaves * kMoveBlocks * kKvBlock;
+    constexpr int CHUNK = WAVES * kKvBlock;
     using Block = MovedBlock<D>;
     struct Chunk {
-      Block b[kMoveBlocks];
-      typename Block::Places f[kMoveBlocks];
+      Block b;
+      typename Block::Places f;
     };
     if (at.start >= at.len) continue;
-    auto ask = [&](int t0, Chunk& x) {
-#pragma unroll
-      for (int i = 0; i < kMoveBlocks; ++i) {
-        const int t = t0 + i * kKvBlock;
-        x.f[i] = Block::places(from + (t < at.len ? t : 0), at.len - t, lane);
-      }
-    };
-    auto fetch = [&](Chunk& x) {
-#pragma unroll
-      for (int i = 0; i < kMoveBlocks; ++i) x.b[i].read(base, x.f[i], lane);
-    };
-    auto move = [&](int t0, Chunk& now, Chunk& next) {
+    auto ask = [&](int t, Chunk& x) { x.f = Block::places(from + (t < at.len ? t : 0), at.len - t, lane); };
+    auto move = [&](int t, Chunk& now, Chunk& next) {
       // (asked for before: loads end in their order)
-      ask(t0 + 2 * CHUNK, now);
-      fetch(next);
-#pragma unroll
-      for (int i = 0; i < kMoveBlocks; ++i) now.b[i].arrive();
+      ask(t + 2 * CHUNK, now);
+      next.b.read(base, next.f, lane);
+      now.b.arrive();
       __syncthreads();  // read, in every wave, before any of it is written
-#pragma unroll
-      for (int i = 0; i < kMoveBlocks; ++i) {
-        const int t = t0 + i * kKvBlock;
-        const int page = t < at.len ? row[t >> p.page_shift] : -1;
-        if ((unsigned)page < (unsigned)p.n_pages)
-          now.b[i].write(base + page * p.page_stride + ((t & ((1 << p.page_shift) - 1)) / kKvBlock) * a.block_bytes, at.len - t, lane);
-      }
+      const int page = t < at.len ? row[t >> p.page_shift] : -1;
+      if ((unsigned)page < (unsigned)p.n_pages)
+        now.b.write(base + page * p.page_stride + ((t & ((1 << p.page_shift) - 1)) / kKvBlock) * a.block_bytes, at.len - t, lane);
     };
-    const int first = at.start & ~(kKvBlock - 1), mine = wave * kMoveBlocks * kKvBlock;
+    const int first = at.start & ~(kKvBlock - 1), mine = wave * kKvBlock;
     Chunk x, y;
     ask(first + mine, x);
     ask(first + mine + CHUNK, y);
-    fetch(x);
+    x.b.read(base, x.f, lane);
     for (int t0 = first; t0 < at.len; t0 += 2 * CHUNK) {
       move(t0 + mine, x, y);
       if (t0 + CHUNK < at.len) move(t0 + mine + CHUNK, y, x);
     }
     __syncthreads();  // (the next unit's tokens are other bytes, but its waves may not run ahead of these)
   }
+}
+
+template <int D>
+void launch_move(const EvictArgs& a, int64_t units, hipStream_t s) {
+  const dim3 grid((unsigned)(units < (1 << 20) ? units : (1 << 20)));
+  if (units >= kManyUnits) launch_kernel(k_evict_move<D, 2>, grid, dim3(128), 0, s, a, units);
+  else launch_kernel(k_evict_move<D, 8>, grid, dim3(512), 0, s, a, units);
 }
 
 size_t pages_evict_scratch(int64_t n_slots, int64_t most) {
@@ -432,10 +429,9 @@ hipError_t launch_pages_evict(int d, int heads, int64_t most, const PagesArgs& p
   a.from = reinterpret_cast<int64_t*>(static_cast<uint8_t*>(workspace) + ((size_t)p.n_slots * sizeof(EvictSlot) + 255) / 256 * 256);
   launch_kernel(k_evict_choose, dim3((unsigned)p.n_slots), dim3(kChoose), 0, s, a);
   const int64_t units = (int64_t)p.n_slots * p.layers * heads;
-  const dim3 grid((unsigned)(units < (1 << 20) ? units : (1 << 20)));
-  if (d == 64) launch_kernel(k_evict_move<64>, grid, dim3(64 * kMoveWaves), 0, s, a, units);
-  else if (d == 128) launch_kernel(k_evict_move<128>, grid, dim3(64 * kMoveWaves), 0, s, a, units);
-  else launch_kernel(k_evict_move<256>, grid, dim3(64 * kMoveWaves), 0, s, a, units);
+  if (d == 64) launch_move<64>(a, units, s);
+  else if (d == 128) launch_move<128>(a, units, s);
+  else launch_move<256>(a, units, s);
   return hipGetLastError();
 }
 
