@@ -66,7 +66,8 @@ __device__ __forceinline__ int threads_before(int x, int* all, int* s_wave) {
 template <int KEPT>
 __device__ __forceinline__ void choose_tokens(const EvictArgs& a, int len, int held) {
   __shared__ uint32_t s_bins[kBins];
-  __shared__ int s_sure[64], s_tie[64], s_wave[16];
+  constexpr int kCounts = KEPT > 0 ? KEPT * 16 : 64;  // of 64 tokens each
+  __shared__ int s_sure[kCounts], s_tie[kCounts], s_wave[16];
   __shared__ int s_shared, s_start, s_digit, s_need;
   const int s = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const PagesArgs& p = a.p;
@@ -82,6 +83,9 @@ __device__ __forceinline__ void choose_tokens(const EvictArgs& a, int len, int h
     const int j = i * kChoose + threadIdx.x;
     mine[i] = j < len ? w[j] : 0.0f;
   }
+  uint32_t order[KEPT > 0 ? KEPT : 1];
+#pragma unroll
+  for (int i = 0; i < KEPT; ++i) order[i] = order_of(mine[i]);
   const int want = a.c.keep[s];
   if (threadIdx.x == 0) {
     s_shared = 0;
@@ -109,14 +113,14 @@ __device__ __forceinline__ void choose_tokens(const EvictArgs& a, int len, int h
 #pragma unroll
     for (int digit = 0; digit < 3; ++digit) {
       const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit == 2 ? 10 : 11;
-      auto count = [&](int j, float x) {
-        const uint32_t o = order_of(x);
+      auto count = [&](int j, uint32_t o) {
         if (j >= front && j < back && (digit == 0 || (o ^ least) >> (shift + bits) == 0))
           atomicAdd(&s_bins[(o >> shift) & ((1 << bits) - 1)], 1u);
       };
       if constexpr (KEPT > 0) {
 #pragma unroll
-        for (int i = 0; i < KEPT; ++i) count(i * kChoose + threadIdx.x, mine[i]);
+        for (int i = 0; i < KEPT; ++i)
+          if (i * kChoose < back) count(i * kChoose + threadIdx.x, order[i]);
       } else {
         for (int j0 = front; j0 < back; j0 += 8 * kChoose) {
           float x[8];
@@ -126,7 +130,7 @@ __device__ __forceinline__ void choose_tokens(const EvictArgs& a, int len, int h
             x[i] = j < back ? w[j] : 0.0f;
           }
 #pragma unroll
-          for (int i = 0; i < 8; ++i) count(j0 + i * kChoose + threadIdx.x, x[i]);
+          for (int i = 0; i < 8; ++i) count(j0 + i * kChoose + threadIdx.x, order_of(x[i]));
         }
       }
       __syncthreads();
@@ -148,88 +152,106 @@ __device__ __forceinline__ void choose_tokens(const EvictArgs& a, int len, int h
   }
 
   // numbers of the kept ones, in order; equal weights are kept from the first on
-  int sure_before = 0, tie_before = 0;
-  constexpr int kTurns = KEPT > 0 ? KEPT / kLook : 1;
-  auto number = [&](int at, const float (&x)[kLook]) {
-    int page[kLook];
-    uint64_t sure[kLook], tie[kLook];
+  auto is_sure = [&](int j, uint32_t o) {
+    return j < len && (n == len || j < front || j >= back || (need > 0 && o > least));
+  };
+  auto is_tie = [&](int j, uint32_t o) { return n < len && need > 0 && j >= front && j < back && o == least; };
+  const uint64_t below = (uint64_t(1) << lane) - 1;
+  int start = len;  // the first that goes
+  // token j of weight x, with `sure` certain and `tie` equal ones before its 64
+  auto give = [&](int j, float x, uint32_t o, int page, int sure_before, int tie_before) {
+    const bool sure = is_sure(j, o), tie = is_tie(j, o);
+    const uint64_t sures = __ballot(sure), ties = __ballot(tie);
+    const int t = tie_before + __popcll(ties & below);
+    const int to = sure_before + __popcll(sures & below) + (t < need ? t : need);
+    if (sure || (tie && t < need)) {
+      const int in_page = j & ((1 << p.page_shift) - 1);
+      from[to] = (unsigned)page < (unsigned)p.n_pages
+                     ? (page * p.page_stride + (in_page / kKvBlock) * a.block_bytes) | (in_page % kKvBlock)
+                     : -1;
+      w_out[to] = x;
+      if (kept) kept[to] = j;
+    } else if (j < start) {
+      start = j;
+    }
+  };
+  auto number_of = [&](const int* s_count, int* all) {  // this lane's sum of the counts before, in their order
+    int x = s_count[lane];
+    const int its = x;
 #pragma unroll
-    for (int i = 0; i < kLook; ++i) {
-      const int j = at + i * kChoose + threadIdx.x;
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(x, o, 64);
+      if (lane >= o) x += y;
+    }
+    *all = __builtin_amdgcn_readlane(x, 63);
+    return x - its;
+  };
+  if constexpr (KEPT > 0) {
+    int page[KEPT];
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) {
+      const int j = i * kChoose + threadIdx.x;
       page[i] = j < len ? row[j >> p.page_shift] : -1;
     }
 #pragma unroll
-    for (int i = 0; i < kLook; ++i) {
-      const int j = at + i * kChoose + threadIdx.x;
-      bool is_sure = n == len && j < len, is_tie = false;
-      if (j < front || (j >= back && j < len)) is_sure = true;
-      else if (j < len && n < len && need > 0) {
-        const uint32_t o = order_of(x[i]);
-        is_sure = o > least;
-        is_tie = o == least;
-      }
-      sure[i] = __ballot(is_sure);
-      tie[i] = __ballot(is_tie);
+    for (int i = 0; i < KEPT; ++i) {
+      const int j = i * kChoose + threadIdx.x;
+      const uint64_t sures = __ballot(is_sure(j, order[i])), ties = __ballot(is_tie(j, order[i]));
       if (lane == 0) {
-        s_sure[i * 16 + wave] = __popcll(sure[i]);
-        s_tie[i * 16 + wave] = __popcll(tie[i]);
+        s_sure[i * 16 + wave] = __popcll(sures);
+        s_tie[i * 16 + wave] = __popcll(ties);
       }
     }
     __syncthreads();
-    int ns = s_sure[lane], nt = s_tie[lane];
-    const int ms = ns, mt = nt;
+    int sure_before = 0, tie_before = 0;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(ns, o, 64), z = __shfl_up(nt, o, 64);
-      if (lane >= o) ns += y, nt += z;
-    }
-    const int all_sure = __builtin_amdgcn_readlane(ns, 63), all_tie = __builtin_amdgcn_readlane(nt, 63);
-    ns -= ms;
-    nt -= mt;
-    const uint64_t below = (uint64_t(1) << lane) - 1;
-    int start = len;
+    for (int k = 0; k < KEPT / 4; ++k) {  // (64 counts are four turns of the 16 waves)
+      int all_sure = 0, all_tie = 0;
+      const int ns = number_of(s_sure + 64 * k, &all_sure), nt = number_of(s_tie + 64 * k, &all_tie);
 #pragma unroll
-    for (int i = 0; i < kLook; ++i) {
-      const int j = at + i * kChoose + threadIdx.x;
-      const int t = tie_before + __shfl(nt, i * 16 + wave, 64) + __popcll(tie[i] & below);
-      const int to = sure_before + __shfl(ns, i * 16 + wave, 64) + __popcll(sure[i] & below) + (t < need ? t : need);
-      const bool stays = (sure[i] >> lane & 1) || ((tie[i] >> lane & 1) && t < need);
-      if (stays) {
-        const int in_page = j & ((1 << p.page_shift) - 1);
-        from[to] = (unsigned)page[i] < (unsigned)p.n_pages
-                       ? (page[i] * p.page_stride + (in_page / kKvBlock) * a.block_bytes) | (in_page % kKvBlock)
-                       : -1;
-        w_out[to] = x[i];
-        if (kept) kept[to] = j;
-      } else if (j < start) {
-        start = j;
+      for (int i = 4 * k; i < 4 * k + 4; ++i) {
+        const int at = i % 4 * 16 + wave;
+        if (i * kChoose < len)
+          give(i * kChoose + threadIdx.x, mine[i], order[i], page[i], sure_before + __builtin_amdgcn_readlane(ns, at),
+               tie_before + __builtin_amdgcn_readlane(nt, at));
       }
-    }
-    if (start < len) atomicMin(&s_start, start);
-    sure_before += all_sure;
-    tie_before += all_tie;
-    __syncthreads();  // the counts are free, the row and these weights read
-  };
-  if constexpr (KEPT > 0) {
-#pragma unroll
-    for (int turn = 0; turn < kTurns; ++turn) {
-      if (turn * kLook * kChoose >= len) continue;
-      float x[kLook];
-#pragma unroll
-      for (int i = 0; i < kLook; ++i) x[i] = mine[turn * kLook + i];
-      number(turn * kLook * kChoose, x);
+      sure_before += all_sure;
+      tie_before += all_tie;
     }
   } else {
+    int sure_before = 0, tie_before = 0;
     for (int at = 0; at < len; at += kLook * kChoose) {
       float x[kLook];
+      int page[kLook];
 #pragma unroll
       for (int i = 0; i < kLook; ++i) {
         const int j = at + i * kChoose + threadIdx.x;
         x[i] = j < len ? w[j] : 0.0f;
+        page[i] = j < len ? row[j >> p.page_shift] : -1;
       }
-      number(at, x);
+#pragma unroll
+      for (int i = 0; i < kLook; ++i) {
+        const int j = at + i * kChoose + threadIdx.x;
+        const uint64_t sures = __ballot(is_sure(j, order_of(x[i]))), ties = __ballot(is_tie(j, order_of(x[i])));
+        if (lane == 0) {
+          s_sure[i * 16 + wave] = __popcll(sures);
+          s_tie[i * 16 + wave] = __popcll(ties);
+        }
+      }
+      __syncthreads();  // (these weights are read too, and may be written over)
+      int all_sure = 0, all_tie = 0;
+      const int ns = number_of(s_sure, &all_sure), nt = number_of(s_tie, &all_tie);
+#pragma unroll
+      for (int i = 0; i < kLook; ++i)
+        give(at + i * kChoose + threadIdx.x, x[i], order_of(x[i]), page[i],
+             sure_before + __builtin_amdgcn_readlane(ns, i * 16 + wave), tie_before + __builtin_amdgcn_readlane(nt, i * 16 + wave));
+      sure_before += all_sure;
+      tie_before += all_tie;
+      __syncthreads();  // the counts are free
     }
   }
+  if (start < len) atomicMin(&s_start, start);
+  __syncthreads();  // the row and all weights are read
   for (int j = n + threadIdx.x; j < len; j += kChoose) w_out[j] = 0.0f;
   const int stay = (n + (1 << p.page_shift) - 1) >> p.page_shift;
   for (int c = stay + threadIdx.x; c < held; c += kChoose) {
@@ -251,6 +273,7 @@ __global__ __launch_bounds__(kChoose) void k_evict_choose(EvictArgs a) {
   const int len = held_len < 0 ? 0 : (held_len < a.most ? held_len : a.most);
   const int held = (len + (1 << p.page_shift) - 1) >> p.page_shift;
   if (len <= 4 * kChoose) choose_tokens<4>(a, len, held);
+  else if (len <= 8 * kChoose) choose_tokens<8>(a, len, held);
   else if (len <= 16 * kChoose) choose_tokens<16>(a, len, held);
   else choose_tokens<0>(a, len, held);
 }
