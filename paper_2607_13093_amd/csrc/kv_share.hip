@@ -30,10 +30,17 @@ struct ShareSeg {
   int32_t first, members, from, to;
 };
 
-// An item: tile `tile` of the rows of such sessions over such tokens, place `part` of
-// each row's parts; alone: no other tile reads them; own: of one session.
+// A session of the order: its rows at positions base ..., its row of the table.
+struct SharePlace {
+  int32_t session, slot, base, rows;
+};
+
+// An item: tile `tile` of the rows of such sessions over such tokens, on the pages of
+// row `slot`, which holds `len` of them; place `part` of each row's parts.
 struct ShareItem {
-  int32_t first, members, tile, from, to, part, alone, own;
+  int32_t first, members, tile, from, to, part;
+  int32_t flags;  // 1: no other tile reads the tokens, 2: of one session
+  int32_t slot;
 };
 
 struct ShareHead {
@@ -59,7 +66,7 @@ struct SharePlanArgs {
   int group, window;
   uint32_t key;
   ShareHead* head;
-  int32_t* order;    // [S]: sessions, those of a segment side by side
+  SharePlace* order; // [S]: sessions, those of a segment side by side
   int32_t* parts;    // [S]: parts of a session's rows
   ShareSeg* segs;    // [(levels + 1) S], scratch
   ShareItem* items;  // [cap]
@@ -327,7 +334,8 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
     }
     alike[at] = from;
     low[at] = length[s] > from ? length[s] : from;
-    a.order[at] = limit[at] = s;
+    a.order[at] = SharePlace{s, slot[s], base[s], length[s] - base[s]};
+    limit[at] = s;
   }
   __syncthreads();
   for (int at = threadIdx.x; at < n2; at += kPlanThreads)
@@ -435,7 +443,7 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
       const int64_t to = (int64_t)t.from + (int64_t)(share + 1) * c;
       if (made + x < a.z.cap)
         a.items[made + x] = ShareItem{t.first, t.members, (int)tile, (int)(t.from + share * c), to < t.to ? (int)to : t.to,
-                                      (int)(part_of[i] + share), nt == 1, kind};
+                                      (int)(part_of[i] + share), (nt == 1 ? 1 : 0) | (kind ? 2 : 0), slot[limit[t.first]]};
     }
     made += sum;
     __syncthreads();
@@ -456,7 +464,7 @@ struct ShareArgs {
   bool q_aligned, o_aligned;
   uint32_t key;
   ShareHead* head;
-  const int32_t* order;
+  const SharePlace* order;
   const int32_t* n_parts;
   const ShareItem* items;
   int cap;
@@ -468,7 +476,8 @@ struct ShareArgs {
 // A row of an item: number fq of its sessions' rows.
 struct ShareRow {
   int session, r, in_group;  // in_group: query head of the key/value head's
-  bool is;
+  bool is, live;             // live: it is one of the session's rows
+  int pos;
 };
 __device__ __forceinline__ ShareRow share_row(const ShareArgs& a, const ShareItem& it, int fq, int RG, int G) {
   const int member = fq / RG, x = fq - member * RG;
@@ -477,9 +486,11 @@ __device__ __forceinline__ ShareRow share_row(const ShareArgs& a, const ShareIte
   w.in_group = x - w.r * G;
   const int at = it.first + member;
   w.is = member < it.members && (unsigned)at < (unsigned)a.kv.n_sessions;
-  w.session = w.is ? a.order[at] : 0;
-  w.is = w.is && (unsigned)w.session < (unsigned)a.kv.n_sessions;
-  if (!w.is) w.session = 0;
+  const SharePlace p = a.order[w.is ? at : 0];
+  w.is = w.is && (unsigned)p.session < (unsigned)a.kv.n_sessions;
+  w.session = w.is ? p.session : 0;
+  w.live = w.is && w.r < p.rows;
+  w.pos = p.base + w.r;
   return w;
 }
 
@@ -497,8 +508,9 @@ __device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& 
   const int wt = wave % WT, wr = wave / WT;
   const int G = a.group, RG = a.kv.R * G;
   {
-    const int lead = (unsigned)it.first < (unsigned)a.kv.n_sessions ? a.order[it.first] : 0;
-    const KvSession ses = kv_session(a.kv, (unsigned)lead < (unsigned)a.kv.n_sessions ? lead : 0);
+    // pages of a row of the table; all of its tokens up to it.to are held
+    KvSession ses;
+    ses.table = a.kv.table + ((unsigned)it.slot < (unsigned)a.kv.n_slots ? it.slot : 0) * a.kv.ld_table;
     const int row0 = (it.tile * WR + wr) * 16 * MT;  // the wave's first
 
     u32x4_t* s_q = reinterpret_cast<u32x4_t*>(smem + NW * NS * Stage<D>::kBytes);
@@ -510,13 +522,11 @@ __device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& 
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
       const ShareRow w = share_row(a, it, row0 + m * 16 + n, RG, G);
-      const KvSession its = kv_session(a.kv, w.session);
-      const bool live = w.is && w.r < its.rows;
-      const int at = its.len - its.rows + w.r;
-      pos[m] = live ? at : -1;
+      const bool live = w.live;
+      pos[m] = live ? w.pos : -1;
       if (live) {
-        low = at < low ? at : low;
-        high = at > high ? at : high;
+        low = w.pos < low ? w.pos : low;
+        high = w.pos > high ? w.pos : high;
       }
       const uint16_t* p = a.q + ((int64_t)w.session * a.kv.R + w.r) * a.q_row + (int64_t)(head * G + w.in_group) * a.q_head + g * (D / 4);
 #pragma unroll
@@ -545,8 +555,7 @@ __device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& 
     low = __builtin_amdgcn_readfirstlane(low);
     high = __builtin_amdgcn_readfirstlane(high);
     int from = it.from > 0 ? it.from & ~(kKvBlock - 1) : 0;
-    int to = it.to < high + 1 ? it.to : high + 1;
-    to = to < ses.len ? to : ses.len;
+    const int to = it.to < high + 1 ? it.to : high + 1;
     int all_lo = 0;
     const int all_hi = low < 0 ? 0 : low + 1;
     if (a.window > 0) {
@@ -579,7 +588,7 @@ __device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& 
 
     uint8_t* ring = smem + wave * (NS * Stage<D>::kBytes);
     uint32_t lane16 = lane * 16;
-    const bool alone = WT >= 4 && it.alone;
+    const bool alone = WT >= 4 && (it.flags & 1);
     const uint32_t ring_at = (uint32_t)(uintptr_t)(lds_void_t*)ring;
     // the lane's places in a stage: keys token n of a block, values as they lie
     const uint32_t key_at = n * (D / 2) + g * (D / 8), value_at = KvLayout<D>::kValues + lane * (D / 8);
@@ -648,8 +657,8 @@ __device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& 
       begin();
       mask_scores(sc, pos, a.window, t0, g);
       take_weights(p, w, sc, a.scale_log2);
-      if (t0 + 32 > ses.len) {
-        const int held[2] = {ses.len - t0, ses.len - t0 - kKvBlock};
+      if (t0 + 32 > it.to) {
+        const int held[2] = {it.to - t0, it.to - t0 - kKvBlock};
         clear_values(values, held, g);
       }
       take_values(w, values, p);
@@ -697,7 +706,7 @@ __device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& 
       const int d0 = g * (D / 4) + wt * PER;  // the first of them
       const ShareRow row = share_row(a, it, row0 + m * 16 + n, RG, G);
       if (row.is && (unsigned)it.part < (unsigned)a.parts) {
-        if (row.r >= kv_session(a.kv, row.session).rows) l = 0.0f;  // a row that is none
+        if (!row.live) l = 0.0f;
         const int64_t at = (((int64_t)row.session * a.kv.R + row.r) * (a.kv.heads * G) + head * G + row.in_group) * a.parts + it.part;
         if (g == 0 && wt == 0) a.part_ml[at] = make_float2(t, l);
         if (!(l == 0.0f)) {
@@ -736,7 +745,7 @@ __global__ __launch_bounds__(64 * waves_in(WT), share_waves(D, MT, WT)) void k_s
     const int head = unit % a.kv.heads;
     const auto* x8 = (const __attribute__((address_space(4))) int32_t*)(a.items + unit / a.kv.heads);
     const ShareItem it{x8[0], x8[1], x8[2], x8[3], x8[4], x8[5], x8[6], x8[7]};
-    if (OWN == MT || !it.own) share_item<D, MT, WT>(a, it, head, smem);
+    if (OWN == MT || !(it.flags & 2)) share_item<D, MT, WT>(a, it, head, smem);
     else share_item<D, OWN, WT>(a, it, head, smem);
     __syncthreads();  // the outputs in LDS are read, the next unit is known
     unit = __builtin_amdgcn_readfirstlane(s_next);
@@ -812,13 +821,16 @@ ShareSizes share_sizes(int d, int64_t S, int64_t R, int64_t heads, int64_t group
   z.mt[0] = d == 256 ? 2 : 4;
   z.wt = d == 256 ? 8 : 4;
   z.mt[1] = RG <= 16 ? 1 : d == 256 || RG <= 32 ? 2 : 4;
+  // Parts of a row beyond one for each segment: as many as some hundred megabytes of them
+  // allow, so that few rows can be cut often.
+  const int64_t rows = S * RG * heads, shares = (max_len + kShareLeast - 1) / kShareLeast;
   if (S * RG > 65536) {  // prompts: nothing to cut
     z.levels = 1;
     z.extra = 0;
   } else {
     z.levels = kShareLevels;
-    const int64_t shares = (max_len + kShareLeast - 1) / kShareLeast;  // that there can be
-    z.extra = S >= 64 ? 2 : S >= 16 ? 8 : S >= 4 ? 24 : 56;
+    const int64_t most = (1 << 18) / rows;
+    z.extra = (int)(most < 2 ? 2 : most > 56 ? 56 : most);
     if (z.extra > shares) z.extra = (int)shares;
   }
   z.parts = z.levels + 1 + z.extra;
@@ -846,7 +858,7 @@ SharePlaces share_places(const ShareSizes& z, int64_t S) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   SharePlaces p{};
   p.order = up(sizeof(ShareHead));
-  p.parts = p.order + up(S * 4);
+  p.parts = p.order + up(S * sizeof(SharePlace));
   p.segs = p.parts + up(S * 4);
   p.items = p.segs + up((z.levels + 1) * S * sizeof(ShareSeg));
   p.all = p.items + up(z.cap * sizeof(ShareItem));
@@ -900,7 +912,7 @@ hipError_t launch_share_plan(int d, const KvArgs& kv, int q_heads, int window, i
   const SharePlaces p = share_places(a.z, kv.n_sessions);
   uint8_t* base = static_cast<uint8_t*>(plan);
   a.head = reinterpret_cast<ShareHead*>(base);
-  a.order = reinterpret_cast<int32_t*>(base + p.order);
+  a.order = reinterpret_cast<SharePlace*>(base + p.order);
   a.parts = reinterpret_cast<int32_t*>(base + p.parts);
   a.segs = reinterpret_cast<ShareSeg*>(base + p.segs);
   a.items = reinterpret_cast<ShareItem*>(base + p.items);
@@ -934,7 +946,7 @@ hipError_t launch_attend_shared(int d, const KvArgs& kv, const AttendCall& c, vo
   uint8_t* base = static_cast<uint8_t*>(plan);
   a.key = share_key(d, kv, a.group, c.window, z.extra);
   a.head = reinterpret_cast<ShareHead*>(base);
-  a.order = reinterpret_cast<const int32_t*>(base + p.order);
+  a.order = reinterpret_cast<const SharePlace*>(base + p.order);
   a.n_parts = reinterpret_cast<const int32_t*>(base + p.parts);
   a.parts = z.parts;
   const int64_t rows = (int64_t)kv.n_sessions * kv.R * c.q_heads;
