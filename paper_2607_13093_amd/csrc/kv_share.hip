@@ -24,6 +24,7 @@ constexpr int kShareStep = 128;   // tokens that shares are multiples of
 constexpr int kShareLeast = 256;  // and at least
 // Tokens whose reading a segment has to save: a part of every row costs about as much.
 constexpr int kShareWorth = 256;
+constexpr float kShareItem = 8.0f;  // us of an item beside its tokens
 
 // Tokens from ... to - 1 of `members` sessions from place `first` of the order.
 struct ShareSeg {
@@ -57,6 +58,7 @@ struct ShareSizes {
   int mt[2], wt;      // row tiles of a wave on shared segments and on own ones, waves that share them
   int rows[2];        // of a tile of an item
   int slots;          // workgroups that run at a time
+  float us[2];        // of one of them for a token of an item
   int cap;            // items at most
 };
 
@@ -342,53 +344,51 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
     key[at] = at < S ? (uint64_t)(uint32_t)(kKvMost - (low[at] - alike[at])) << 12 | (uint64_t)at : ~uint64_t(0);
   sort_keys(key, n2);
 
-  // Shares, of each kind the shortest that fill the device about once: eight waves
-  // sum up a kind's items for a candidate each.
+  // Shares: each wave tries a length of its own, in time, and what all items then take,
+  // kShareItem more than their tokens each.
   const int RG = a.kv.R * a.group, row_shift[2] = {__ffs(a.z.rows[0]) - 1, __ffs(a.z.rows[1]) - 1};
   auto tiles_of = [&](int members, int kind) { return (int)(((uint32_t)members * RG + a.z.rows[kind] - 1) >> row_shift[kind]); };
+  const int room = a.z.extra > 0 ? (longest + a.z.extra - 1) / a.z.extra : longest;
+  auto chunk_of = [&](int kind, int candidate) {
+    const float us = (float)(2 << (candidate / 2)) * (candidate & 1 ? 1.5f : 1.0f);  // 2, 3, 4, 6 ... 384
+    const float c = us / a.z.us[kind];
+    int n = c < (float)longest ? (int)c : longest;
+    n = n > room ? n : room;
+    n = n > kShareLeast ? n : kShareLeast;
+    return (n + kShareStep - 1) / kShareStep * kShareStep;
+  };
   {
-    const int kind = wave >> 3, candidate = wave & 7;
-    const int n = kind ? S : shared;
-    auto segment = [&](int i) { return kind ? ShareSeg{i, 1, alike[i], low[i]} : a.segs[i]; };
-    // (in floating point: the number of shares is free)
-    float load = 0.0f, tiles = 0.0f;
-    for (int i = lane; i < n; i += 64) {
-      const ShareSeg t = segment(i);
-      const float k = (float)tiles_of(t.members, kind);
-      tiles += k;
-      load += k * (float)(t.to - t.from);
+    float load = 0.0f, items = 0.0f, most = 0.0f;
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+      const int n = kind ? S : shared, c = chunk_of(kind, wave);
+      for (int i = lane; i < n; i += 64) {
+        const ShareSeg t = kind ? ShareSeg{i, 1, alike[i], low[i]} : a.segs[i];
+        const float k = (float)tiles_of(t.members, kind);
+        const int tokens = t.to - t.from;
+        load += k * (float)tokens * a.z.us[kind];
+        items += k * (float)((uint32_t)(tokens + c - 1) / (uint32_t)c);
+        most = fmaxf(most, (float)(tokens < c ? tokens : c) * a.z.us[kind]);
+      }
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
       load += __shfl_xor(load, o, 64);
-      tiles += __shfl_xor(tiles, o, 64);
+      items += __shfl_xor(items, o, 64);
+      most = fmaxf(most, __shfl_xor(most, o, 64));
     }
-    load *= (float)a.kv.heads;
-    tiles *= (float)a.kv.heads;
+    items *= (float)a.kv.heads;
+    load = load * (float)a.kv.heads + items * kShareItem;
     const float slots = (float)a.z.slots;
-    const bool few = tiles < 2 * slots;
-    const float target = 2 * tiles <= slots ? slots : 2 * slots;
-    float c = few ? load * (0.125f * (8 + 2 * candidate)) / target : load / slots;
-    const int room = a.z.extra > 0 ? (longest + a.z.extra - 1) / a.z.extra : longest;
-    const bool last = !few || candidate == 7;
-    if (few && last) c = (float)longest;
-    int chunk = c < (float)longest ? (int)c : longest;
-    chunk = chunk > room ? chunk : room;
-    chunk = chunk > kShareLeast ? chunk : kShareLeast;
-    chunk = (chunk + kShareStep - 1) / kShareStep * kShareStep;
-    float items = 0.0f;
-    for (int i = lane; i < n; i += 64) {
-      const ShareSeg t = segment(i);
-      items += (float)(tiles_of(t.members, kind) * ((uint32_t)(t.to - t.from + chunk - 1) / (uint32_t)chunk));
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) items += __shfl_xor(items, o, 64);
-    if (lane == 0) s_chunk[wave] = last || items * a.kv.heads <= target ? chunk : INT32_MAX;
+    // (the last items fill their places to half)
+    const float us = items <= slots ? most + kShareItem : load / slots + 0.5f * (most + kShareItem);
+    if (lane == 0) s_chunk[wave] = (int)(us * 16.0f);
   }
   __syncthreads();
-  int chunk[2] = {INT32_MAX, INT32_MAX};
+  int best = 0;
 #pragma unroll
-  for (int k = 0; k < 16; ++k) chunk[k >> 3] = s_chunk[k] < chunk[k >> 3] ? s_chunk[k] : chunk[k >> 3];
+  for (int k = 1; k < 16; ++k) best = s_chunk[k] < s_chunk[best] ? k : best;
+  const int chunk[2] = {chunk_of(0, best), chunk_of(1, best)};
 
   // Parts of each segment, level by level along the paths, and the items, one a
   // thread, which looks for its segment in the sums of them.
@@ -513,6 +513,27 @@ __device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& 
     ses.table = a.kv.table + ((unsigned)it.slot < (unsigned)a.kv.n_slots ? it.slot : 0) * a.kv.ld_table;
     const int row0 = (it.tile * WR + wr) * 16 * MT;  // the wave's first
 
+    // Without a window the first tiles are known before the rows are: they come while
+    // those are looked up.  (The rows may see fewer of them: waits are for the newest.)
+    constexpr int STEP = 32 * WT;
+    int from = it.from > 0 ? it.from & ~(kKvBlock - 1) : 0;
+    uint8_t* ring = smem + wave * (NS * Stage<D>::kBytes);
+    uint32_t lane16 = lane * 16;
+    const bool alone = WT >= 4 && (it.flags & 1);
+    uint32_t none = 0;  // of the tiles in flight, the next in the low bits: blocks without a page
+    auto none_of = [](const KvPages& p) { return (uint32_t)(p.page[0] < 0) | ((uint32_t)(p.page[1] < 0) << 1); };
+    if (a.window == 0) {
+#pragma unroll
+      for (int i = 0; i < NS - 1; ++i) {
+        const int at = from + 32 * wt + i * STEP;
+        if (at < it.to) {
+          const KvPages pages = tile_pages(a.kv, ses, at, it.to);
+          none |= none_of(pages) << (2 * i);
+          copy_tile<D>(ring + i * Stage<D>::kBytes, a.kv, head, at, pages, lane16, lane, alone);
+        }
+      }
+    }
+
     u32x4_t* s_q = reinterpret_cast<u32x4_t*>(smem + NW * NS * Stage<D>::kBytes);
     Queries<D, MT, QL> q;
     q.l = s_q;
@@ -554,7 +575,6 @@ __device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& 
     }
     low = __builtin_amdgcn_readfirstlane(low);
     high = __builtin_amdgcn_readfirstlane(high);
-    int from = it.from > 0 ? it.from & ~(kKvBlock - 1) : 0;
     const int to = it.to < high + 1 ? it.to : high + 1;
     int all_lo = 0;
     const int all_hi = low < 0 ? 0 : low + 1;
@@ -574,7 +594,6 @@ __device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& 
     }
 
     // The wave's tiles as in kv_attend.hip: those that all its rows see whole first.
-    constexpr int STEP = 32 * WT;
     const int start = from + 32 * wt;
     int whole = start + (all_lo > start ? (all_lo - start + STEP - 1) / STEP * STEP : 0);
     int part = whole + ((all_hi < to ? all_hi : to) - whole + STEP - 32) / STEP * STEP;
@@ -586,23 +605,20 @@ __device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& 
       return k < n_whole ? whole + k * STEP : (k < n_whole + n_head ? start : part - n_head * STEP) + (k - n_whole) * STEP;
     };
 
-    uint8_t* ring = smem + wave * (NS * Stage<D>::kBytes);
-    uint32_t lane16 = lane * 16;
-    const bool alone = WT >= 4 && (it.flags & 1);
     const uint32_t ring_at = (uint32_t)(uintptr_t)(lds_void_t*)ring;
     // the lane's places in a stage: keys token n of a block, values as they lie
     const uint32_t key_at = n * (D / 2) + g * (D / 8), value_at = KvLayout<D>::kValues + lane * (D / 8);
     const uint32_t ks_at = Stage<D>::kCodes + (D == 64 ? g >> 1 : D == 128 ? g : 2 * g) * kKvBlock + n;
     const uint32_t vs_at = Stage<D>::kCodes + D / 2 + n * D / 512 * kKvBlock + 4 * g;
-    uint32_t none = 0;  // of the tiles in flight, the next in the low bits: blocks without a page
-    auto none_of = [](const KvPages& p) { return (uint32_t)(p.page[0] < 0) | ((uint32_t)(p.page[1] < 0) << 1); };
+    if (a.window > 0) {
 #pragma unroll
-    for (int i = 0; i < NS - 1; ++i)
-      if (i < n_tiles) {
-        const KvPages pages = tile_pages(a.kv, ses, place(i), to);
-        none |= none_of(pages) << (2 * i);
-        copy_tile<D>(ring + i * Stage<D>::kBytes, a.kv, head, place(i), pages, lane16, lane, alone);
-      }
+      for (int i = 0; i < NS - 1; ++i)
+        if (i < n_tiles) {
+          const KvPages pages = tile_pages(a.kv, ses, place(i), to);
+          none |= none_of(pages) << (2 * i);
+          copy_tile<D>(ring + i * Stage<D>::kBytes, a.kv, head, place(i), pages, lane16, lane, alone);
+        }
+    }
     if constexpr (QL) __syncthreads();
     else  // here, not in the loop: the compiler's wait would be for all copies in flight
 #pragma unroll
@@ -667,8 +683,10 @@ __device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& 
     for (int m = 0; m < MT; ++m) w.sum[m] = sum_over_groups(w.sum[m]);
 
     // the waves' outputs, in what were rings
-    float* s_o = reinterpret_cast<float*>(smem);       // NW x 16 D
+    constexpr int VP = VC / WT;  // of its D/16 columns of outputs, those that a wave ends with
+    f32x4_t* s_o = reinterpret_cast<f32x4_t*>(smem);   // [NW][VC][64 lanes]
     float* s_ml = reinterpret_cast<float*>(smem) + NW * 16 * D;
+    wait_copies<0>();  // tiles that no row saw
     __syncthreads();
     if (g == 0)
 #pragma unroll
@@ -679,7 +697,6 @@ __device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& 
     __syncthreads();
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      constexpr int PER = D / 4 / WT;  // values a lane ends with
       float t = kNoScore, l = 0.0f;
 #pragma unroll
       for (int k = 0; k < WT; ++k) t = fmaxf(t, s_ml[(((wr * WT + k) * MT + m) * 16 + n) * 2]);
@@ -691,19 +708,15 @@ __device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& 
       const float f = __builtin_amdgcn_exp2f(w.top[m] - t);
       if (m > 0) __syncthreads();
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int c = 0; c < VC; ++c) s_o[((wave * 4 + e) * VC + c) * 64 + lane] = w.o[m][c][e] * f;
+      for (int c = 0; c < VC; ++c) s_o[(wave * VC + c) * 64 + lane] = w.o[m][c] * f;
       __syncthreads();
-      float y[PER];
+      f32x4_t y[VP];
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        float x = 0.0f;
+      for (int i = 0; i < VP; ++i) {
+        y[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int k = 0; k < WT; ++k) x += s_o[((wr * WT + k) * 4 * VC + wt * PER + i) * 64 + lane];
-        y[i] = x;
+        for (int k = 0; k < WT; ++k) y[i] += s_o[((wr * WT + k) * VC + wt * VP + i) * 64 + lane];
       }
-      const int d0 = g * (D / 4) + wt * PER;  // the first of them
       const ShareRow row = share_row(a, it, row0 + m * 16 + n, RG, G);
       if (row.is && (unsigned)it.part < (unsigned)a.parts) {
         if (!row.live) l = 0.0f;
@@ -711,8 +724,8 @@ __device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& 
         if (g == 0 && wt == 0) a.part_ml[at] = make_float2(t, l);
         if (!(l == 0.0f)) {
 #pragma unroll
-          for (int i = 0; i < PER; i += 4)
-            *reinterpret_cast<f32x4_t*>(a.part_o + at * D + d0 + i) = f32x4_t{y[i], y[i + 1], y[i + 2], y[i + 3]};
+          for (int i = 0; i < VP; ++i)
+            *reinterpret_cast<f32x4_t*>(a.part_o + at * D + ((g * VC) + wt * VP + i) * 4) = y[i];
         }
       }
     }
@@ -753,11 +766,13 @@ __global__ __launch_bounds__(64 * waves_in(WT), share_waves(D, MT, WT)) void k_s
   }
 }
 
-// A row's parts joined, in their order; D/4 lanes a row and head.
+// A row's parts joined, in their order, by D/16 lanes a row and head.  Parts hold
+// outputs in the order of the lanes that made them: value ((4 g + e) D/16 + c) of a row at
+// (g D/16 + c) 4 + e; a lane takes four c of one g.
 template <int D>
 __global__ __launch_bounds__(256) void k_share_join(ShareArgs a, int64_t rows) {
-  constexpr int LPS = D / 4;
-  const int d4 = threadIdx.x % LPS;
+  constexpr int LPS = D / 16;
+  const int lane = threadIdx.x % LPS;
   const int64_t i = (int64_t)blockIdx.x * (256 / LPS) + threadIdx.x / LPS;
   if (blockIdx.x == 0 && threadIdx.x == 0) a.head->next = 0;  // for the next call
   if (i >= rows) return;
@@ -768,47 +783,56 @@ __global__ __launch_bounds__(256) void k_share_join(ShareArgs a, int64_t rows) {
   const bool planned = a.head->key == a.key;
   int n = planned ? a.n_parts[session] : 0;
   n = n < a.parts ? n : a.parts;
-  if (row - (int64_t)session * a.kv.R >= kv_session(a.kv, session).rows) n = 0;
   const float2* ml = a.part_ml + i * a.parts;
-  const float* part = a.part_o + i * a.parts * D + d4 * 4;
+  const float* part = a.part_o + i * a.parts * D + lane * 16;
   float top = kNoScore, l = planned ? 0.0f : NAN;
-  f32x4_t y{l, l, l, l};
-  for (int k0 = 0; k0 < n; k0 += 4) {
-    float2 x[4];
-    f32x4_t o[4];
+  f32x4_t y[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+  for (int c = 0; c < 4; ++c) y[c] = f32x4_t{l, l, l, l};
+  for (int k0 = 0; k0 < n; k0 += 2) {
+    float2 x[2];
+    f32x4_t o[2][4];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
       const int k = k0 + u;
       x[u] = k < n ? ml[k] : make_float2(kNoScore, 0.0f);
       // parts without a token left their place unwritten: read, not used
-      if (k < n) o[u] = *reinterpret_cast<const f32x4_t*>(part + (int64_t)k * D);
-    }
-    float t = top;
+      if (k < n) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) t = fmaxf(t, x[u].x);
+        for (int c = 0; c < 4; ++c) o[u][c] = *reinterpret_cast<const f32x4_t*>(part + (int64_t)k * D + 4 * c);
+      }
+    }
+    const float t = fmaxf(fmaxf(top, x[0].x), x[1].x);
     const float f = __builtin_amdgcn_exp2f(top - t);
     l *= f;
-    y *= f;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) y[c] *= f;
     top = t;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < 2; ++u) {
       if (x[u].y == 0.0f) continue;
       const float e = __builtin_amdgcn_exp2f(x[u].x - top);
       l += x[u].y * e;
-      y += o[u] * e;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) y[c] += o[u][c] * e;
     }
   }
   const float f = l == 0.0f ? 0.0f : 1.0f / l;
-  uint16_t* dst = a.out + row * a.o_row + hq * a.o_head + d4 * 4;
-  const uint32_t lo = l == 0.0f ? 0u : pack_bf16(y[0] * f, y[1] * f), hi = l == 0.0f ? 0u : pack_bf16(y[2] * f, y[3] * f);
-  if (a.o_aligned) {
-    *reinterpret_cast<uint32_t*>(dst) = lo;
-    *reinterpret_cast<uint32_t*>(dst + 2) = hi;
-  } else {
-    dst[0] = (uint16_t)lo, dst[1] = (uint16_t)(lo >> 16);
-    dst[2] = (uint16_t)hi, dst[3] = (uint16_t)(hi >> 16);
+  const int g = lane / (LPS / 4), c0 = lane % (LPS / 4) * 4;
+  uint16_t* dst = a.out + row * a.o_row + hq * a.o_head;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    uint16_t* at = dst + (4 * g + e) * LPS + c0;
+    const uint32_t lo = l == 0.0f ? 0u : pack_bf16(y[0][e] * f, y[1][e] * f), hi = l == 0.0f ? 0u : pack_bf16(y[2][e] * f, y[3][e] * f);
+    if (a.o_aligned) {
+      *reinterpret_cast<uint32_t*>(at) = lo;
+      *reinterpret_cast<uint32_t*>(at + 2) = hi;
+    } else {
+      at[0] = (uint16_t)lo, at[1] = (uint16_t)(lo >> 16);
+      at[2] = (uint16_t)hi, at[3] = (uint16_t)(hi >> 16);
+    }
   }
-  if (a.lse && d4 == 0)
+  if (a.lse && lane == 0)
     a.lse[i] = l == 0.0f ? -INFINITY : fmaf(top, a.binade, __builtin_amdgcn_logf(l) * kLn2);
 }
 
@@ -835,6 +859,9 @@ ShareSizes share_sizes(int d, int64_t S, int64_t R, int64_t heads, int64_t group
   }
   z.parts = z.levels + 1 + z.extra;
   for (int k = 0; k < 2; ++k) z.rows[k] = 16 * z.mt[k];
+  // (as in kv_attend.hip: the issue of a tile's instructions, times the waves of a SIMD)
+  for (int k = 0; k < 2; ++k)
+    z.us[k] = (float)((4.0 * (0.9 * d + 20 + 36 * z.mt[k]) + (32.0 + d / 2.0) * z.mt[k]) * 1.35 / 2100 * 2 / (32 * z.wt));
   z.slots = kCUs * (d == 64 ? share_resident(64, 4, 4, 4) : d == 128 ? share_resident(128, 4, 4, 4) : share_resident(256, 2, 2, 8));
   // A level's segments have a tile more each than their rows fill, and shares.
   const int64_t wide = (S * RG + z.rows[0] - 1) / z.rows[0] + S / 2 + 1, own = S * ((RG + z.rows[1] - 1) / z.rows[1]);
@@ -958,7 +985,7 @@ hipError_t launch_attend_shared(int d, const KvArgs& kv, const AttendCall& c, vo
                        : d == 128 ? launch_own<128>(z.mt[1], a, z.slots, s)
                                   : launch_own<256>(z.mt[1], a, z.slots, s);
   if (e != hipSuccess) return e;
-  const int64_t per = 256 / (d / 4);
+  const int64_t per = 256 / (d / 16);
   const dim3 grid((unsigned)((rows + per - 1) / per));
   if (d == 64) launch_kernel(k_share_join<64>, grid, dim3(256), 0, s, a, rows);
   else if (d == 128) launch_kernel(k_share_join<128>, grid, dim3(256), 0, s, a, rows);
