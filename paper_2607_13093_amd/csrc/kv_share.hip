@@ -24,7 +24,7 @@ constexpr int kShareStep = 128;   // tokens that shares are multiples of
 constexpr int kShareLeast = 256;  // and at least
 // Tokens whose reading a segment has to save: a part of every row costs about as much.
 constexpr int kShareWorth = 256;
-constexpr float kShareItem = 8.0f;  // us of an item beside its tokens
+constexpr double kShareItem = 8.0;  // us of an item beside its tokens and outputs
 
 // Tokens from ... to - 1 of `members` sessions from place `first` of the order.
 struct ShareSeg {
@@ -59,6 +59,7 @@ struct ShareSizes {
   int rows[2];        // of a tile of an item
   int slots;          // workgroups that run at a time
   float us[2];        // of one of them for a token of an item
+  float item_us[2];   // and for an item, its outputs' way out and back with it
   int cap;            // items at most
 };
 
@@ -213,7 +214,8 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
   uint16_t* count = reinterpret_cast<uint16_t*>(low + n2);     // by place: parts so far
   uint16_t* group = count + n2;                                // by place
   uint16_t* first = group + n2;                                // [n2 + 1] by group: its first place
-  __shared__ int s_segs, s_longest, s_chunk[16];
+  __shared__ int s_segs, s_longest;
+  __shared__ float s_us[16];
   const int S = a.kv.n_sessions, shift = a.kv.page_shift, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   auto row_of = [&](int at) { return a.kv.table + (int64_t)slot[(int)(key[at] & 4095)] * a.kv.ld_table; };
 
@@ -344,13 +346,13 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
     key[at] = at < S ? (uint64_t)(uint32_t)(kKvMost - (low[at] - alike[at])) << 12 | (uint64_t)at : ~uint64_t(0);
   sort_keys(key, n2);
 
-  // Shares: each wave tries a length of its own, in time, and what all items then take,
-  // kShareItem more than their tokens each.
+  // Shares: each wave tries a length, in time, and what all items then take, an item's own
+  // time with their tokens'.
   const int RG = a.kv.R * a.group, row_shift[2] = {__ffs(a.z.rows[0]) - 1, __ffs(a.z.rows[1]) - 1};
   auto tiles_of = [&](int members, int kind) { return (int)(((uint32_t)members * RG + a.z.rows[kind] - 1) >> row_shift[kind]); };
   const int room = a.z.extra > 0 ? (longest + a.z.extra - 1) / a.z.extra : longest;
   auto chunk_of = [&](int kind, int candidate) {
-    const float us = (float)(2 << (candidate / 2)) * (candidate & 1 ? 1.5f : 1.0f);  // 2, 3, 4, 6 ... 384
+    const float us = __builtin_amdgcn_exp2f(2.0f + 0.42f * candidate);  // 4 ... 315
     const float c = us / a.z.us[kind];
     int n = c < (float)longest ? (int)c : longest;
     n = n > room ? n : room;
@@ -358,7 +360,7 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
     return (n + kShareStep - 1) / kShareStep * kShareStep;
   };
   {
-    float load = 0.0f, items = 0.0f, most = 0.0f;
+    float load = 0.0f, most = 0.0f;  // of all items, the longest
 #pragma unroll
     for (int kind = 0; kind < 2; ++kind) {
       const int n = kind ? S : shared, c = chunk_of(kind, wave);
@@ -366,28 +368,23 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
         const ShareSeg t = kind ? ShareSeg{i, 1, alike[i], low[i]} : a.segs[i];
         const float k = (float)tiles_of(t.members, kind);
         const int tokens = t.to - t.from;
-        load += k * (float)tokens * a.z.us[kind];
-        items += k * (float)((uint32_t)(tokens + c - 1) / (uint32_t)c);
-        most = fmaxf(most, (float)(tokens < c ? tokens : c) * a.z.us[kind]);
+        load += k * ((float)tokens * a.z.us[kind] + (float)((uint32_t)(tokens + c - 1) / (uint32_t)c) * a.z.item_us[kind]);
+        most = fmaxf(most, (float)(tokens < c ? tokens : c) * a.z.us[kind] + a.z.item_us[kind]);
       }
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
       load += __shfl_xor(load, o, 64);
-      items += __shfl_xor(items, o, 64);
       most = fmaxf(most, __shfl_xor(most, o, 64));
     }
-    items *= (float)a.kv.heads;
-    load = load * (float)a.kv.heads + items * kShareItem;
-    const float slots = (float)a.z.slots;
-    // (the last items fill their places to half)
-    const float us = items <= slots ? most + kShareItem : load / slots + 0.5f * (most + kShareItem);
-    if (lane == 0) s_chunk[wave] = (int)(us * 16.0f);
+    // The last items fill their places to half; of two workgroups of a CU the one that
+    // came first goes ahead, so that one item for each place is no better.
+    if (lane == 0) s_us[wave] = fmaxf(0.67f * most, load * (float)a.kv.heads / (float)a.z.slots + 0.5f * most);
   }
   __syncthreads();
   int best = 0;
 #pragma unroll
-  for (int k = 1; k < 16; ++k) best = s_chunk[k] < s_chunk[best] ? k : best;
+  for (int k = 1; k < 16; ++k) best = s_us[k] < s_us[best] ? k : best;
   const int chunk[2] = {chunk_of(0, best), chunk_of(1, best)};
 
   // Parts of each segment, level by level along the paths, and the items, one a
@@ -452,6 +449,21 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
   if (threadIdx.x == 0) *a.head = ShareHead{a.key, made, 0, shared};
 }
 
+// Division by a number that is the same for all: by its reciprocal, one short at most.
+struct Divisor {
+  uint32_t d, r;
+};
+inline Divisor divisor_of(uint32_t d) { return Divisor{d, d == 1 ? 0xFFFFFFFFu : (uint32_t)((uint64_t(1) << 32) / d)}; }
+__device__ __forceinline__ uint32_t divide(uint32_t n, const Divisor& d, uint32_t* rest) {
+  uint32_t q = __umulhi(n, d.r), x = n - q * d.d;
+  if (x >= d.d) {
+    x -= d.d;
+    ++q;
+  }
+  *rest = x;
+  return q;
+}
+
 struct ShareArgs {
   KvArgs kv;
   const uint16_t* q;
@@ -460,6 +472,7 @@ struct ShareArgs {
   int64_t o_row, o_head;
   float* lse;
   int group, window;
+  Divisor of_rows, of_group;  // by the rows of a session and head, and by group
   float scale_log2, binade;
   bool q_aligned, o_aligned;
   uint32_t key;
@@ -479,11 +492,12 @@ struct ShareRow {
   bool is, live;             // live: it is one of the session's rows
   int pos;
 };
-__device__ __forceinline__ ShareRow share_row(const ShareArgs& a, const ShareItem& it, int fq, int RG, int G) {
-  const int member = fq / RG, x = fq - member * RG;
+__device__ __forceinline__ ShareRow share_row(const ShareArgs& a, const ShareItem& it, int fq) {
   ShareRow w;
-  w.r = x / G;
-  w.in_group = x - w.r * G;
+  uint32_t x, in;
+  const int member = (int)divide((uint32_t)fq, a.of_rows, &x);
+  w.r = (int)divide(x, a.of_group, &in);
+  w.in_group = (int)in;
   const int at = it.first + member;
   w.is = member < it.members && (unsigned)at < (unsigned)a.kv.n_sessions;
   const SharePlace p = a.order[w.is ? at : 0];
@@ -506,7 +520,9 @@ __device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& 
   const int lane = threadIdx.x & 63, g = lane >> 4, n = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int wt = wave % WT, wr = wave / WT;
-  const int G = a.group, RG = a.kv.R * G;
+  const int G = a.group;
+  // of each row: its place among all parts (-1: none), whether it is one of its session's
+  __shared__ int s_row[WR * MT * 16][2];
   {
     // pages of a row of the table; all of its tokens up to it.to are held
     KvSession ses;
@@ -542,8 +558,12 @@ __device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& 
     int low = kKvMost, high = -1;  // of the rows that are
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      const ShareRow w = share_row(a, it, row0 + m * 16 + n, RG, G);
+      const ShareRow w = share_row(a, it, row0 + m * 16 + n);
       const bool live = w.live;
+      if (g == 0 && wt == 0) {
+        s_row[(wr * MT + m) * 16 + n][0] = w.is ? (w.session * a.kv.R + w.r) * (a.kv.heads * G) + head * G + w.in_group : -1;
+        s_row[(wr * MT + m) * 16 + n][1] = live;
+      }
       pos[m] = live ? w.pos : -1;
       if (live) {
         low = w.pos < low ? w.pos : low;
@@ -717,10 +737,10 @@ __device__ __forceinline__ void share_item(const ShareArgs& a, const ShareItem& 
 #pragma unroll
         for (int k = 0; k < WT; ++k) y[i] += s_o[((wr * WT + k) * VC + wt * VP + i) * 64 + lane];
       }
-      const ShareRow row = share_row(a, it, row0 + m * 16 + n, RG, G);
-      if (row.is && (unsigned)it.part < (unsigned)a.parts) {
-        if (!row.live) l = 0.0f;
-        const int64_t at = (((int64_t)row.session * a.kv.R + row.r) * (a.kv.heads * G) + head * G + row.in_group) * a.parts + it.part;
+      const int row = s_row[(wr * MT + m) * 16 + n][0];
+      if (row >= 0 && (unsigned)it.part < (unsigned)a.parts) {
+        if (!s_row[(wr * MT + m) * 16 + n][1]) l = 0.0f;
+        const int64_t at = (int64_t)row * a.parts + it.part;
         if (g == 0 && wt == 0) a.part_ml[at] = make_float2(t, l);
         if (!(l == 0.0f)) {
 #pragma unroll
@@ -769,13 +789,16 @@ __global__ __launch_bounds__(64 * waves_in(WT), share_waves(D, MT, WT)) void k_s
 // A row's parts joined, in their order, by D/16 lanes a row and head.  Parts hold
 // outputs in the order of the lanes that made them: value ((4 g + e) D/16 + c) of a row at
 // (g D/16 + c) 4 + e; a lane takes four c of one g.
-template <int D>
+// TURNS groups of lanes take the parts of a row in turns.
+template <int D, int TURNS>
 __global__ __launch_bounds__(256) void k_share_join(ShareArgs a, int64_t rows) {
-  constexpr int LPS = D / 16;
-  const int lane = threadIdx.x % LPS;
-  const int64_t i = (int64_t)blockIdx.x * (256 / LPS) + threadIdx.x / LPS;
+  constexpr int LPS = D / 16, PER = 256 / LPS / TURNS;  // rows of a workgroup
+  __shared__ float s_l[256 / LPS], s_top[256 / LPS];
+  __shared__ f32x4_t s_y[TURNS > 1 ? 4 * 256 : 1];
+  const int lane = threadIdx.x % LPS, turn = threadIdx.x / LPS % TURNS;
+  const int64_t want = (int64_t)blockIdx.x * PER + threadIdx.x / (LPS * TURNS);
+  const int64_t i = want < rows ? want : rows - 1;
   if (blockIdx.x == 0 && threadIdx.x == 0) a.head->next = 0;  // for the next call
-  if (i >= rows) return;
   const int heads = a.kv.heads * a.group;
   const int64_t row = i / heads;
   const int hq = (int)(i - row * heads);
@@ -789,12 +812,12 @@ __global__ __launch_bounds__(256) void k_share_join(ShareArgs a, int64_t rows) {
   f32x4_t y[4];
 #pragma unroll
   for (int c = 0; c < 4; ++c) y[c] = f32x4_t{l, l, l, l};
-  for (int k0 = 0; k0 < n; k0 += 2) {
+  for (int k0 = turn; k0 < n; k0 += 2 * TURNS) {
     float2 x[2];
     f32x4_t o[2][4];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int k = k0 + u;
+      const int k = k0 + u * TURNS;
       x[u] = k < n ? ml[k] : make_float2(kNoScore, 0.0f);
       // parts without a token left their place unwritten: read, not used
       if (k < n) {
@@ -817,6 +840,32 @@ __global__ __launch_bounds__(256) void k_share_join(ShareArgs a, int64_t rows) {
       for (int c = 0; c < 4; ++c) y[c] += o[u][c] * e;
     }
   }
+  if constexpr (TURNS > 1) {
+    const int group = threadIdx.x / LPS;
+    if (lane == 0) {
+      s_l[group] = l;
+      s_top[group] = top;
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) s_y[c * 256 + threadIdx.x] = y[c];
+    __syncthreads();
+    if (turn != 0) return;
+    float t = top;
+#pragma unroll
+    for (int k = 1; k < TURNS; ++k) t = fmaxf(t, s_top[group + k]);
+    l = 0.0f;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) y[c] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < TURNS; ++k) {
+      const float e = __builtin_amdgcn_exp2f(s_top[group + k] - t);
+      l += s_l[group + k] * e;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) y[c] += s_y[c * 256 + threadIdx.x + k * LPS] * e;
+    }
+    top = t;
+  }
+  if (want >= rows) return;
   const float f = l == 0.0f ? 0.0f : 1.0f / l;
   const int g = lane / (LPS / 4), c0 = lane % (LPS / 4) * 4;
   uint16_t* dst = a.out + row * a.o_row + hq * a.o_head;
@@ -859,10 +908,11 @@ ShareSizes share_sizes(int d, int64_t S, int64_t R, int64_t heads, int64_t group
   }
   z.parts = z.levels + 1 + z.extra;
   for (int k = 0; k < 2; ++k) z.rows[k] = 16 * z.mt[k];
+  z.slots = kCUs * (d == 64 ? share_resident(64, 4, 4, 4) : d == 128 ? share_resident(128, 4, 4, 4) : share_resident(256, 2, 2, 8));
   // (as in kv_attend.hip: the issue of a tile's instructions, times the waves of a SIMD)
   for (int k = 0; k < 2; ++k)
     z.us[k] = (float)((4.0 * (0.9 * d + 20 + 36 * z.mt[k]) + (32.0 + d / 2.0) * z.mt[k]) * 1.35 / 2100 * 2 / (32 * z.wt));
-  z.slots = kCUs * (d == 64 ? share_resident(64, 4, 4, 4) : d == 128 ? share_resident(128, 4, 4, 4) : share_resident(256, 2, 2, 8));
+  for (int k = 0; k < 2; ++k) z.item_us[k] = (float)(kShareItem + (double)z.rows[k] * (d * 8 + 16) * z.slots / 4e6);
   // A level's segments have a tile more each than their rows fill, and shares.
   const int64_t wide = (S * RG + z.rows[0] - 1) / z.rows[0] + S / 2 + 1, own = S * ((RG + z.rows[1] - 1) / z.rows[1]);
   z.cap = (int)((z.levels * wide + own) * (1 + z.extra));
@@ -911,6 +961,14 @@ hipError_t launch_own(int own, const ShareArgs& a, int slots, hipStream_t s) {
     return own == 1 ? launch_parts<D, 4, 1, 4>(a, slots, s)
            : own == 2 ? launch_parts<D, 4, 2, 4>(a, slots, s)
                       : launch_parts<D, 4, 4, 4>(a, slots, s);
+}
+
+// (2560 rows of up to 35 parts of 128 dimensions: 13.1 us by one group of lanes a row)
+template <int D>
+void launch_share_join(const ShareArgs& a, int64_t rows, hipStream_t s) {
+  constexpr int ALL = 256 / (D / 16);  // groups of lanes of a workgroup
+  if (a.parts <= 6) launch_kernel(k_share_join<D, 1>, dim3((unsigned)((rows + ALL - 1) / ALL)), dim3(256), 0, s, a, rows);
+  else launch_kernel(k_share_join<D, 8>, dim3((unsigned)((rows * 8 + ALL - 1) / ALL)), dim3(256), 0, s, a, rows);
 }
 
 }  // namespace
@@ -963,6 +1021,8 @@ hipError_t launch_attend_shared(int d, const KvArgs& kv, const AttendCall& c, vo
   a.o_head = c.o_head;
   a.lse = c.lse;
   a.group = c.q_heads / kv.heads;
+  a.of_rows = divisor_of((uint32_t)(kv.R * a.group));
+  a.of_group = divisor_of((uint32_t)a.group);
   a.window = c.window;
   a.scale_log2 = c.scale * 1.44269504088896f;
   a.binade = (float)((double)c.scale / a.scale_log2);
@@ -985,11 +1045,9 @@ hipError_t launch_attend_shared(int d, const KvArgs& kv, const AttendCall& c, vo
                        : d == 128 ? launch_own<128>(z.mt[1], a, z.slots, s)
                                   : launch_own<256>(z.mt[1], a, z.slots, s);
   if (e != hipSuccess) return e;
-  const int64_t per = 256 / (d / 16);
-  const dim3 grid((unsigned)((rows + per - 1) / per));
-  if (d == 64) launch_kernel(k_share_join<64>, grid, dim3(256), 0, s, a, rows);
-  else if (d == 128) launch_kernel(k_share_join<128>, grid, dim3(256), 0, s, a, rows);
-  else launch_kernel(k_share_join<256>, grid, dim3(256), 0, s, a, rows);
+  if (d == 64) launch_share_join<64>(a, rows, s);
+  else if (d == 128) launch_share_join<128>(a, rows, s);
+  else launch_share_join<256>(a, rows, s);
   return hipGetLastError();
 }
 
