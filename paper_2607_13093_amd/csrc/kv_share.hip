@@ -152,29 +152,37 @@ template <int M, int COLS>
 __device__ __forceinline__ void compare_rows(const Alike& a, int S) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   for (int at0 = wave; at0 < S; at0 += 16 * M) {
+    // lane m looks up session m
+    const int at = at0 + 16 * lane;
+    const bool in = lane < M && at < S;
+    const int group = a.group[in ? at : at0], lead = a.first[group];
+    const int64_t row_x = a.slot[(int)(a.key[lead] & 4095)] * a.ld_table, row_y = a.slot[(int)(a.key[in ? at : at0] & 4095)] * a.ld_table;
+    const int begin = in && at != lead ? a.depth[at] + 1 : kKvMost;
+    uint32_t open = (uint32_t)__ballot(in && at != lead);
+    int c = begin;
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) {
+      const int z = __shfl_xor(c, o, 64);
+      c = z < c ? z : c;
+    }
+    c = __builtin_amdgcn_readfirstlane(c);
     const int32_t *x[M], *y[M];
-    int g[M], c = kKvMost;
-    uint32_t open = 0;
+    auto of_lane = [](int64_t v, int m) {
+      return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), m) << 32 |
+                       (uint32_t)__builtin_amdgcn_readlane((int)v, m));
+    };
 #pragma unroll
     for (int m = 0; m < M; ++m) {
-      const int at = at0 + 16 * m < S ? at0 + 16 * m : at0;
-      g[m] = __builtin_amdgcn_readfirstlane((int)a.group[at]);
-      const int lead = __builtin_amdgcn_readfirstlane((int)a.first[g[m]]);
-      const int sx = a.slot[(int)(a.key[lead] & 4095)], sy = a.slot[(int)(a.key[at] & 4095)];
-      x[m] = a.table + __builtin_amdgcn_readfirstlane(sx) * a.ld_table;
-      y[m] = a.table + __builtin_amdgcn_readfirstlane(sy) * a.ld_table;
-      if (at0 + 16 * m < S && at != lead) {
-        const int d = __builtin_amdgcn_readfirstlane(a.depth[at]) + 1;
-        open |= 1u << m;
-        c = d < c ? d : c;
-      }
+      x[m] = a.table + of_lane(row_x, m);
+      y[m] = a.table + of_lane(row_y, m);
     }
     while (open) {
       int32_t p[M][COLS], q[M][COLS];
-      int end[M];  // at most a row's places
+      const int ends = *(volatile const int32_t*)&a.alike[group];  // at most a row's places
+      int end[M];
 #pragma unroll
       for (int m = 0; m < M; ++m) {
-        end[m] = open >> m & 1 ? __builtin_amdgcn_readfirstlane(*(volatile const int32_t*)&a.alike[g[m]]) : 0;
+        end[m] = open >> m & 1 ? __builtin_amdgcn_readlane(ends, m) : 0;
 #pragma unroll
         for (int i = 0; i < COLS; ++i)
           if (c + i * 64 < end[m]) {
@@ -190,7 +198,7 @@ __device__ __forceinline__ void compare_rows(const Alike& a, int S) {
         for (int i = COLS - 1; i >= 0; --i)
           if (c + i * 64 < end[m] && p[m][i] != q[m][i]) differs = c + i * 64 + lane;
         const bool any = __any(differs != kKvMost);
-        if (differs != kKvMost) atomicMin(&a.alike[g[m]], differs);
+        if (differs != kKvMost) atomicMin(&a.alike[__builtin_amdgcn_readlane(group, m)], differs);
         if (any || c + COLS * 64 >= end[m]) open &= ~(1u << m);
       }
       c += COLS * 64;
@@ -214,7 +222,7 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
   uint16_t* count = reinterpret_cast<uint16_t*>(low + n2);     // by place: parts so far
   uint16_t* group = count + n2;                                // by place
   uint16_t* first = group + n2;                                // [n2 + 1] by group: its first place
-  __shared__ int s_segs, s_longest;
+  __shared__ int s_segs, s_longest, s_ends[kShareLevels];  // segments up to the end of each level
   __shared__ float s_us[16];
   const int S = a.kv.n_sessions, shift = a.kv.page_shift, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   auto row_of = [&](int at) { return a.kv.table + (int64_t)slot[(int)(key[at] & 4095)] * a.kv.ld_table; };
@@ -247,14 +255,10 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
   __syncthreads();
   longest = s_longest;
 
-  int groups = 1, ends[kShareLevels + 1];  // segments up to each level
-#pragma unroll
-  for (int k = 0; k <= kShareLevels; ++k) ends[k] = 0;
-  bool more = S > 1;
-#pragma unroll
-  for (int level = 0; level < kShareLevels; ++level) {
-    ends[level + 1] = ends[level];
-    if (!more || level >= a.z.levels) continue;
+  // (loops that are not unrolled: run once, code costs its way from memory)
+  int groups = 1, levels = 0;
+#pragma nounroll
+  for (int level = 0; level < a.z.levels && S > 1; ++level) {
     for (int at = threadIdx.x; at < S; at += kPlanThreads) {
       const int s = (int)(key[at] & 4095), d = depth[at];
       const int page = d >= limit[s] ? -1 : level == 0 ? page0[s] : row_of(at)[d];
@@ -267,10 +271,7 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
     int starts = 0;
     for (int i = mine; i < mine + each && i < S; ++i) starts += i == 0 || key[i] >> 12 != key[i - 1] >> 12;
     int id = sum_before(starts, &groups);
-    if (groups == S) {  // no two alike
-      more = false;
-      continue;
-    }
+    if (groups == S) break;  // no two alike
     for (int i = mine; i < mine + each && i < S; ++i) {
       if (i == 0 || key[i] >> 12 != key[i - 1] >> 12) first[id++] = (uint16_t)i;
       group[i] = (uint16_t)(id - 1);
@@ -322,12 +323,12 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
       if (low[g]) depth[at] = alike[g];
       else limit[(int)(key[at] & 4095)] = 0;  // nothing further
     }
-    if (threadIdx.x == 0) s_segs = before + made;
-    ends[level + 1] = before + made;
-    more = made > 0;
+    if (threadIdx.x == 0) s_segs = s_ends[level] = before + made;
+    levels = level + 1;
     __syncthreads();
+    if (made == 0) break;
   }
-  const int shared = ends[kShareLevels];
+  const int shared = s_segs;
   // What sessions hold alone, the longest first.
   for (int at = threadIdx.x; at < S; at += kPlanThreads) {
     const int s = (int)(key[at] & 4095);
@@ -361,7 +362,7 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
   };
   {
     float load = 0.0f, most = 0.0f;  // of all items, the longest
-#pragma unroll
+#pragma nounroll
     for (int kind = 0; kind < 2; ++kind) {
       const int n = kind ? S : shared, c = chunk_of(kind, wave);
       for (int i = lane; i < n; i += 64) {
@@ -391,10 +392,10 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
   // thread, which looks for its segment in the sums of them.
   int32_t *before = page0, *part_of = base;  // of up to n2 segments
   int made = 0;
-#pragma unroll
-  for (int level = 0; level <= kShareLevels; ++level) {
-    const int kind = level == kShareLevels;
-    const int lo = kind ? 0 : ends[level], hi = kind ? S : ends[level + 1];
+#pragma nounroll
+  for (int level = 0; level <= levels; ++level) {
+    const int kind = level == levels;
+    const int lo = kind || level == 0 ? 0 : s_ends[level - 1], hi = kind ? S : s_ends[level];
     const uint32_t c = chunk[kind];
     auto segment = [&](int i) {
       if (!kind) return a.segs[i];
