@@ -148,6 +148,34 @@ def test_shared_pages_stay(page, trunk, own):
     check(c, was, w, [0] * 6, 0, 0, host(weights), None, w)
 
 
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 32), (256, 16)])
+def test_many_layers_and_slots(d, page):
+    # 4160 units of a slot, layer and head: workgroups of two waves
+    rng = np.random.default_rng(d)
+    lens = [int(n) for n in rng.integers(0, 150, 65)]
+    c = cache_of(rng, lens, 2, d, page, 32)
+    assert c.n_slots * c.layers * c.kv_heads >= 4096
+    was = look(c)
+    w = weights_of(rng, 65, c.table.shape[1] * page, "ties")
+    weights = torch.from_numpy(w).cuda()
+    keep = [int(n) for n in rng.integers(0, 150, 65)]
+    sph.pages_evict(c, weights, ints(keep), 3, 9)
+    check(c, was, w, keep, 3, 9, host(weights), None, w)
+
+
+@pytest.mark.parametrize("n", [4096, 4097, 8192, 8193, 16384, 16385, 40000])
+def test_long_slots(n):
+    # weights in registers up to 4096, 8192 and 16384 tokens, read again beyond
+    rng = np.random.default_rng(n)
+    c = cache_of(rng, [n, 5], 1, 64, 256, 1)
+    for kind, keep in (("odd", n // 2), ("random", n // 3), ("equal", n // 4)):
+        was = look(c)
+        w = weights_of(rng, 2, c.table.shape[1] * 256, kind)
+        weights = torch.from_numpy(w).cuda()
+        _, kept = sph.pages_evict(c, weights, ints([keep, 2]), 1, 100, want_kept=True)
+        check(c, was, w, [keep, 2], 1, 100, host(weights), host(kept), w)
+
+
 def test_every_slot_emptied_and_filled_again():
     rng = np.random.default_rng(5)
     c = cache_of(rng, [100, 50, 7], 1, 128, 16, 2)

@@ -151,6 +151,25 @@ def test_prompts_behind_a_common_one(d, page, rows):
     check(t, 2, [rows + 50, rows, 100])
 
 
+@pytest.mark.parametrize("d,window", [(64, 0), (128, 0), (256, 0), (64, 90)])
+def test_many_rows_are_not_cut(d, window):
+    # more than 65536 rows of a head: one shared level, no shares of a segment; against the plain call
+    t = Text(np.random.default_rng(d), 3, 80, 200, 1, d, 16)
+    t.write([300, 0, 0])
+    t.fork([0, 0], [1, 2])
+    t.write([700, 699, 650])
+    q, _ = bf16(np.random.default_rng(40), 3 * 700, 32, d)
+    plan = sph.kv_share(t.c, 32, 700, rows=ints([700, 699, 650]), window=window)
+    assert host(plan.buffer)[:16].view(np.int32)[3] == 1
+    out, lse = sph.kv_attend_shared(t.c, 0, q, plan, d ** -0.5, want_lse=True)
+    want, wl = sph.kv_attend(t.c, 0, q, 700, d ** -0.5, rows=ints([700, 699, 650]), window=window, want_lse=True)
+    # both are within 2^-8 |o| + (2^-8 + 2^-18 + 4 s) sum |p v| of the exact outputs, |v| at most its largest
+    most = max(np.abs(x).max() for x in t.v)
+    assert (out.float() - want.float()).abs().max() <= 2 * (2.0 ** -8 + 2.0 ** -8 + 2.0 ** -12) * most
+    seen = torch.isfinite(wl)
+    assert torch.equal(seen, torch.isfinite(lse)) and (lse[seen] - wl[seen]).abs().max() <= 1e-4
+
+
 def test_rows_that_are_none_and_empty_slots():
     t = Text(np.random.default_rng(30), 6, 20, 60, 2, 128, 16)
     t.write([100, 0, 0, 0, 0, 0])
