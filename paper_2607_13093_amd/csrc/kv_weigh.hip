@@ -96,30 +96,6 @@ __device__ __forceinline__ void give_weights(const WeighArgs& a, const KvSession
   }
 }
 
-// A lane's query operand of row fq of a head, and the row's log-sum-exp in binades: q of
-// a row that is none is 0.
-template <int D>
-__device__ __forceinline__ float fetch_query(const WeighArgs& a, u32x4_t (&q)[D / 32], int s, int head, int r, int in_group,
-                                             bool in, int g) {
-  const int64_t row = (int64_t)s * a.kv.R + r;
-  const int hq = head * a.group + in_group;
-  const uint16_t* p = a.q + row * a.q_row + (int64_t)hq * a.q_head + g * (D / 4);
-#pragma unroll
-  for (int j = 0; j < D / 32; ++j) {
-    u32x4_t x{0u, 0u, 0u, 0u};
-    if (in) {
-      if (a.q_aligned) {
-        x = *reinterpret_cast<const u32x4_t*>(p + 8 * j);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = (uint32_t)p[8 * j + 2 * i] | ((uint32_t)p[8 * j + 2 * i + 1] << 16);
-      }
-    }
-    q[j] = x;
-  }
-  return in ? a.lse[row * (a.kv.heads * a.group) + hq] : -INFINITY;
-}
-
 // Adds the weights of two blocks' scores against a tile of rows.
 __device__ __forceinline__ void add_weights(f32x4_t (&acc)[2], const f32x4_t (&sc)[2], float scale_log2, float l) {
 #pragma unroll
@@ -411,17 +387,39 @@ __global__ __launch_bounds__(256, 2) void k_weigh_many(WeighArgs a) {
     int rt0, rt1;
     rows_that_see(ses, G, a.window, t0, t1, &rt0, &rt1);
     rt0 += share.phase;
-    // a lane's row goes 16 x step further each time
+    // A lane's row goes 16 x step further each time; one past the session's is its last.
     const int step = share.step, far_r = 16 * step / G, far_in = 16 * step - far_r * G;
     const int first_r = (rt0 * 16 + n) / G, first_in = rt0 * 16 + n - first_r * G;
+    const int64_t heads = (int64_t)a.kv.heads * G;
+    const int last_r = (live - 1) / G, last_in = live - 1 - last_r * G;
 
     f32x4_t acc[TT][2];
 #pragma unroll
     for (int t = 0; t < TT; ++t) acc[t][0] = acc[t][1] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     for (int head = share.h0; head < share.h1 && rt0 < rt1; ++head) {
-      int r = first_r, in = first_in;
-      u32x4_t next[KJ];
-      float next_l = fetch_query<D>(a, next, s, head, r, in, rt0 * 16 + n < live, g);
+      const uint16_t* q0 = a.q + (int64_t)s * a.kv.R * a.q_row + (int64_t)head * G * a.q_head + g * (D / 4);
+      const float* l0 = a.lse + (int64_t)s * a.kv.R * heads + head * G;
+      int r = first_r, in = first_in, fq = rt0 * 16 + n;
+      struct Fetched {
+        u32x4_t q[KJ];
+        float l;
+      };
+      Fetched even, odd;
+      auto fetch = [&](Fetched& f) {
+        const int at_r = fq < live ? r : last_r, at_in = fq < live ? in : last_in;
+        const uint16_t* p = q0 + at_r * a.q_row + at_in * a.q_head;
+        if (a.q_aligned) {
+#pragma unroll
+          for (int j = 0; j < KJ; ++j) f.q[j] = *reinterpret_cast<const u32x4_t*>(p + 8 * j);
+        } else {
+#pragma unroll
+          for (int j = 0; j < KJ; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f.q[j][i] = (uint32_t)p[8 * j + 2 * i] | ((uint32_t)p[8 * j + 2 * i + 1] << 16);
+        }
+        f.l = l0[at_r * heads + at_in];
+      };
+      fetch(even);
       bf16x8_t k[TT][2][KJ];
 #pragma unroll
       for (int t = 0; t < TT; ++t)
@@ -439,28 +437,30 @@ __global__ __launch_bounds__(256, 2) void k_weigh_many(WeighArgs a) {
             k[t][b][j] = __builtin_bit_cast(bf16x8_t, y);
           }
         }
-      for (int rt = rt0; rt < rt1; rt += step) {
-        bf16x8_t q[KJ];
-#pragma unroll
-        for (int j = 0; j < KJ; ++j) q[j] = __builtin_bit_cast(bf16x8_t, next[j]);
-        const float l = next_l * kLog2e;
+      // tile rt of the rows, with the next on its way
+      auto take = [&](int rt, const Fetched& now, Fetched& next) {
+        const bool dead = now.l == -INFINITY || fq >= live;  // the row sees nothing, or is none
+        const float l = now.l * kLog2e;
         const int pos = base + r;
+        const int low_pos = __builtin_amdgcn_readlane(pos, 0), high_pos = __builtin_amdgcn_readlane(pos, 15);
+        const bool whole = paged && low_pos >= t1 - 1 && (a.window == 0 || t0 > high_pos - a.window) && !__any(dead);
         r += far_r;
         in += far_in;
-        if (in >= G) in -= G, ++r;
-        if (rt + step < rt1) next_l = fetch_query<D>(a, next, s, head, r, in, (rt + step) * 16 + n < live, g);
-        const int low = rt * 16, high = low + 15 < live ? low + 15 : live - 1;
-        const bool dead = l == -INFINITY;  // the row sees nothing
-        const bool whole = paged && low + 16 <= live && base + low / G >= t1 - 1 &&
-                           (a.window == 0 || t0 > base + high / G - a.window) && !__any(dead);
+        fq += 16 * step;
+        if (in >= G) {
+          in -= G;
+          ++r;
+        }
+        if (rt + step < rt1) fetch(next);
         f32x4_t sc[2][2];
         auto score = [&](int t) {
           f32x4_t(&x)[2] = sc[t & 1];
           x[0] = x[1] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
           for (int j = 0; j < KJ; ++j) {
-            x[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t][0][j], q[j], x[0], 0, 0, 0);
-            x[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t][1][j], q[j], x[1], 0, 0, 0);
+            const bf16x8_t q = __builtin_bit_cast(bf16x8_t, now.q[j]);
+            x[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t][0][j], q, x[0], 0, 0, 0);
+            x[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t][1][j], q, x[1], 0, 0, 0);
           }
         };
         score(0);
@@ -486,6 +486,10 @@ __global__ __launch_bounds__(256, 2) void k_weigh_many(WeighArgs a) {
             add_seen(acc[t], sc[t & 1], a.scale_log2, l, from + 32 * t, span, pages[t]);
           }
         }
+      };
+      for (int rt = rt0; rt < rt1; rt += 2 * step) {
+        take(rt, even, odd);
+        if (rt + step < rt1) take(rt + step, odd, even);
       }
     }
     give_weights<TT>(a, ses, s, slot, part_of, share.whole, t0, TOKENS, acc, g, n);
