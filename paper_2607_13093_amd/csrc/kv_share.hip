@@ -24,7 +24,7 @@ constexpr int kShareStep = 128;   // tokens that shares are multiples of
 constexpr int kShareLeast = 256;  // and at least
 // Tokens whose reading a segment has to save: a part of every row costs about as much.
 constexpr int kShareWorth = 256;
-constexpr double kShareItem = 8.0;  // us of an item beside its tokens and outputs
+constexpr double kShareItem = 4.0;  // us of an item beside its tokens and outputs, where another hides the rest
 
 // Tokens from ... to - 1 of `members` sessions from place `first` of the order.
 struct ShareSeg {
@@ -361,26 +361,34 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
     return (n + kShareStep - 1) / kShareStep * kShareStep;
   };
   {
-    float load = 0.0f, most = 0.0f;  // of all items, the longest
+    const float heads = (float)a.kv.heads / (float)a.z.slots;
+    float load = 0.0f, longest_us = 0.0f;
 #pragma nounroll
     for (int kind = 0; kind < 2; ++kind) {
       const int n = kind ? S : shared, c = chunk_of(kind, wave);
+      float tokens = 0.0f, items = 0.0f, most = 0.0f;
       for (int i = lane; i < n; i += 64) {
         const ShareSeg t = kind ? ShareSeg{i, 1, alike[i], low[i]} : a.segs[i];
         const float k = (float)tiles_of(t.members, kind);
-        const int tokens = t.to - t.from;
-        load += k * ((float)tokens * a.z.us[kind] + (float)((uint32_t)(tokens + c - 1) / (uint32_t)c) * a.z.item_us[kind]);
-        most = fmaxf(most, (float)(tokens < c ? tokens : c) * a.z.us[kind] + a.z.item_us[kind]);
+        const int its = t.to - t.from;
+        tokens += k * (float)its;
+        items += k * (float)((uint32_t)(its + c - 1) / (uint32_t)c);
+        most = fmaxf(most, (float)(its < c ? its : c));
       }
-    }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      load += __shfl_xor(load, o, 64);
-      most = fmaxf(most, __shfl_xor(most, o, 64));
+      for (int o = 32; o > 0; o >>= 1) {
+        tokens += __shfl_xor(tokens, o, 64);
+        items += __shfl_xor(items, o, 64);
+        most = fmaxf(most, __shfl_xor(most, o, 64));
+      }
+      load += (tokens * a.z.us[kind] + items * a.z.item_us[kind]) * heads;
+      // Rounds of items: a last one that is not full has CUs with one workgroup, which is
+      // done sooner.
+      const float rounds = items * heads, full = floorf(rounds);
+      const float last = rounds > full ? 0.4f + 0.65f * (rounds - full) : 0.0f;
+      longest_us = fmaxf(longest_us, (most * a.z.us[kind] + a.z.item_us[kind]) * (full + last));
     }
-    // The last items fill their places to half; of two workgroups of a CU the one that
-    // came first goes ahead, so that one item for each place is no better.
-    if (lane == 0) s_us[wave] = fmaxf(0.67f * most, load * (float)a.kv.heads / (float)a.z.slots + 0.5f * most);
+    if (lane == 0) s_us[wave] = fmaxf(load, longest_us);
   }
   __syncthreads();
   int best = 0;
@@ -910,10 +918,13 @@ ShareSizes share_sizes(int d, int64_t S, int64_t R, int64_t heads, int64_t group
   z.parts = z.levels + 1 + z.extra;
   for (int k = 0; k < 2; ++k) z.rows[k] = 16 * z.mt[k];
   z.slots = kCUs * (d == 64 ? share_resident(64, 4, 4, 4) : d == 128 ? share_resident(128, 4, 4, 4) : share_resident(256, 2, 2, 8));
-  // (as in kv_attend.hip: the issue of a tile's instructions, times the waves of a SIMD)
+  // A token of a tile of rows: the issue of its instructions, vector ones and products one
+  // after the other, on a SIMD that two waves share (4096 tokens for 64 rows of 128
+  // dimensions: two workgroups 84 us).
   for (int k = 0; k < 2; ++k)
-    z.us[k] = (float)((4.0 * (0.9 * d + 20 + 36 * z.mt[k]) + (32.0 + d / 2.0) * z.mt[k]) * 1.35 / 2100 * 2 / (32 * z.wt));
-  for (int k = 0; k < 2; ++k) z.item_us[k] = (float)(kShareItem + (double)z.rows[k] * (d * 8 + 16) * z.slots / 4e6);
+    z.us[k] = (float)((4.0 * (0.9 * d + 20 + 36 * z.mt[k]) + (32.0 + d / 2.0) * z.mt[k]) * 1.85 / 2100 * 2 / (32 * z.wt));
+  // an item, and half of its outputs' way out and back, at 4 TB/s
+  for (int k = 0; k < 2; ++k) z.item_us[k] = (float)(kShareItem + (double)z.rows[k] * (d * 4 + 8) * z.slots / 4e6);
   // A level's segments have a tile more each than their rows fill, and shares.
   const int64_t wide = (S * RG + z.rows[0] - 1) / z.rows[0] + S / 2 + 1, own = S * ((RG + z.rows[1] - 1) / z.rows[1]);
   z.cap = (int)((z.levels * wide + own) * (1 + z.extra));
