@@ -10,6 +10,12 @@
 // Tokens only ever move down, so they move in place: a workgroup takes one slot,
 // layer and head and goes up its blocks, a chunk at a time; all of a chunk is read
 // before any of it is written, and what later chunks read lies above it.
+//
+// Moving is bound by memory: 64 slots of up to 4096 tokens in 16 layers, 2.2 GB read
+// and written in 445 us, 5.0 TB/s, a copy's rate.  Where a quarter of the tokens stays,
+// the lines that hold them are read nearly whole (a value's codes lie between those of
+// three other tokens): 569 MB kept and written in 197 us.  Choosing is one workgroup's
+// latency, 9 us for 700 tokens and 27 for 16384.
 #include "kv_cache.h"
 
 namespace sph {
@@ -265,8 +271,8 @@ __device__ __forceinline__ void choose_tokens(const EvictArgs& a, int len, int h
   }
 }
 
-// A slot of 16384 tokens takes 72 us where its weights are read again for each digit of
-// eight bits.
+// (16384 tokens 72 us where weights were read again for each of four digits, and numbered
+// 4096 at a time)
 __global__ __launch_bounds__(kChoose) void k_evict_choose(EvictArgs a) {
   const PagesArgs& p = a.p;
   const int held_len = p.lens[blockIdx.x];

@@ -14,12 +14,21 @@
 // The parts are computed as in kv_attend.hip, by workgroups that go over a list of
 // items, a share of a segment for a tile of the rows of all its sessions each: many
 // rows on a shared segment, so that its codes are converted once for 64 rows, few on
-// a session's own.
+// a session's own.  One launch takes both kinds, the shared first, from a queue, so
+// that what own tokens wait for memory hides behind the products of shared ones; a second
+// joins the parts.
+//
+// 16 windows of five rows on one document of 65504 tokens: 127 us (0.68 PFLOP/s; the
+// plain call, which reads and converts the document 16 times, 200).  Bound by issue:
+// vector instructions 57% of the clocks, matrix cores 35%, one after the other (256
+// windows behind one prompt: 500 us, as much as the plain call's, whose tiles of 64 rows
+// are as full).  The plan takes 14 us for two sessions and 35 for 256, once for all layers.
 #include "kv_tile.h"
 
 namespace sph {
 
-constexpr int kShareLevels = 3;
+constexpr int kShareLevels = 3;             // segments of a path that are shared, at most
+constexpr int kShareLooks = kShareLevels + 2;  // groups of groups that are looked at
 constexpr int kShareStep = 128;   // tokens that shares are multiples of
 constexpr int kShareLeast = 256;  // and at least
 // Tokens whose reading a segment has to save: a part of every row costs about as much.
@@ -206,7 +215,7 @@ __device__ __forceinline__ void compare_rows(const Alike& a, int S) {
   }
 }
 
-constexpr int plan_lds(int n2) { return 46 * n2 + 16; }
+constexpr int plan_lds(int n2) { return 50 * n2 + 16; }
 
 __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a, int n2) {
   extern __shared__ __align__(16) uint8_t smem[];
@@ -216,13 +225,14 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
   int32_t* base = slot + n2;                                   // by session: position of its first row
   int32_t* length = base + n2;                                 // by session
   int32_t* page0 = length + n2;                                // by session: its first page; later parts and items before a segment's
-  int32_t* depth = page0 + n2;                                 // by place: pages shared so far
-  int32_t* alike = depth + n2;                                 // by group: pages named alike
+  int32_t* depth = page0 + n2;                                 // by place: pages that its group names alike
+  int32_t* start = depth + n2;                                 // by place: those in segments
+  int32_t* alike = start + n2;                                 // by group: pages named alike
   int32_t* low = alike + n2;                                   // by group: least position of a first row
   uint16_t* count = reinterpret_cast<uint16_t*>(low + n2);     // by place: parts so far
   uint16_t* group = count + n2;                                // by place
   uint16_t* first = group + n2;                                // [n2 + 1] by group: its first place
-  __shared__ int s_segs, s_longest, s_ends[kShareLevels];  // segments up to the end of each level
+  __shared__ int s_segs, s_longest, s_ends[kShareLooks];  // segments up to the end of each level
   __shared__ float s_us[16];
   const int S = a.kv.n_sessions, shift = a.kv.page_shift, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   auto row_of = [&](int at) { return a.kv.table + (int64_t)slot[(int)(key[at] & 4095)] * a.kv.ld_table; };
@@ -247,7 +257,7 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
     base[s] = b;
     length[s] = len;
     page0[s] = p0;
-    depth[s] = count[s] = 0;
+    depth[s] = start[s] = count[s] = 0;
     group[s] = 0;
     key[s] = s < S ? (uint64_t)s : ~uint64_t(0);
   }
@@ -258,7 +268,7 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
   // (loops that are not unrolled: run once, code costs its way from memory)
   int groups = 1, levels = 0;
 #pragma nounroll
-  for (int level = 0; level < a.z.levels && S > 1; ++level) {
+  for (int level = 0; level < kShareLooks && S > 1; ++level) {
     for (int at = threadIdx.x; at < S; at += kPlanThreads) {
       const int s = (int)(key[at] & 4095), d = depth[at];
       const int page = d >= limit[s] ? -1 : level == 0 ? page0[s] : row_of(at)[d];
@@ -300,9 +310,9 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
       int from = 0, to = 0, members = 0;
       if (g < groups) {
         members = first[g + 1] - first[g];
-        from = depth[first[g]] << shift;
+        from = start[first[g]] << shift;
         to = alike[g] << shift;
-        take = members > 1 && (int64_t)(to - from) * (members - 1) >= kShareWorth;
+        take = members > 1 && count[first[g]] < a.z.levels && (int64_t)(to - from) * (members - 1) >= kShareWorth;
       }
       int all = 0;
       const int at = sum_before(take ? 1 : 0, &all);
@@ -320,19 +330,24 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
     __syncthreads();
     for (int at = threadIdx.x; at < S; at += kPlanThreads) {
       const int g = group[at];
-      if (low[g]) depth[at] = alike[g];
-      else limit[(int)(key[at] & 4095)] = 0;  // nothing further
+      if (first[g + 1] - first[g] == 1) limit[(int)(key[at] & 4095)] = 0;  // nothing further
+      else depth[at] = alike[g];
+      // (what is not worth a segment of its own is left to those of smaller groups)
+      if (low[g]) {
+        start[at] = alike[g];
+        ++count[at];
+      }
     }
     if (threadIdx.x == 0) s_segs = s_ends[level] = before + made;
     levels = level + 1;
     __syncthreads();
-    if (made == 0) break;
   }
   const int shared = s_segs;
   // What sessions hold alone, the longest first.
   for (int at = threadIdx.x; at < S; at += kPlanThreads) {
     const int s = (int)(key[at] & 4095);
-    int from = depth[at] << shift;
+    int from = start[at] << shift;
+    count[at] = 0;
     if (a.window > 0) {
       const int64_t lowest = (int64_t)base[s] - a.window + 1;
       if (lowest > from) from = (int)lowest & ~(kKvBlock - 1);

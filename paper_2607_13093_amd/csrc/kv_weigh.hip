@@ -3,15 +3,24 @@
 //   w[j] += sum_{r, h} exp(scale q[r, h] . K[j, h / G] - lse[r, h])
 //   over the rows r that see j (kv_attend.hip), lse the log-sum-exp of their scores.
 //
-// A wave owns TT tiles of 32 tokens and goes over the key/value heads: a head's
-// codes become operands of the first product once, in registers, and every tile of 16
-// of the R G rows is multiplied with them,
+// A wave owns TT tiles of 32 tokens and goes over the key/value heads; every tile of 16
+// of the R G rows is multiplied with the tokens' keys,
 //   S^T = K Q^T   (tokens x rows) 16x16x32 products,
 // lane l = 16 g + n holding row n against tokens 4 g ... 4 g + 3 of each block.  Weights
 // of one token stay apart by lanes and are added up over the rows and heads in
 // registers; the 16 lanes meet once, at the end.  Every token is one wave's (or one
 // wave's of each part of the heads and rows, joined in their order), so that sums do
 // not depend on timing and nothing is added atomically.
+//
+// Up to 64 rows of a head (k_weigh_few) the keys of all heads stream through rings of
+// LDS stages: 256 sessions' windows of four rows over 8192 tokens read their keys at
+// 5.2 TB/s (226 us), 64 at 4.7; the conversion of codes and the exponentials take the rest.
+// More rows (k_weigh_many) pass a head's keys held as operands in registers (330 us in
+// place of 700 for prompts when the keys' conversion and the spilled registers around it
+// were in the loop): 0.92 PFLOP/s where sessions are alike.  There vector instructions
+// take 57% of the clocks and the matrix cores 34%, and the two do not overlap on a SIMD,
+// though one product stands beside four vector instructions in the loop: what is left is
+// an exponential, a multiply-add and an addition for each score.
 #include "kv_tile.h"
 
 namespace sph {

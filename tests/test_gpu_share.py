@@ -115,6 +115,18 @@ def test_levels_of_groups():
     check(t, 2, [3, 3, 3], slots=[-1, 4, 99])
 
 
+def test_little_in_common_of_all_and_much_of_some():
+    # one page of all three is worth no segment; two of them share 300 tokens more
+    t = Text(np.random.default_rng(21), 4, 40, 120, 1, 64, 16)
+    t.write([20, 0, 0, 0])
+    t.fork([0, 0], [1, 2])
+    t.write([310, 40, 0, 5])
+    t.fork([0], [2])
+    t.write([4, 4, 9, 4])
+    check(t, 4, [3, 2, 3, 1], seen=True)
+    check(t, 4, [3, 2, 3, 1], window=200)
+
+
 @pytest.mark.parametrize("n", [1, 2, 3, 64, 65, 130])
 def test_numbers_of_sessions(n):
     t = Text(np.random.default_rng(n), n, 24, 24 * n + 20, 1, 64, 16)
