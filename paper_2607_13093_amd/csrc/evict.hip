@@ -384,7 +384,7 @@ struct MovedBlock {
 // Waves of a workgroup, a block of tokens each at a time: two where there are many
 // workgroups, which leaves more of them room (8192 units of 64 dimensions: 2.2 GB in 442 us,
 // 5.0 TB/s, 482 with eight waves), eight where few have to take a slot's tokens faster
-// (1024 units of 128 dimensions 43 -> 38 us).  Two blocks a wave cost registers and
+// (1024 units of 128 dimensions 43 -> 38 us; 43 again with sixteen).  Two blocks a wave cost registers and
 // starts: 527 us.
 constexpr int64_t kManyUnits = 4096;
 
