@@ -49,7 +49,7 @@ struct SharePlace {
 // row `slot`, which holds `len` of them; place `part` of each row's parts.
 struct ShareItem {
   int32_t first, members, tile, from, to, part;
-  int32_t flags;  // 1: no other tile reads the tokens, 2: of one session
+  int32_t flags;  // 1: no other tile reads the tokens, 2: a tile of few rows
   int32_t slot;
 };
 
@@ -64,7 +64,7 @@ struct ShareHead {
 struct ShareSizes {
   int levels, parts;  // segments of a path that are shared at most, parts of a row
   int extra;          // parts beyond one for each segment of a path
-  int mt[2], wt;      // row tiles of a wave on shared segments and on own ones, waves that share them
+  int mt[2], wt;      // row tiles of a wave on segments of many rows and of few (own ones), waves that share them
   int rows[2];        // of a tile of an item
   int slots;          // workgroups that run at a time
   float us[2];        // of one of them for a token of an item
@@ -365,6 +365,7 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
   // Shares: each wave tries a length, in time, and what all items then take, an item's own
   // time with their tokens'.
   const int RG = a.kv.R * a.group, row_shift[2] = {__ffs(a.z.rows[0]) - 1, __ffs(a.z.rows[1]) - 1};
+  auto kind_of = [&](int members) { return members == 1 || members * RG <= a.z.rows[1]; };  // 1: few rows
   auto tiles_of = [&](int members, int kind) { return (int)(((uint32_t)members * RG + a.z.rows[kind] - 1) >> row_shift[kind]); };
   const int room = a.z.extra > 0 ? (longest + a.z.extra - 1) / a.z.extra : longest;
   auto chunk_of = [&](int kind, int candidate) {
@@ -378,30 +379,31 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
   {
     const float heads = (float)a.kv.heads / (float)a.z.slots;
     float load = 0.0f, longest_us = 0.0f;
+    const int chunk[2] = {chunk_of(0, wave), chunk_of(1, wave)};
 #pragma nounroll
-    for (int kind = 0; kind < 2; ++kind) {
-      const int n = kind ? S : shared, c = chunk_of(kind, wave);
-      float tokens = 0.0f, items = 0.0f, most = 0.0f;
+    for (int own = 0; own < 2; ++own) {
+      const int n = own ? S : shared;
+      float us = 0.0f, items = 0.0f, most = 0.0f;
       for (int i = lane; i < n; i += 64) {
-        const ShareSeg t = kind ? ShareSeg{i, 1, alike[i], low[i]} : a.segs[i];
-        const float k = (float)tiles_of(t.members, kind);
-        const int its = t.to - t.from;
-        tokens += k * (float)its;
-        items += k * (float)((uint32_t)(its + c - 1) / (uint32_t)c);
-        most = fmaxf(most, (float)(its < c ? its : c));
+        const ShareSeg t = own ? ShareSeg{i, 1, alike[i], low[i]} : a.segs[i];
+        const int kind = kind_of(t.members), c = chunk[kind], its = t.to - t.from;
+        const float k = (float)tiles_of(t.members, kind), shares = (float)((uint32_t)(its + c - 1) / (uint32_t)c);
+        us += k * ((float)its * a.z.us[kind] + shares * a.z.item_us[kind]);
+        items += k * shares;
+        most = fmaxf(most, (float)(its < c ? its : c) * a.z.us[kind] + a.z.item_us[kind]);
       }
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) {
-        tokens += __shfl_xor(tokens, o, 64);
+        us += __shfl_xor(us, o, 64);
         items += __shfl_xor(items, o, 64);
         most = fmaxf(most, __shfl_xor(most, o, 64));
       }
-      load += (tokens * a.z.us[kind] + items * a.z.item_us[kind]) * heads;
+      load += us * heads;
       // Rounds of items: a last one that is not full has CUs with one workgroup, which is
       // done sooner.
       const float rounds = items * heads, full = floorf(rounds);
       const float last = rounds > full ? 0.4f + 0.65f * (rounds - full) : 0.0f;
-      longest_us = fmaxf(longest_us, (most * a.z.us[kind] + a.z.item_us[kind]) * (full + last));
+      longest_us = fmaxf(longest_us, most * (full + last));
     }
     if (lane == 0) s_us[wave] = fmaxf(load, longest_us);
   }
@@ -417,11 +419,10 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
   int made = 0;
 #pragma nounroll
   for (int level = 0; level <= levels; ++level) {
-    const int kind = level == levels;
-    const int lo = kind || level == 0 ? 0 : s_ends[level - 1], hi = kind ? S : s_ends[level];
-    const uint32_t c = chunk[kind];
+    const bool own = level == levels;
+    const int lo = own || level == 0 ? 0 : s_ends[level - 1], hi = own ? S : s_ends[level];
     auto segment = [&](int i) {
-      if (!kind) return a.segs[i];
+      if (!own) return a.segs[i];
       const int at = (int)(key[i] & 4095);
       return ShareSeg{at, 1, alike[at], low[at]};
     };
@@ -432,6 +433,8 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
       ShareSeg t{0, 0, 0, 0};
       if (i < hi) {
         t = segment(i);
+        const int kind = kind_of(t.members);
+        const uint32_t c = chunk[kind];
         shares = (uint32_t)(t.to - t.from + c - 1) / c;
         n = tiles_of(t.members, kind) * shares;
         part_of[i - lo] = count[t.first];
@@ -439,7 +442,7 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
       const int at = sum + sum_before(n, &all);
       if (i < hi) before[i - lo] = at;
       sum += all;
-      if (kind) {
+      if (own) {
         if (i < hi) count[t.first] = (uint16_t)(count[t.first] + shares);
       } else {  // (a segment's members by a wave)
         const int mine = hi - i0 - wave * 64 < 64 ? hi - i0 - wave * 64 : 64;
@@ -459,7 +462,8 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
         else past = mid;
       }
       const ShareSeg t = segment(lo + i);
-      const uint32_t nt = tiles_of(t.members, kind), rest = x - before[i];
+      const int kind = kind_of(t.members);
+      const uint32_t c = chunk[kind], nt = tiles_of(t.members, kind), rest = x - before[i];
       const uint32_t share = rest / nt, tile = rest - share * nt;
       const int64_t to = (int64_t)t.from + (int64_t)(share + 1) * c;
       if (made + x < a.z.cap)
