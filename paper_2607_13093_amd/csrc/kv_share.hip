@@ -22,7 +22,7 @@
 // plain call, which reads and converts the document 16 times, 200).  Bound by issue:
 // vector instructions 57% of the clocks, matrix cores 35%, one after the other (256
 // windows behind one prompt: 500 us, as much as the plain call's, whose tiles of 64 rows
-// are as full).  The plan takes 14 us for two sessions and 35 for 256, once for all layers.
+// are as full).  The plan takes 16 us for two sessions and 33 for 256, once for all layers.
 #include "kv_tile.h"
 
 namespace sph {
@@ -80,7 +80,6 @@ struct SharePlanArgs {
   ShareHead* head;
   SharePlace* order; // [S]: sessions, those of a segment side by side
   int32_t* parts;    // [S]: parts of a session's rows
-  ShareSeg* segs;    // [(levels + 1) S], scratch
   ShareItem* items;  // [cap]
 };
 
@@ -215,11 +214,14 @@ __device__ __forceinline__ void compare_rows(const Alike& a, int S) {
   }
 }
 
-constexpr int plan_lds(int n2) { return 50 * n2 + 16; }
+// 50 bytes a session, and as many segments as two sessions each can have
+constexpr int plan_lds(int n2) { return 50 * n2 + 16 + kShareLevels * n2 / 2 * (int)sizeof(ShareSeg); }
+static_assert(plan_lds(kShareSessions) + 1024 <= 160 * 1024, "LDS of a plan");
 
 __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a, int n2) {
   extern __shared__ __align__(16) uint8_t smem[];
-  uint64_t* key = reinterpret_cast<uint64_t*>(smem);           // [n2] by place: group, page, session
+  ShareSeg* segs = reinterpret_cast<ShareSeg*>(smem);          // [3 n2 / 2] those that several sessions hold
+  uint64_t* key = reinterpret_cast<uint64_t*>(segs + kShareLevels * n2 / 2);  // [n2] by place: group, page, session
   int32_t* limit = reinterpret_cast<int32_t*>(key + n2);       // [n2] by session: pages that may be shared
   int32_t* slot = limit + n2;                                  // by session: its row of the table
   int32_t* base = slot + n2;                                   // by session: position of its first row
@@ -322,7 +324,7 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
           const int64_t lowest = (int64_t)low[g] - a.window + 1;
           if (lowest > seen) seen = lowest < to ? (int)lowest & ~(kKvBlock - 1) : to;
         }
-        a.segs[before + made + at] = ShareSeg{first[g], members, seen, to};
+        segs[before + made + at] = ShareSeg{first[g], members, seen, to};
       }
       if (g < groups) low[g] = take;
       made += all;
@@ -385,7 +387,7 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
       const int n = own ? S : shared;
       float us = 0.0f, items = 0.0f, most = 0.0f;
       for (int i = lane; i < n; i += 64) {
-        const ShareSeg t = own ? ShareSeg{i, 1, alike[i], low[i]} : a.segs[i];
+        const ShareSeg t = own ? ShareSeg{i, 1, alike[i], low[i]} : segs[i];
         const int kind = kind_of(t.members), c = chunk[kind], its = t.to - t.from;
         const float k = (float)tiles_of(t.members, kind), shares = (float)((uint32_t)(its + c - 1) / (uint32_t)c);
         us += k * ((float)its * a.z.us[kind] + shares * a.z.item_us[kind]);
@@ -422,7 +424,7 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
     const bool own = level == levels;
     const int lo = own || level == 0 ? 0 : s_ends[level - 1], hi = own ? S : s_ends[level];
     auto segment = [&](int i) {
-      if (!own) return a.segs[i];
+      if (!own) return segs[i];
       const int at = (int)(key[i] & 4095);
       return ShareSeg{at, 1, alike[at], low[at]};
     };
@@ -960,15 +962,14 @@ uint32_t share_key(int d, const KvArgs& a, int group, int window, int extra) {
 }
 
 struct SharePlaces {
-  size_t order, parts, segs, items, all;
+  size_t order, parts, items, all;
 };
 SharePlaces share_places(const ShareSizes& z, int64_t S) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   SharePlaces p{};
   p.order = up(sizeof(ShareHead));
   p.parts = p.order + up(S * sizeof(SharePlace));
-  p.segs = p.parts + up(S * 4);
-  p.items = p.segs + up((z.levels + 1) * S * sizeof(ShareSeg));
+  p.items = p.parts + up(S * 4);
   p.all = p.items + up(z.cap * sizeof(ShareItem));
   return p;
 }
@@ -1030,7 +1031,6 @@ hipError_t launch_share_plan(int d, const KvArgs& kv, int q_heads, int window, i
   a.head = reinterpret_cast<ShareHead*>(base);
   a.order = reinterpret_cast<SharePlace*>(base + p.order);
   a.parts = reinterpret_cast<int32_t*>(base + p.parts);
-  a.segs = reinterpret_cast<ShareSeg*>(base + p.segs);
   a.items = reinterpret_cast<ShareItem*>(base + p.items);
   int n2 = 2;
   while (n2 < kv.n_sessions) n2 *= 2;
