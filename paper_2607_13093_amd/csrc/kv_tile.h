@@ -74,7 +74,7 @@ __device__ __forceinline__ void copy_with(uint8_t* to, const KvArgs& a, int head
     if constexpr (D >= 128) __builtin_amdgcn_global_load_lds(blk[b] + lane16, at, 16, 1024, AUX);
     if constexpr (D >= 256) {
       __builtin_amdgcn_global_load_lds(blk[b] + lane16, at, 16, 2048, AUX);
-      __builtin_amdgcn_global_load_lds(blk[b] + lane16, at, 16, 3072, AUX);
+      __builtin_amdgcn_global_load_lds(blk[b] + lane16, at, 16, 3 * 1024, AUX);
     }
   }
   lds_void_t* at = (lds_void_t*)(to + Stage<D>::kCodes);
