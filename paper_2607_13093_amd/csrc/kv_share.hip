@@ -119,7 +119,11 @@ __device__ __forceinline__ void sort_keys(uint64_t* key, int n) {
     int below = 0;
     if (i < n) {
 #pragma unroll 8
-      for (int k = quarter; k < n; k += 4) below += key[k] < mine;
+      for (int k = 2 * quarter; k < n; k += 8) {
+        typedef uint64_t u64x2_t __attribute__((ext_vector_type(2)));
+        const u64x2_t two = *reinterpret_cast<const u64x2_t*>(key + k);
+        below += (two[0] < mine) + (two[1] < mine);
+      }
     }
     below += __shfl_xor(below, 1, 64);
     below += __shfl_xor(below, 2, 64);
@@ -151,13 +155,16 @@ struct Alike {
   const uint16_t *group, *first;
   const int32_t* table;
   int64_t ld_table;
+  int max_pages;
 };
 
 // Each session's row against its group's first from the place after `depth` on, up to
 // alike[group], which is lowered to the first place where they differ.  A wave takes M
-// sessions at a time, 64 COLS places of each, so that their loads are on their way together.
+// sessions at a time, 256 COLS places of each, four a lane, so that their loads are on their
+// way together.  (Places from `c` on are compared, those before are alike.)
 template <int M, int COLS>
 __device__ __forceinline__ void compare_rows(const Alike& a, int S) {
+  typedef int32_t places_t __attribute__((ext_vector_type(4), aligned(4)));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   for (int at0 = wave; at0 < S; at0 += 16 * M) {
     // lane m looks up session m
@@ -185,7 +192,13 @@ __device__ __forceinline__ void compare_rows(const Alike& a, int S) {
       y[m] = a.table + of_lane(row_y, m);
     }
     while (open) {
-      int32_t p[M][COLS], q[M][COLS];
+      places_t p[M][COLS], q[M][COLS];
+      int col[COLS];  // the last places of a row again for those past it
+#pragma unroll
+      for (int i = 0; i < COLS; ++i) {
+        const int64_t to = (int64_t)c + i * 256 + lane * 4;
+        col[i] = to < a.max_pages - 4 ? (int)to : a.max_pages - 4;
+      }
       const int ends = *(volatile const int32_t*)&a.alike[group];  // at most a row's places
       int end[M];
 #pragma unroll
@@ -193,10 +206,9 @@ __device__ __forceinline__ void compare_rows(const Alike& a, int S) {
         end[m] = open >> m & 1 ? __builtin_amdgcn_readlane(ends, m) : 0;
 #pragma unroll
         for (int i = 0; i < COLS; ++i)
-          if (c + i * 64 < end[m]) {
-            const int col = c + i * 64 + lane < end[m] ? c + i * 64 + lane : end[m] - 1;
-            p[m][i] = x[m][col];
-            q[m][i] = y[m][col];
+          if (c + i * 256 < end[m]) {
+            p[m][i] = *reinterpret_cast<const places_t*>(x[m] + col[i]);
+            q[m][i] = *reinterpret_cast<const places_t*>(y[m] + col[i]);
           }
       }
 #pragma unroll
@@ -204,13 +216,33 @@ __device__ __forceinline__ void compare_rows(const Alike& a, int S) {
         int differs = kKvMost;
 #pragma unroll
         for (int i = COLS - 1; i >= 0; --i)
-          if (c + i * 64 < end[m] && p[m][i] != q[m][i]) differs = c + i * 64 + lane;
-        const bool any = __any(differs != kKvMost);
-        if (differs != kKvMost) atomicMin(&a.alike[__builtin_amdgcn_readlane(group, m)], differs);
-        if (any || c + COLS * 64 >= end[m]) open &= ~(1u << m);
+          if (c + i * 256 < end[m]) {
+            const places_t d = p[m][i] ^ q[m][i];
+            const uint64_t others = __ballot((d[0] | d[1] | d[2] | d[3]) != 0);
+            if (others) {
+              const int mine = col[i] + (d[0] ? 0 : d[1] ? 1 : d[2] ? 2 : 3);
+              differs = __builtin_amdgcn_readlane(mine, __builtin_ctzll(others));
+            }
+          }
+        // (one lane: 64 atomics on one place take 64 turns, 45 us for 196 sessions)
+        if (differs != kKvMost && lane == 0) atomicMin(&a.alike[__builtin_amdgcn_readlane(group, m)], differs);
+        if (differs != kKvMost || c + COLS * 256 >= end[m]) open &= ~(1u << m);
       }
-      c += COLS * 64;
+      c += COLS * 256;
     }
+  }
+}
+// The same where rows have fewer than four places: a session a thread.
+__device__ __forceinline__ void compare_short_rows(const Alike& a, int S) {
+  for (int at = threadIdx.x; at < S; at += kPlanThreads) {
+    const int group = a.group[at];
+    const int32_t *x = a.table + a.slot[(int)(a.key[a.first[group]] & 4095)] * a.ld_table, *y = a.table + a.slot[(int)(a.key[at] & 4095)] * a.ld_table;
+#pragma nounroll
+    for (int c = a.depth[at] + 1; c < a.max_pages; ++c)
+      if (x[c] != y[c]) {
+        atomicMin(&a.alike[group], c);
+        break;
+      }
   }
 }
 
@@ -298,10 +330,11 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
     }
     __syncthreads();
     // pages named alike by a group's first session and each of the others
-    const Alike all{key, slot, depth, alike, group, first, a.kv.table, a.kv.ld_table};
-    if (S <= 16) compare_rows<1, 16>(all, S);
-    else if (S <= 64) compare_rows<4, 4>(all, S);
-    else compare_rows<16, 1>(all, S);
+    const Alike all{key, slot, depth, alike, group, first, a.kv.table, a.kv.ld_table, a.kv.max_pages};
+    if (a.kv.max_pages < 4) compare_short_rows(all, S);
+    else if (S <= 16) compare_rows<1, 4>(all, S);
+    else if (S <= 64) compare_rows<4, 2>(all, S);
+    else compare_rows<8, 1>(all, S);
     __syncthreads();
     // segments of the level, in the order of their groups
     const int before = s_segs;

@@ -120,6 +120,38 @@ def test_thousands_of_sessions(n):
     check(t, 2, [1 + i % 2 for i in range(n)], slots=order, window=70)
 
 
+@pytest.mark.parametrize("n", [3, 20, 70])
+@pytest.mark.parametrize("places", [1, 2, 3, 4, 5, 7])
+def test_rows_of_few_places(places, n):
+    # tables of as many pages as the longest slot holds, the last row of them at the end of its memory
+    t = Text(np.random.default_rng(places), n, places, places * n + 4, 1, 64, 64)
+    t.write([max(64 * (places - 1), 40)] + [0] * (n - 1))
+    t.fork([0] * (n - 1), list(range(1, n)))
+    t.write([1 + i % 20 for i in range(n)])
+    *_, plan = check(t, 2, [1 + i % 2 for i in range(n)])
+    assert host(plan.buffer)[:16].view(np.int32)[3] == (64 * (places - 1) * (n - 1) >= 256)
+
+
+@pytest.mark.parametrize("n", [4, 40, 100])
+def test_rows_differ_at_any_place(n):
+    # sessions leave their prompt at places all along its 600 pages, some but at the last
+    rng = np.random.default_rng(n)
+    t = Text(rng, n, 620, 620 * 3 + 3 * n, 1, 64, 16)
+    t.write([9601] + [0] * (n - 1))
+    t.fork([0] * (n - 1), list(range(1, n)))
+    t.write([1 + i % 3 for i in range(n)])
+    base = host(t.c.table)
+    table, other = base.copy(), base[0].copy()
+    other[:600] = np.setdiff1d(np.arange(t.c.n_pages), base)[:600]
+    t.c.pool[:, other[:600]] = t.c.pool[:, base[0, :600]]  # the same text on pages of its own
+    at = np.unique(np.concatenate([rng.integers(0, 600, n - 1), [599, 3, 255, 256]]))[-(n - 1):]
+    for s in range(1, n):
+        p = at[s % len(at)]
+        table[s, p:600] = other[p:600]
+    t.c.table.copy_(torch.from_numpy(table))
+    check(t, 1, [1] * n, seen=True)
+
+
 def test_weights_and_eviction_of_many_slots():
     n = 3000
     t = Text(np.random.default_rng(7), n, 6, 4 * n, 1, 64, 16)
