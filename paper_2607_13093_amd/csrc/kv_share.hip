@@ -69,6 +69,7 @@ struct ShareSizes {
   int slots;          // workgroups that run at a time
   float us[2];        // of one of them for a token of an item
   float item_us[2];   // and for an item, its outputs' way out and back with it
+  float read_us;      // for a token's way from memory, all workgroups at it
   int cap;            // items at most
 };
 
@@ -299,6 +300,19 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
   __syncthreads();
   longest = s_longest;
 
+  const int RG = a.kv.R * a.group, row_shift[2] = {__ffs(a.z.rows[0]) - 1, __ffs(a.z.rows[1]) - 1};
+  auto kind_of = [&](int members) { return members == 1 || members * RG <= a.z.rows[1]; };  // 1: few rows
+  auto tiles_of = [&](int members, int kind) { return (int)(((uint32_t)members * RG + a.z.rows[kind] - 1) >> row_shift[kind]); };
+  // Whether tokens are better read once for tiles of all members' rows, with a part more for
+  // each of them, than beside each session's own.  (16 tokens that 32 sessions of eight rows
+  // and 4931 tokens hold in common, four layers: shared 248 us, left to the sessions 202; where
+  // the two accounts are within a factor of two of each other, calls took as long either way.)
+  auto worth = [&](int members, int tokens) {
+    const int kind = kind_of(members);
+    const float n = (float)tokens, shared = (float)tiles_of(members, kind) * (n * a.z.us[kind] + a.z.item_us[kind]) + n * a.z.read_us;
+    return shared < 2.0f * n * (float)members * ((float)tiles_of(1, 1) * a.z.us[1] + a.z.read_us);
+  };
+
   // (loops that are not unrolled: run once, code costs its way from memory)
   int groups = 1, levels = 0;
 #pragma nounroll
@@ -347,7 +361,8 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
         members = first[g + 1] - first[g];
         from = start[first[g]] << shift;
         to = alike[g] << shift;
-        take = members > 1 && count[first[g]] < a.z.levels && (int64_t)(to - from) * (members - 1) >= kShareWorth;
+        take = members > 1 && count[first[g]] < a.z.levels && (int64_t)(to - from) * (members - 1) >= kShareWorth &&
+               worth(members, to - from);
       }
       int all = 0;
       const int at = sum_before(take ? 1 : 0, &all);
@@ -399,9 +414,6 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
 
   // Shares: each wave tries a length, in time, and what all items then take, an item's own
   // time with their tokens'.
-  const int RG = a.kv.R * a.group, row_shift[2] = {__ffs(a.z.rows[0]) - 1, __ffs(a.z.rows[1]) - 1};
-  auto kind_of = [&](int members) { return members == 1 || members * RG <= a.z.rows[1]; };  // 1: few rows
-  auto tiles_of = [&](int members, int kind) { return (int)(((uint32_t)members * RG + a.z.rows[kind] - 1) >> row_shift[kind]); };
   const int room = a.z.extra > 0 ? (longest + a.z.extra - 1) / a.z.extra : longest;
   auto chunk_of = [&](int kind, int candidate) {
     const float us = __builtin_amdgcn_exp2f(2.0f + 0.42f * candidate);  // 4 ... 315
@@ -977,6 +989,7 @@ ShareSizes share_sizes(int d, int64_t S, int64_t R, int64_t heads, int64_t group
   // dimensions: two workgroups 84 us).
   for (int k = 0; k < 2; ++k)
     z.us[k] = (float)((4.0 * (0.9 * d + 20 + 36 * z.mt[k]) + (32.0 + d / 2.0) * z.mt[k]) * 1.85 / 2100 * 2 / (32 * z.wt));
+  z.read_us = (float)(17.0 / 16 * d * z.slots / 5.5e6);  // at 5.5 TB/s
   // an item, and half of its outputs' way out and back, at 4 TB/s
   for (int k = 0; k < 2; ++k) z.item_us[k] = (float)(kShareItem + (double)z.rows[k] * (d * 4 + 8) * z.slots / 4e6);
   // A level's segments have a tile more each than their rows fill, and shares.

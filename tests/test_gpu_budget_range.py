@@ -132,6 +132,15 @@ def test_rows_of_few_places(places, n):
     assert host(plan.buffer)[:16].view(np.int32)[3] == (64 * (places - 1) * (n - 1) >= 256)
 
 
+def test_what_is_not_worth_a_part_is_left_to_the_sessions():
+    # 32 tokens in common of 40 sessions with 40 rows each: read beside each session's own
+    t = Text(np.random.default_rng(11), 40, 8, 200, 1, 64, 16)
+    t.write([32] + [0] * 39)
+    t.fork([0] * 39, list(range(1, 40)))
+    t.write([5 + i % 9 for i in range(40)])
+    check(t, 8, [5] * 40, seen=False)
+
+
 @pytest.mark.parametrize("n", [4, 40, 100])
 def test_rows_differ_at_any_place(n):
     # sessions leave their prompt at places all along its 600 pages, some but at the last

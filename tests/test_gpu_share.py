@@ -154,7 +154,7 @@ def test_long_documents_are_cut(d, page, long):
 @pytest.mark.parametrize("d,page,rows", [(64, 16, 300), (128, 16, 200), (256, 32, 130)])
 def test_prompts_behind_a_common_one(d, page, rows):
     t = Text(np.random.default_rng(rows), 3, 60, 200, 2, d, page)
-    t.write([200, 0, 0])
+    t.write([640, 0, 0])
     t.fork([0, 0], [1, 2])
     t.write([rows, rows - 7, 20])
     check(t, 2, [rows, rows - 7, 20], seen=True)
@@ -166,8 +166,8 @@ def test_prompts_behind_a_common_one(d, page, rows):
 @pytest.mark.parametrize("d,window", [(64, 0), (128, 0), (256, 0), (64, 90)])
 def test_many_rows_are_not_cut(d, window):
     # more than 65536 rows of a head: one shared level, no shares of a segment; against the plain call
-    t = Text(np.random.default_rng(d), 3, 80, 200, 1, d, 16)
-    t.write([300, 0, 0])
+    t = Text(np.random.default_rng(d), 3, 90, 220, 1, d, 16)
+    t.write([640, 0, 0])
     t.fork([0, 0], [1, 2])
     t.write([700, 699, 650])
     q, _ = bf16(np.random.default_rng(40), 3 * 700, 32, d)
