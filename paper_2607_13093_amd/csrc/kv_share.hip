@@ -18,10 +18,10 @@
 // that what own tokens wait for memory hides behind the products of shared ones; a second
 // joins the parts.
 //
-// 16 windows of five rows on one document of 65504 tokens: 127 us (0.68 PFLOP/s; the
-// plain call, which reads and converts the document 16 times, 200).  Bound by issue:
+// 16 windows of five rows on one document of 65504 tokens: 128 us (0.67 PFLOP/s; the
+// plain call, which reads and converts the document 16 times, 185).  Bound by issue:
 // vector instructions 57% of the clocks, matrix cores 35%, one after the other (256
-// windows behind one prompt: 500 us, as much as the plain call's, whose tiles of 64 rows
+// windows behind one prompt: 495 us, the plain call 448: its tiles of 64 rows
 // are as full).  The plan takes 16 us for two sessions and 33 for 256, once for all layers.
 #include "kv_tile.h"
 
