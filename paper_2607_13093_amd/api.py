@@ -675,7 +675,8 @@ def kv_attend(cache: KvCache, layer: int, q: torch.Tensor, rows_per_session: int
 
 class KvSharePlan:
     """What sessions hold in common, as kv_share found it: for kv_attend_shared on the
-    same cache, until its tables or lengths change."""
+    same cache, until its tables or lengths change.  Calls go by the sizes of when it was
+    made: its attributes are fixed, but for the rows and slots that kv_share was given last."""
 
     def __init__(self, cache: KvCache, q_heads: int, n_sessions: int, rows_per_session: int,
                  rows: Optional[torch.Tensor], slots: Optional[torch.Tensor], window: int, max_len: int):
@@ -686,6 +687,12 @@ class KvSharePlan:
         sizes = cache.ptr, self.q_heads, self.n_sessions, self.rows_per_session, self.max_len
         self.bytes, self.workspace_bytes = int(lib.sph_kv_share_bytes(*sizes)), int(lib.sph_kv_attend_shared_workspace(*sizes))
         self.buffer = torch.empty(max(self.bytes, 1), dtype=torch.uint8, device=cache.device)
+        self._fixed = frozenset(self.__dict__) - {"rows", "slots"}
+
+    def __setattr__(self, name, value):
+        if name in self.__dict__.get("_fixed", ()):
+            raise AttributeError(f"KvSharePlan.{name} is fixed: make another plan")
+        super().__setattr__(name, value)
 
 
 def kv_share(cache: KvCache, q_heads: int, rows_per_session: int, rows: Optional[torch.Tensor] = None,
