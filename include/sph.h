@@ -484,7 +484,9 @@ int sph_kv_attend(const sph_kv_cache* cache, int64_t layer, const void* q, int64
  * max_len      as in sph_kv_attend
  * plan         device memory of sph_kv_share_bytes, 16-byte aligned.  Calls that share
  *              one must not overlap (it holds the calls' work queue).
- * workspace    >= sph_kv_attend_shared_workspace bytes, 16-byte aligned
+ * workspace    >= sph_kv_attend_shared_workspace bytes, 16-byte aligned: 4 head_dim + 8
+ *              for each row, head and part of its tokens, of which few rows have up to
+ *              60, in all a GiB, or two parts of each where those are more
  */
 size_t sph_kv_share_bytes(const sph_kv_cache* cache, int64_t q_heads, int64_t n_sessions,
                           int64_t R, int64_t max_len);

@@ -34,6 +34,7 @@ constexpr int kShareLeast = 256;  // and at least
 // Tokens whose reading a segment has to save: a part of every row costs about as much.
 constexpr int kShareWorth = 256;
 constexpr double kShareItem = 4.0;  // us of an item beside its tokens and outputs, where another hides the rest
+constexpr int64_t kShareRoom = int64_t(1) << 30;  // bytes of all rows' parts, where two of each fit
 
 // Tokens from ... to - 1 of `members` sessions from place `first` of the order.
 struct ShareSeg {
@@ -969,9 +970,12 @@ ShareSizes share_sizes(int d, int64_t S, int64_t R, int64_t heads, int64_t group
   z.mt[0] = d == 256 ? 2 : 4;
   z.wt = d == 256 ? 8 : 4;
   z.mt[1] = RG <= 16 ? 1 : d == 256 || RG <= 32 ? 2 : 4;
-  // Parts of a row beyond one for each segment: as many as some hundred megabytes of them
-  // allow, so that few rows can be cut often.
+  // Parts of a row beyond one for each segment, so that few rows can be cut often; for more
+  // rows than kShareRoom has places for, fewer segments too, at least a shared one and the
+  // row's own (four prompts of 4095 rows of 64 heads of 256 dimensions behind 4096 tokens: 2.2 GB
+  // for 6.5, 9.8 ms either way; eight of 1000 rows in two branches 1.1 for 3.2, 5.9 ms for 6.5).
   const int64_t rows = S * RG * heads, shares = (max_len + kShareLeast - 1) / kShareLeast;
+  const int64_t places = kShareRoom / (rows * (8 + 4 * d));
   if (S * RG > 65536) {  // prompts: nothing to cut
     z.levels = 1;
     z.extra = 0;
@@ -981,6 +985,8 @@ ShareSizes share_sizes(int d, int64_t S, int64_t R, int64_t heads, int64_t group
     z.extra = (int)(most < 2 ? 2 : most > 56 ? 56 : most);
     if (z.extra > shares) z.extra = (int)shares;
   }
+  if (z.levels > places - 1) z.levels = places > 2 ? (int)places - 1 : 1;
+  if (z.extra > places - 1 - z.levels) z.extra = places - 1 > z.levels ? (int)places - 1 - z.levels : 0;
   z.parts = z.levels + 1 + z.extra;
   for (int k = 0; k < 2; ++k) z.rows[k] = 16 * z.mt[k];
   z.slots = kCUs * (d == 64 ? share_resident(64, 4, 4, 4) : d == 128 ? share_resident(128, 4, 4, 4) : share_resident(256, 2, 2, 8));

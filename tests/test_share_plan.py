@@ -29,3 +29,25 @@ def test_a_plan_is_fixed():
             setattr(plan, name, was)
         assert getattr(plan, name) is was
     plan.rows = plan.slots = torch.zeros(3, dtype=torch.int32)  # those of the next kv_share
+
+
+SIZES = [  # kv heads, group, d, sessions, R
+    (8, 4, 128, 1, 1), (1, 1, 64, 2, 1), (8, 4, 128, 16, 5), (8, 8, 128, 256, 8), (16, 4, 256, 256, 9),
+    (8, 5, 128, 4, 2047), (64, 1, 256, 4, 4095), (64, 1, 256, 3, 1811), (64, 1, 256, 3, 1355), (64, 1, 256, 3, 1084),
+    (128, 1, 64, 4, 8191), (16, 4, 256, 4, 4095), (8, 8, 256, 2048, 3), (1, 32, 64, 3, 700), (2, 1, 256, 3, 1 << 23),
+    (32768, 1, 128, 2048, 1),
+]
+
+
+@pytest.mark.parametrize("max_len", [0, 1, 300, 9000])
+@pytest.mark.parametrize("case", range(len(SIZES)))
+def test_parts_stay_within_their_bound(case, max_len):
+    # 4 d + 8 bytes a row, head and part: at most a GiB, or two parts where those are more
+    lib = _lib.load()
+    heads, group, d, n, R = SIZES[case]
+    c = described(kv_heads=heads, head_dim=d)
+    need = lib.sph_kv_attend_shared_workspace(ctypes.addressof(c), heads * group, n, R, max_len)
+    part = n * R * heads * group * (4 * d + 8)
+    assert 2 * part <= need <= max(1 << 30, 2 * part) + 256
+    assert need <= 60 * part + 256
+    assert lib.sph_kv_share_bytes(ctypes.addressof(c), heads * group, n, R, max_len) > 0
