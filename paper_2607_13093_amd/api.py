@@ -723,7 +723,9 @@ def kv_attend_shared(cache: KvCache, layer: int, q: torch.Tensor, plan: KvShareP
                      want_lse: bool = False, workspace: Optional[torch.Tensor] = None, out=None):
     """kv_attend of the plan's sessions, rows and window, pages that sessions hold in
     common read once for all of them.  Returns what kv_attend does, equal up to the order
-    of sums.  workspace: plan.workspace_bytes, 16-byte aligned."""
+    of sums; faster where eight sessions or more hold about ten thousand tokens or more in
+    common, else mostly slower (include/sph.h).  workspace: plan.workspace_bytes (up to a GiB, or two
+    parts of each row where those are more), 16-byte aligned."""
     lib = _lib.load()
     dev = cache.device
     if plan.cache is not cache:
@@ -854,7 +856,7 @@ def pages_evict(cache: KvCache, weights: torch.Tensor, keep: torch.Tensor, first
     those up to its last page that other slots hold too, and of the others those with
     the largest weights (fp32 [slots, >= max_pages * page_tokens], as kv_weigh adds
     them up; equal ones by position).  They move together, in order, in every layer, and
-    pages past them are given back.  Returns (the kept tokens' weights, their former
+    pages past them are given back; positions count held tokens from then on.  Returns (the kept tokens' weights, their former
     positions int32 or None): `weights` itself, changed in place, and with want_kept a
     new tensor with -1 past the length, or `out` = (weights, positions or None)."""
     lib = _lib.load()

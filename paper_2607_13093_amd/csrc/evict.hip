@@ -14,8 +14,10 @@
 // Moving is bound by memory: 64 slots of up to 4096 tokens in 16 layers, 2.2 GB read
 // and written in 445 us, 5.0 TB/s, a copy's rate.  Where a quarter of the tokens stays,
 // the lines that hold them are read nearly whole (a value's codes lie between those of
-// three other tokens): 569 MB kept and written in 197 us.  Choosing is one workgroup's
-// latency, 9 us for 700 tokens and 27 for 16384.
+// three other tokens): 569 MB kept and written in 197 us.  Where slots, layers and heads are
+// few a unit's chunks follow one another: half of 16384 tokens of one layer takes 116 us with
+// one head and 125 with eight, 188 in 32 layers, choosing 27 of it (one workgroup's latency, 9
+// for 700 tokens).
 #include "kv_cache.h"
 
 namespace sph {

@@ -18,11 +18,15 @@
 // that what own tokens wait for memory hides behind the products of shared ones; a second
 // joins the parts.
 //
-// 16 windows of five rows on one document of 65504 tokens: 128 us (0.67 PFLOP/s; the
-// plain call, which reads and converts the document 16 times, 185).  Bound by issue:
-// vector instructions 57% of the clocks, matrix cores 35%, one after the other (256
-// windows behind one prompt: 495 us, the plain call 448: its tiles of 64 rows
-// are as full).  The plan takes 16 us for two sessions and 33 for 256, once for all layers.
+// 16 windows of five rows on one document of 65504 tokens: 129 us (0.67 PFLOP/s; the
+// plain call, which reads and converts the document 16 times, 185): vector instructions
+// 47% of the clocks, matrix cores 28%, one after the other, CUs busy 86%.  256 windows of
+// eight rows behind one prompt of 4096: 501 us, 57% and 35%, bound by issue; the plain
+// call, whose tiles of 64 rows are as full, 448.  The plan takes 16 us for two sessions and
+// 30 for 256, once for all layers.  Most calls are faster by the plain call: beside a plan
+// that is there already, 40 of 45 (15 of them share nothing: 1.4 times as long at the
+// median, 2.0 at most): every row's parts go out in fp32 and come back for the join, and
+// few rows run at the occupancy of many.
 #include "kv_tile.h"
 
 namespace sph {
@@ -33,7 +37,11 @@ constexpr int kShareStep = 128;   // tokens that shares are multiples of
 constexpr int kShareLeast = 256;  // and at least
 // Tokens whose reading a segment has to save: a part of every row costs about as much.
 constexpr int kShareWorth = 256;
-constexpr double kShareItem = 4.0;  // us of an item beside its tokens and outputs, where another hides the rest
+// us of an item beside its tokens and outputs, where another hides the rest.  This and the
+// other constants of the account of time are fitted: with them its choice of a length is
+// within 3% of the best of the sixteen that it tries (one row of 32 sessions on 2037 tokens,
+// five of 16 on 65504, eight of 256 on 4096, a tree of six times eight sessions).
+constexpr double kShareItem = 4.0;
 constexpr int64_t kShareRoom = int64_t(1) << 30;  // bytes of all rows' parts, where two of each fit
 
 // Tokens from ... to - 1 of `members` sessions from place `first` of the order.
@@ -304,10 +312,13 @@ __global__ __launch_bounds__(kPlanThreads, 4) void k_share_plan(SharePlanArgs a,
   const int RG = a.kv.R * a.group, row_shift[2] = {__ffs(a.z.rows[0]) - 1, __ffs(a.z.rows[1]) - 1};
   auto kind_of = [&](int members) { return members == 1 || members * RG <= a.z.rows[1]; };  // 1: few rows
   auto tiles_of = [&](int members, int kind) { return (int)(((uint32_t)members * RG + a.z.rows[kind] - 1) >> row_shift[kind]); };
-  // Whether tokens are better read once for tiles of all members' rows, with a part more for
-  // each of them, than beside each session's own.  (16 tokens that 32 sessions of eight rows
-  // and 4931 tokens hold in common, four layers: shared 248 us, left to the sessions 202; where
-  // the two accounts are within a factor of two of each other, calls took as long either way.)
+  // Whether tokens are read once for tiles of all members' rows, with a part more for each of
+  // them, or beside each session's own: shared unless this account has it take twice as long.
+  // (16 tokens that 32 sessions of eight rows and 4931 tokens hold in common, four layers:
+  // shared 248 us, left to the sessions 202.  With 1, 1.5 or 3 for the factor calls took as long
+  // as with two.  The account leaves out what the parts cost the join and the sessions' own
+  // items: of 30 calls with a segment, sharing none at all was more than 3% faster in 11, most
+  // where the common part is short or rows are few (53.6 -> 41.8 us), and slower in 9 (344 -> 546).)
   auto worth = [&](int members, int tokens) {
     const int kind = kind_of(members);
     const float n = (float)tokens, shared = (float)tiles_of(members, kind) * (n * a.z.us[kind] + a.z.item_us[kind]) + n * a.z.read_us;

@@ -14,10 +14,13 @@
 //
 // Up to 64 rows of a head (k_weigh_few) the keys of all heads stream through rings of
 // LDS stages: 256 sessions' windows of four rows over 8192 tokens read their keys at
-// 5.2 TB/s (226 us), 64 at 4.7; the conversion of codes and the exponentials take the rest.
-// More rows (k_weigh_many) pass a head's keys held as operands in registers (330 us in
-// place of 700 for prompts when the keys' conversion and the spilled registers around it
-// were in the loop): 0.92 PFLOP/s where sessions are alike.  There vector instructions
+// 5.2 TB/s (226 us), 64 at 4.7.  Sessions of 5 to 8192 tokens leave CUs idle (busy 62%): a
+// workgroup's tokens are as many for all.  A window masks what rows do not see, its keys
+// are read all the same: four rows of 32 sessions of 65536 tokens take 223 us with a window
+// of 1024, 239 without.
+// More rows (k_weigh_many) pass a head's keys held as operands in registers, those that see
+// none of them left out (330 us in place of 700 for prompts when the keys' conversion and the
+// spilled registers around it were in the loop): 0.92 PFLOP/s where sessions are alike.  There vector instructions
 // take 57% of the clocks and the matrix cores 34%, and the two do not overlap on a SIMD,
 // though one product stands beside four vector instructions in the loop: what is left is
 // an exponential, a multiply-add and an addition for each score.
