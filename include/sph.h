@@ -456,8 +456,11 @@ int sph_kv_read(const sph_kv_cache* cache, int64_t layer, void* k, int64_t k_row
  * workspace   >= sph_kv_attend_workspace bytes for the same arguments, 16-byte
  *             aligned (NULL if that is 0)
  * Sums, maxima and the softmax are held in fp32; the weights softmax(x) enter
- * the second product as bf16.  Scores are fp32 too: a row with an x[j] above
- * about 2e38 answers NaN, an x[j] below -2e38 has no weight.
+ * the second product as bf16.  Scores are fp32 too, rounded to 2^-24 of their
+ * size: a row with an x[j] above about 2e38 answers NaN, an x[j] below -2e38 has
+ * no weight.  A row whose largest |x[j]| is past 5e8 may answer NaN before that, or as if it
+ * saw nothing: the rounding of the reference that weights are taken against is then
+ * more than fp32's exponents hold.
  */
 size_t sph_kv_attend_workspace(const sph_kv_cache* cache, int64_t q_heads, int64_t n_sessions,
                                int64_t R, int64_t window, int64_t max_len);
@@ -570,7 +573,8 @@ int sph_pages_compact(const sph_kv_cache* cache, int32_t* table_out, int64_t ld_
  *              once in a call.
  * workspace    >= sph_kv_weigh_workspace bytes for the same arguments, 16-byte aligned
  *              (NULL if that is 0)
- * Products and sums are fp32, in an order that does not depend on timing.
+ * Products and sums are fp32, in an order that does not depend on timing; the
+ * rounding of lse alone puts weights off by the factor exp(2^-24 |lse|).
  */
 size_t sph_kv_weigh_workspace(const sph_kv_cache* cache, int64_t q_heads, int64_t n_sessions,
                               int64_t R, int64_t max_len);

@@ -262,7 +262,8 @@ __device__ __forceinline__ void clear_values(KvValues<D>& v, const int (&held)[2
 // score so far, so that they stay below 2^kLate: lanes look at their own scores
 // and exchange them only when one goes past that, which is rare after the first
 // tiles.  A score past fp32 makes the row NaN (infinity less itself), one below it
-// weighs nothing.
+// weighs nothing.  The reference is a rounded product, weights are exact against it: their
+// largest is 2^(half a step of it) at most, in range up to references of 2^30 binades.
 template <int D, int MT>
 __device__ __forceinline__ void take_weights(bf16x8_t (&p)[MT], Rows<D, MT>& w, const f32x4_t (&sc)[MT][2],
                                              float scale_log2) {
